@@ -1,5 +1,6 @@
-"""Builds, in-tree: libts_attn.so (the HIP kernels and their C ABI) for gfx950 with hipcc, and
-libts_sched.so (the closed-loop session scheduler, host code only) with g++."""
+"""Builds, in-tree: libts_attn.so (the attention kernels and their C ABI) and libts_cache.so (the 8-bit
+session cache) for gfx950 with hipcc, and libts_sched.so (the closed-loop session scheduler, host code
+only) with g++."""
 import os
 import subprocess
 
@@ -11,11 +12,15 @@ LIB = os.path.join(HERE, "libts_attn.so")
 SOURCES = [os.path.join(CSRC, "attn_kernels.hip"), os.path.join(CSRC, "state_copy.hip"),
            os.path.join(CSRC, "attn_plan.cpp"), os.path.join(CSRC, "ts_attn.cpp")]
 
+CACHE_LIB = os.path.join(HERE, "libts_cache.so")
+CACHE_SOURCES = [os.path.join(CSRC, "cache_attn.hip"), os.path.join(CSRC, "cache_pages.hip"),
+                 os.path.join(CSRC, "cache_plan.cpp"), os.path.join(CSRC, "ts_cache.cpp")]
+
 SCHED_LIB = os.path.join(HERE, "libts_sched.so")
 SCHED_SOURCES = [os.path.join(CSRC, "sched.cpp")]
 # no contraction into fused multiply-adds: the scheduler's comparisons of latency gains are
 # specified in plain IEEE double arithmetic
-# only the C ABI is exported from either library
+# only the C ABI is exported from the libraries
 EXPORTS = ["-Wl,--version-script=" + os.path.join(CSRC, "exports.map")]
 GXX_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-shared", "-ffp-contract=off", "-Wall", "-Wextra",
              "-I" + INCLUDE] + EXPORTS
@@ -30,15 +35,20 @@ def hipcc():
     return os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 
-def build(out=LIB, extra_flags=()):
+def build(out=LIB, extra_flags=(), sources=SOURCES):
     """Compile every source into the shared library `out` (always recompiles); returns out."""
     tmp = out + ".tmp%d" % os.getpid()
-    cmd = [hipcc()] + HIPCC_FLAGS + list(extra_flags) + SOURCES + ["-o", tmp]
+    cmd = [hipcc()] + HIPCC_FLAGS + list(extra_flags) + list(sources) + ["-o", tmp]
     proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if proc.returncode != 0:
         raise RuntimeError("hipcc failed:\n" + proc.stdout)
     os.replace(tmp, out)
     return out
+
+
+def build_cache(out=CACHE_LIB, extra_flags=()):
+    """Compile the session cache's library `out` (always recompiles); returns out."""
+    return build(out, extra_flags, CACHE_SOURCES)
 
 
 def build_sched(out=SCHED_LIB):
@@ -54,4 +64,5 @@ def build_sched(out=SCHED_LIB):
 
 if __name__ == "__main__":
     print(build())
+    print(build_cache())
     print(build_sched())

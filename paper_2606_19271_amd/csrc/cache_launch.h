@@ -1,0 +1,96 @@
+// cache_launch.h -- internal interface between the C ABI of the session cache (ts_cache.cpp) and its
+// kernels (cache_attn.hip, cache_pages.hip).  Not installed; the public interface is include/ts_cache.h.
+#pragma once
+#include <hip/hip_runtime_api.h>
+#include <stdint.h>
+
+namespace tscache {
+
+constexpr int kPage = 64;               // tokens of a page
+constexpr int kMergeThreads = 256;      // threads per workgroup of the merge kernel
+constexpr int64_t kGridLimit = (int64_t)1 << 23;  // workgroups per launch
+
+// The pool of pages (ts_cache).
+struct Pool {
+  uint8_t* k;
+  uint8_t* v;
+  uint8_t* k_exp;
+  uint8_t* v_exp;
+  float* weight;  // null where the call has none
+  int32_t pages, H;
+};
+
+// The sessions of a call: packed rows cu[s] .. cu[s + 1] (null where the call has no rows), lens[s] cached
+// tokens in the pages table[s][..].
+struct Sessions {
+  const int32_t* cu;
+  const int32_t* table;
+  const int32_t* lens;
+  int32_t nseq, width, max_rows, max_len, total;
+};
+
+struct AttnArgs {
+  Pool pool;
+  Sessions ss;
+  const void* q;
+  void* o;
+  float* lse;       // or null
+  float* part_o;    // [n_split][total][Hq][d] (n_split > 1)
+  float* part_lse;  // [n_split][total][Hq]
+  int32_t d, G, n_split;
+  float scale;
+  int32_t cus;
+};
+
+struct WeighArgs {
+  Pool pool;
+  Sessions ss;
+  const void* q;
+  const float* lse;
+  float* out;
+  int32_t d, G;
+  float scale;
+  int32_t cus;
+};
+
+struct AppendArgs {
+  Pool pool;
+  Sessions ss;  // max_len: 64 * width
+  const void* k;
+  const void* v;
+  int32_t* new_lens;
+  int32_t d;
+};
+
+struct EvictArgs {
+  Pool pool;
+  Sessions ss;
+  const int32_t* new_table;
+  int32_t* new_lens;
+  int32_t* kept;
+  int32_t d, new_width, keep, first, last;
+};
+
+// Host-side sizes (cache_plan.cpp).
+// Query rows (tokens x G) of an attention workgroup's tile.
+int row_tile(int64_t rows);
+// Workgroups of an unsplit attention call, and of its merge kernel.
+int64_t attn_items(int32_t nseq, int32_t max_rows, int32_t H, int32_t G);
+int64_t merge_blocks(int32_t nseq, int32_t max_rows, int32_t Hq, int32_t d);
+// Page ranges per query tile when the caller leaves the choice to the library.
+int32_t auto_splits(int32_t nseq, int32_t max_rows, int32_t max_len, int32_t H, int32_t G, int32_t d,
+                    int32_t cus);
+// Bytes of workspace of a call of n page ranges: the partial lse [n][total][Hq], then O [n][total][Hq][d].
+int64_t workspace_bytes(int32_t n, int32_t total, int32_t Hq, int32_t d);
+int64_t part_o_offset(int32_t n, int32_t total, int32_t Hq);
+int64_t weigh_items(int32_t nseq, int32_t max_len, int32_t H);
+int64_t append_items(int32_t nseq, int32_t max_rows, int32_t H);
+int64_t gather_items(int32_t nseq, int32_t keep, int32_t H);
+
+hipError_t configure_kernels();
+hipError_t launch_attn(const AttnArgs& a, hipStream_t st);
+hipError_t launch_weigh(const WeighArgs& a, hipStream_t st);
+hipError_t launch_append(const AppendArgs& a, hipStream_t st);
+hipError_t launch_evict(const EvictArgs& a, hipStream_t st);
+
+}  // namespace tscache

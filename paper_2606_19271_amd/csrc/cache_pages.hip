@@ -1,0 +1,320 @@
+// cache_pages.hip -- gfx950 kernels that write the session cache's pages: append and evict.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "cache_launch.h"
+#include "cache_tile.h"
+
+namespace tscache {
+
+constexpr int kPageThreads = 256;
+constexpr int kPageWaves = kPageThreads / 64;
+
+// Largest of the workgroup's two values of every thread (buf: 2 * kPageWaves words of LDS).
+__device__ __forceinline__ void block_max2(unsigned& a, unsigned& b, unsigned* buf) {
+#pragma unroll
+  for (int m = 32; m > 0; m >>= 1) {
+    a = max(a, (unsigned)__shfl_xor((int)a, m));
+    b = max(b, (unsigned)__shfl_xor((int)b, m));
+  }
+  if ((threadIdx.x & 63) == 0) {
+    buf[threadIdx.x >> 6] = a;
+    buf[kPageWaves + (threadIdx.x >> 6)] = b;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kPageWaves; ++w) {
+    a = max(a, buf[w]);
+    b = max(b, buf[kPageWaves + w]);
+  }
+}
+
+// ---- append: one workgroup per (session, touched page, head).  A thread holds pieces of 16 channels of a
+// token (32 bytes in, 16 out), so K and V are each read once, the page's amax formed and the pieces
+// converted from registers.
+template <int D>
+__global__ void __launch_bounds__(kPageThreads)
+cache_append_kernel(Pool pool, Sessions ss, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
+                    int32_t* __restrict__ new_lens, int page_slots) {
+  constexpr int kPieces = D / 16;                           // of a token
+  constexpr int kPer = kPage * kPieces / kPageThreads;      // of a thread
+  __shared__ unsigned buf[2 * kPageWaves];
+  const int b = blockIdx.x;
+  const int h = b % pool.H, sj = b / pool.H, j = sj % page_slots, s = sj / page_slots;
+  const Session se = session_of(ss, s);
+  const bool fits = se.ok && se.rows <= ss.max_len - se.len;
+  if (j == 0 && h == 0 && threadIdx.x == 0) new_lens[s] = se.len + (fits ? se.rows : 0);
+  if (!fits) return;
+  const int p = se.len / kPage + j;                  // page of the session
+  const int old = max(0, se.len - p * kPage);        // its slots that hold older tokens
+  const int end = min(kPage, se.len + se.rows - p * kPage);
+  if (se.rows == 0 || old >= end) return;
+  const int page = ss.table[(int64_t)s * ss.width + p];
+  if ((unsigned)page >= (unsigned)pool.pages) return;
+  const int64_t ph = (int64_t)page * pool.H + h;
+  const int64_t row0 = (int64_t)se.q0 - se.len + (int64_t)p * kPage;  // packed row of slot 0
+  u32x4 kx[kPer][2] = {}, vx[kPer][2] = {};
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int n = threadIdx.x + kPageThreads * i, slot = n / kPieces, c = n % kPieces;
+    if (slot >= old && slot < end) {
+      const int64_t at = ((row0 + slot) * pool.H + h) * D + 16 * c;
+      kx[i][0] = *(const u32x4*)(k + at), kx[i][1] = *(const u32x4*)(k + at + 8);
+      vx[i][0] = *(const u32x4*)(v + at), vx[i][1] = *(const u32x4*)(v + at + 8);
+    }
+  }
+  const int k_was = old > 0 ? pool.k_exp[ph] : 0, v_was = old > 0 ? pool.v_exp[ph] : 0;
+  unsigned ka = 0, va = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        ka = amax_bits(ka, kx[i][u][x]);
+        va = amax_bits(va, vx[i][u][x]);
+      }
+  block_max2(ka, va, buf);
+  const int ke = max(exponent_of(ka), k_was), ve = max(exponent_of(va), v_was);
+  auto put = [&](uint8_t* base, const u32x4 (&x)[kPer][2], int exp, int was) {
+    const float up = scale_of(254 - exp, false);  // 2^-n; exp is at most 247 unless the page's was more
+    uint8_t* const at = base + ph * (kPage * D);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int n = threadIdx.x + kPageThreads * i, slot = n / kPieces;
+      u32x4 r;
+      if (slot >= old && slot < end) {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const u32x4 w = x[i][y / 2];
+          const unsigned a = w[2 * (y & 1)], c = w[2 * (y & 1) + 1];
+          r[y] = narrow4(__uint_as_float(a << 16) * up, __uint_as_float(a & 0xffff0000u) * up,
+                         __uint_as_float(c << 16) * up, __uint_as_float(c & 0xffff0000u) * up);
+        }
+      } else if (slot < old && exp != was) {
+        const u32x4 w = *(const u32x4*)(at + n * 16);
+        const float s0 = scale_of(was, false);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const bf16x4 f = widen4(w[y], s0);
+          r[y] = narrow4((float)f[0] * up, (float)f[1] * up, (float)f[2] * up, (float)f[3] * up);
+        }
+      } else {
+        continue;
+      }
+      *(u32x4*)(at + n * 16) = r;
+    }
+  };
+  put(pool.k, kx, ke, k_was);
+  put(pool.v, vx, ve, v_was);
+  if (threadIdx.x == 0) {
+    pool.k_exp[ph] = (uint8_t)ke;
+    pool.v_exp[ph] = (uint8_t)ve;
+  }
+  if (pool.weight != nullptr && (int)threadIdx.x >= old && (int)threadIdx.x < end)
+    pool.weight[ph * kPage + threadIdx.x] = 0.0f;
+}
+
+// ---- evict, first kernel: which tokens stay.  One workgroup per (session, head).
+//
+// The tokens of the middle (neither the first nor the last protected ones) are ranked by their weight as an
+// ordered integer.  Three passes over 11, 11 and 10 bits find the m-th largest, threshold, each narrowing the
+// prefix by a histogram in LDS; then a pass counts what every wave keeps and one writes the positions.
+constexpr int kSelectThreads = 1024;
+constexpr int kSelectWaves = kSelectThreads / 64;
+constexpr int kBins = 2048;
+
+// Monotone in the weight: -infinity (and NaN) lowest, -0 equal to 0.
+__device__ __forceinline__ unsigned rank_bits(float w) {
+  unsigned u = __float_as_uint(w);
+  if (w != w) u = 0xff800000u;
+  if (w == 0.0f) u = 0u;
+  return u >> 31 ? ~u : u | 0x80000000u;
+}
+
+__global__ void __launch_bounds__(kSelectThreads)
+cache_select_kernel(Pool pool, Sessions ss, int32_t* __restrict__ new_lens, int32_t* __restrict__ kept,
+                    int keep, int first, int last) {
+  __shared__ unsigned hist[kBins];
+  __shared__ unsigned wave_a[kSelectWaves], wave_b[kSelectWaves];
+  __shared__ unsigned found[2];
+  const int h = blockIdx.x % pool.H, s = blockIdx.x / pool.H;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const Session se = session_of(ss, s);
+  int32_t* const out = kept + (int64_t)blockIdx.x * keep;
+  if (h == 0 && tid == 0) new_lens[s] = se.ok ? min(se.len, keep) : se.len;
+  if (!se.ok || se.len <= keep) {
+    for (int i = tid; i < keep; i += kSelectThreads) out[i] = se.ok && i < se.len ? i : -1;
+    return;
+  }
+  const int begin = first, end = se.len - last;  // the middle; begin < end since len > keep >= first + last
+  const int32_t* const table = ss.table + (int64_t)s * ss.width;
+  auto rank_at = [&](int i) -> unsigned {
+    const int page = table[i / kPage];
+    const bool bad = (unsigned)page >= (unsigned)pool.pages;
+    const float w = pool.weight[page_offset(page, bad, pool.H, h, kPage) + i % kPage];
+    return rank_bits(bad ? -INFINITY : w);
+  };
+  unsigned want = (unsigned)(keep - first - last);  // tokens of the middle that stay
+  unsigned prefix = 0, mask = 0;
+  bool none = want == 0;
+  for (int pass = 0; pass < 3 && !none; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
+    for (int i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
+    __syncthreads();
+    for (int i = begin + tid; i < end; i += kSelectThreads) {
+      const unsigned u = rank_at(i);
+      if ((u & mask) == prefix) atomicAdd(&hist[u >> shift & (bins - 1)], 1u);
+    }
+    __syncthreads();
+    // the bin that holds the want-th largest: suffix sums of two bins a thread, from the top
+    const int b1 = bins - 1 - 2 * tid, b0 = b1 - 1;
+    const unsigned c1 = b1 >= 0 ? hist[b1] : 0, c0 = b0 >= 0 ? hist[b0] : 0;
+    unsigned sum = c1 + c0;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const unsigned y = (unsigned)__shfl_up((int)sum, m);
+      if (lane >= m) sum += y;
+    }
+    if (lane == 63) wave_a[wave] = sum;
+    __syncthreads();
+    unsigned before = sum - (c1 + c0);
+    for (int w = 0; w < wave; ++w) before += wave_a[w];
+    if (before < want && before + c1 >= want) found[0] = (unsigned)b1, found[1] = before;
+    if (before + c1 < want && before + c1 + c0 >= want) found[0] = (unsigned)b0, found[1] = before + c1;
+    __syncthreads();
+    prefix |= found[0] << shift;
+    mask |= (unsigned)(bins - 1) << shift;
+    want -= found[1];
+  }
+  // kept of the middle: every rank above prefix, and of those equal to it the first `want`
+  const int per = ((end - begin + kSelectWaves - 1) / kSelectWaves + 63) / 64 * 64;
+  const int wb = begin + wave * per, we = min(end, wb + per);
+  unsigned above = 0, equal = 0;
+  if (!none)
+    for (int i = wb; i < we; i += 64) {
+      const bool in = i + lane < we;
+      const unsigned u = in ? rank_at(i + lane) : 0u;
+      above += (unsigned)__builtin_popcountll(__builtin_amdgcn_ballot_w64(in && u > prefix));
+      equal += (unsigned)__builtin_popcountll(__builtin_amdgcn_ballot_w64(in && u == prefix));
+    }
+  if (lane == 0) wave_a[wave] = above, wave_b[wave] = equal;
+  __syncthreads();
+  unsigned at = (unsigned)first, eq = 0;
+  for (int w = 0; w < wave; ++w) {
+    at += wave_a[w] + (eq < want ? min(want - eq, wave_b[w]) : 0u);
+    eq += wave_b[w];
+  }
+  const unsigned long long below = ((unsigned long long)1 << lane) - 1;
+  if (!none)
+    for (int i = wb; i < we; i += 64) {
+      const bool in = i + lane < we;
+      const unsigned u = in ? rank_at(i + lane) : 0u;
+      const unsigned long long be = __builtin_amdgcn_ballot_w64(in && u == prefix);
+      const bool stay = in && (u > prefix || (u == prefix && eq + (unsigned)__builtin_popcountll(be & below) < want));
+      const unsigned long long bs = __builtin_amdgcn_ballot_w64(stay);
+      if (stay) out[at + (unsigned)__builtin_popcountll(bs & below)] = i + lane;
+      at += (unsigned)__builtin_popcountll(bs);
+      eq += (unsigned)__builtin_popcountll(be);
+    }
+  for (int i = tid; i < first; i += kSelectThreads) out[i] = i;
+  for (int i = tid; i < last; i += kSelectThreads) out[keep - last + i] = end + i;
+}
+
+// ---- evict, second kernel: the kept tokens into their new pages.  One workgroup per (session, new page,
+// head); a thread holds pieces of 16 channels of a token.
+template <int D>
+__global__ void __launch_bounds__(kPageThreads)
+cache_gather_kernel(Pool pool, Sessions ss, const int32_t* __restrict__ new_table,
+                    const int32_t* __restrict__ kept, int new_width, int keep, int page_slots) {
+  constexpr int kPieces = D / 16;
+  constexpr int kPer = kPage * kPieces / kPageThreads;
+  __shared__ unsigned buf[2 * kPageWaves];
+  const int b = blockIdx.x;
+  const int h = b % pool.H, sj = b / pool.H, j = sj % page_slots, s = sj / page_slots;
+  const Session se = session_of(ss, s);
+  if (!se.ok) return;
+  const int live = min(kPage, min(se.len, keep) - j * kPage);
+  if (live <= 0) return;
+  const int page = new_table[(int64_t)s * new_width + j];
+  if ((unsigned)page >= (unsigned)pool.pages) return;
+  const int64_t ph = (int64_t)page * pool.H + h;
+  const int32_t* const table = ss.table + (int64_t)s * ss.width;
+  const int32_t* const ids = kept + ((int64_t)s * pool.H + h) * keep + j * kPage;
+  u32x4 kx[kPer] = {}, vx[kPer] = {};
+  float ks[kPer] = {}, vs[kPer] = {};
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int n = threadIdx.x + kPageThreads * i, slot = n / kPieces, c = n % kPieces;
+    if (slot < live) {
+      const int id = ids[slot], from = table[id / kPage];
+      const bool bad = (unsigned)from >= (unsigned)pool.pages;
+      const int64_t fh = page_offset(from, bad, pool.H, h, 1);
+      const int64_t at = fh * (kPage * D) + (id % kPage) * D + 16 * c;
+      kx[i] = *(const u32x4*)(pool.k + at);
+      vx[i] = *(const u32x4*)(pool.v + at);
+      ks[i] = scale_of(pool.k_exp[fh], bad);
+      vs[i] = scale_of(pool.v_exp[fh], bad);
+      if (c == 0) pool.weight[ph * kPage + slot] = bad ? -INFINITY : pool.weight[fh * kPage + id % kPage];
+    }
+  }
+  unsigned ka = 0, va = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const u32x2 a = __builtin_bit_cast(u32x2, widen4(kx[i][x], ks[i]));
+      const u32x2 c = __builtin_bit_cast(u32x2, widen4(vx[i][x], vs[i]));
+      ka = amax_bits(amax_bits(ka, a[0]), a[1]);
+      va = amax_bits(amax_bits(va, c[0]), c[1]);
+    }
+  block_max2(ka, va, buf);
+  const int ke = exponent_of(ka), ve = exponent_of(va);
+  auto put = [&](uint8_t* base, const u32x4 (&x)[kPer], const float (&from)[kPer], int exp) {
+    const float up = scale_of(254 - exp, false);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int n = threadIdx.x + kPageThreads * i;
+      if (n / kPieces >= live) continue;
+      u32x4 r;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const bf16x4 f = widen4(x[i][y], from[i]);
+        r[y] = narrow4((float)f[0] * up, (float)f[1] * up, (float)f[2] * up, (float)f[3] * up);
+      }
+      *(u32x4*)(base + ph * (kPage * D) + n * 16) = r;
+    }
+  };
+  put(pool.k, kx, ks, ke);
+  put(pool.v, vx, vs, ve);
+  if (threadIdx.x == 0) {
+    pool.k_exp[ph] = (uint8_t)ke;
+    pool.v_exp[ph] = (uint8_t)ve;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// host-side launchers
+
+hipError_t launch_append(const AppendArgs& a, hipStream_t st) {
+  const int64_t items = append_items(a.ss.nseq, a.ss.max_rows, a.pool.H);
+  const int page_slots = (int)(items / ((int64_t)a.ss.nseq * a.pool.H));
+  auto kern = a.d == 64 ? cache_append_kernel<64> : cache_append_kernel<128>;
+  hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(kPageThreads), 0, st, a.pool, a.ss,
+                     (const __bf16*)a.k, (const __bf16*)a.v, a.new_lens, page_slots);
+  return hipGetLastError();
+}
+
+hipError_t launch_evict(const EvictArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(cache_select_kernel, dim3((unsigned)(a.ss.nseq * a.pool.H)), dim3(kSelectThreads), 0,
+                     st, a.pool, a.ss, a.new_lens, a.kept, a.keep, a.first, a.last);
+  const hipError_t e = hipGetLastError();
+  const int64_t items = gather_items(a.ss.nseq, a.keep, a.pool.H);
+  if (e != hipSuccess || items == 0) return e;
+  auto kern = a.d == 64 ? cache_gather_kernel<64> : cache_gather_kernel<128>;
+  hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(kPageThreads), 0, st, a.pool, a.ss, a.new_table,
+                     a.kept, a.new_width, a.keep, (a.keep + kPage - 1) / kPage);
+  return hipGetLastError();
+}
+
+}  // namespace tscache

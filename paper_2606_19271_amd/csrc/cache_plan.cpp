@@ -1,0 +1,63 @@
+// cache_plan.cpp -- host-side sizes of the session cache's launches, shared by the argument checks of
+// ts_cache.cpp and the launch code; no device code.
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "cache_launch.h"
+
+namespace tscache {
+
+namespace {
+int64_t ceil_div(int64_t a, int64_t b) { return a / b + (a % b != 0); }
+}  // namespace
+
+int row_tile(int64_t rows) { return rows <= 16 ? 16 : 32; }
+
+int64_t attn_items(int32_t nseq, int32_t max_rows, int32_t H, int32_t G) {
+  const int64_t rows = (int64_t)max_rows * G;
+  const int64_t tiles = ceil_div(rows, row_tile(rows));
+  // nseq * H * tiles, saturating well above the limit
+  const int64_t heads = (int64_t)nseq * H;
+  return tiles > 0 && heads > 4 * kGridLimit / tiles ? 4 * kGridLimit : heads * tiles;
+}
+
+int64_t merge_blocks(int32_t nseq, int32_t max_rows, int32_t Hq, int32_t d) {
+  const int64_t per = ceil_div((int64_t)max_rows * Hq * (d / 8), kMergeThreads);
+  return per > 0 && nseq > 4 * kGridLimit / per ? 4 * kGridLimit : nseq * per;
+}
+
+int32_t auto_splits(int32_t nseq, int32_t max_rows, int32_t max_len, int32_t H, int32_t G, int32_t,
+                    int32_t cus) {
+  const int64_t items = attn_items(nseq, max_rows, H, G);
+  const int64_t pages = ceil_div(max_len, kPage);
+  if (items <= 0) return 1;
+  const int64_t want = 4 * (int64_t)cus / items;
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, pages / 4, 64}));
+}
+
+int64_t part_o_offset(int32_t n, int32_t total, int32_t Hq) {
+  return ((int64_t)n * total * Hq * 4 + 255) / 256 * 256;
+}
+
+int64_t workspace_bytes(int32_t n, int32_t total, int32_t Hq, int32_t d) {
+  return n > 1 ? part_o_offset(n, total, Hq) + (int64_t)n * total * Hq * d * 4 : 0;
+}
+
+int64_t weigh_items(int32_t nseq, int32_t max_len, int32_t H) {
+  const int64_t pages = ceil_div(max_len, kPage), heads = (int64_t)nseq * H;
+  return pages > 0 && heads > 4 * kGridLimit / pages ? 4 * kGridLimit : heads * pages;
+}
+
+int64_t append_items(int32_t nseq, int32_t max_rows, int32_t H) {
+  // max_rows new tokens lie in at most that many pages, one more than the full ones on each side
+  const int64_t pages = ((int64_t)max_rows + 2 * kPage - 2) / kPage, heads = (int64_t)nseq * H;
+  return pages > 0 && heads > 4 * kGridLimit / pages ? 4 * kGridLimit : heads * pages;
+}
+
+int64_t gather_items(int32_t nseq, int32_t keep, int32_t H) {
+  const int64_t pages = ceil_div(keep, kPage), heads = (int64_t)nseq * H;
+  return pages > 0 && heads > 4 * kGridLimit / pages ? 4 * kGridLimit : heads * pages;
+}
+
+}  // namespace tscache

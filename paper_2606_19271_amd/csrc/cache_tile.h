@@ -1,0 +1,94 @@
+// cache_tile.h -- device code shared by the session cache's kernels: sessions, pages and the 8-bit format.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "cache_launch.h"
+
+namespace tscache {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// One session of a call, read by every workgroup that works on it.  ok: it is worked on at all (every
+// bound is checked before a difference is formed, so nothing wraps).
+struct Session {
+  int q0, rows, len;
+  bool ok;
+};
+
+__device__ __forceinline__ Session session_of(const Sessions& ss, int s) {
+  Session r;
+  r.q0 = 0, r.rows = 0;
+  r.len = ss.lens[s];
+  r.ok = r.len >= 0 && r.len <= ss.max_len;
+  if (ss.cu != nullptr) {
+    const int a = ss.cu[s], b = ss.cu[s + 1];
+    r.ok = r.ok && a >= 0 && b <= ss.total && b >= a && b - a <= ss.max_rows;
+    r.q0 = a, r.rows = r.ok ? b - a : 0;
+  }
+  return r;
+}
+
+// The bits of the float 2^(exp - 127); exponent 255 and pages outside the pool (bad) give infinity, with
+// which the conversion below makes every element NaN.
+__device__ __forceinline__ float scale_of(unsigned exp, bool bad) {
+  return __uint_as_float((bad ? 255u : exp) << 23);
+}
+
+// Four e4m3 bytes as four bfloat16, times the scale's power of two (exact for the exponents that this
+// library writes: e4m3 has 4 significant bits, and 2^-9 2^-100 is a normal bfloat16).
+__device__ __forceinline__ bf16x4 widen4(unsigned x, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true);
+  return bf16x4{a[0], a[1], b[0], b[1]};
+}
+
+__device__ __forceinline__ bf16x8 widen8(unsigned x, unsigned y, float scale) {
+  const bf16x4 a = widen4(x, scale), b = widen4(y, scale);
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// Four floats, already scaled, rounded to nearest even e4m3.  |x| <= 448 here but for infinities and NaN,
+// which both become NaN.
+__device__ __forceinline__ unsigned narrow4(float a, float b, float c, float d) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  r = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+  return (unsigned)r;
+}
+
+// The largest finite magnitude of packed bfloat16 bits, as bits (a positive bfloat16 orders as its bits).
+__device__ __forceinline__ unsigned amax_bits(unsigned amax, unsigned packed) {
+  const unsigned lo = packed & 0x7fffu, hi = packed >> 16 & 0x7fffu;
+  amax = max(amax, lo < 0x7f80u ? lo : 0u);
+  return max(amax, hi < 0x7f80u ? hi : 0u);
+}
+
+// The biased exponent of a page whose largest magnitude has these bfloat16 bits: 448 = 1.75 * 2^8, so
+// 1.m * 2^x <= 448 * 2^n from n = x - 8 on where 1.m <= 1.75 (m <= 96 of 128), else one more; n >= -100.
+__device__ __forceinline__ int exponent_of(unsigned amax) {
+  const int x = (int)(amax >> 7), m = (int)(amax & 127u);
+  return max(x - 8 + (m > 96 ? 1 : 0), 27);
+}
+
+// Bytes from a page's start to its head h, and the page itself; a page number outside the pool reads
+// page 0 (in bounds, and poisoned through its scale).
+__device__ __forceinline__ int64_t page_offset(int page, bool bad, int H, int h, int bytes) {
+  return ((int64_t)(bad ? 0 : page) * H + h) * bytes;
+}
+
+}  // namespace tscache
