@@ -12,21 +12,12 @@
 #include <stdint.h>
 
 #include "cache_launch.h"
-#include "cache_tile.h"
+#include "cache_device.h"
 
 namespace tscache {
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-}
-
-// Row r of (session, cached head h) in q and o, in units of d elements (and in lse): its token's and head's.
-__device__ __forceinline__ int64_t row_of(const Session& se, int r, int h, int H, int G) {
-  const int t = G == 1 ? r : r / G;
-  return ((int64_t)se.q0 + t) * (H * G) + h * G + (r - t * G);
 }
 
 // ---- attention of a tile of 16 NB query rows over a range of pages, one workgroup of four waves.
@@ -41,19 +32,6 @@ __device__ __forceinline__ int64_t row_of(const Session& se, int r, int h, int H
 // banks).
 constexpr int kRowThreads = 256;
 constexpr int kRowWaves = kRowThreads / 64;
-
-struct RowArgs {
-  Pool pool;
-  Sessions ss;
-  const __bf16* q;
-  __bf16* o;
-  float* lse;
-  float* part_o;
-  float* part_lse;
-  int G, n_split, tiles;
-  float c;
-  unsigned flip;  // sign bits of Q to invert (negative scales)
-};
 
 template <int D>
 __device__ __forceinline__ constexpr int v_chunk(int row, int chunk) {
@@ -357,11 +335,13 @@ static void launch_rows(const RowArgs& r, int tile, unsigned grid, hipStream_t s
 template <int D>
 static hipError_t launch_attn_d(const AttnArgs& a, hipStream_t st) {
   const int64_t rows = (int64_t)a.ss.max_rows * a.G;
-  const int tile = row_tile(rows);
+  const int tile = row_tile(rows, a.scale);
   RowArgs r{a.pool, a.ss, (const __bf16*)a.q, (__bf16*)a.o, a.lse, a.part_o, a.part_lse, a.G, a.n_split,
             (int)((rows + tile - 1) / tile), fabsf(a.scale) * kLog2e, a.scale < 0.0f ? 0x80008000u : 0u};
-  const unsigned grid = (unsigned)(attn_items(a.ss.nseq, a.ss.max_rows, a.pool.H, a.G) * a.n_split);
-  if (a.n_split > 1) launch_rows<D, true>(r, tile, grid, st);
+  const unsigned grid =
+      (unsigned)(attn_items(a.ss.nseq, a.ss.max_rows, a.ss.total, a.pool.H, a.G, tile) * a.n_split);
+  if (tile == kTileRows) launch_tiles(r, D, grid, a.cus, st);
+  else if (a.n_split > 1) launch_rows<D, true>(r, tile, grid, st);
   else launch_rows<D, false>(r, tile, grid, st);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_split == 1) return e;
@@ -384,6 +364,6 @@ hipError_t launch_weigh(const WeighArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t configure_kernels() { return hipSuccess; }
+hipError_t configure_kernels() { return configure_tiles(); }
 
 }  // namespace tscache

@@ -1,28 +1,17 @@
-// cache_tile.h -- device code shared by the session cache's kernels: sessions, pages and the 8-bit format.
+// cache_device.h -- device code shared by the session cache's kernels: sessions, pages and the 8-bit format.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "attn_tile.h"
 #include "cache_launch.h"
 
 namespace tscache {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-typedef int i32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-typedef __attribute__((address_space(3))) char lds_char;
-typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
-typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+using namespace tsattn;  // the types and products of attn_tile.h
 
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 
 // One session of a call, read by every workgroup that works on it.  ok: it is worked on at all (every
 // bound is checked before a difference is formed, so nothing wraps).
@@ -90,5 +79,31 @@ __device__ __forceinline__ int exponent_of(unsigned amax) {
 __device__ __forceinline__ int64_t page_offset(int page, bool bad, int H, int h, int bytes) {
   return ((int64_t)(bad ? 0 : page) * H + h) * bytes;
 }
+
+// Row r of (session, cached head h) in q and o, in units of d elements (and in lse): the rows are the
+// session's tokens, and of each the G query heads of h.
+__device__ __forceinline__ int64_t row_of(const Session& se, int r, int h, int H, int G) {
+  const int t = G == 1 ? r : r / G;
+  return ((int64_t)se.q0 + t) * (H * G) + h * G + (r - t * G);
+}
+
+// What the attention kernels take.
+struct RowArgs {
+  Pool pool;
+  Sessions ss;
+  const __bf16* q;
+  __bf16* o;
+  float* lse;
+  float* part_o;
+  float* part_lse;
+  int G, n_split;
+  int tiles;      // row tiles of a session at most (cache_rows_kernel)
+  float c;        // |scale| log2(e)
+  unsigned flip;  // sign bits of Q to invert (negative scales)
+};
+
+// cache_tiles.hip
+hipError_t configure_tiles();
+void launch_tiles(const RowArgs& r, int d, unsigned grid, int cus, hipStream_t st);
 
 }  // namespace tscache

@@ -72,17 +72,20 @@ struct EvictArgs {
 };
 
 // Host-side sizes (cache_plan.cpp).
-// Query rows (tokens x G) of an attention workgroup's tile.
-int row_tile(int64_t rows);
+// Query rows (tokens x G) of an attention workgroup's tile: 256 (cache_tiles_kernel), or 32 or 16
+// (cache_rows_kernel).
+constexpr int kTileRows = 256;
+int row_tile(int64_t rows, float scale);
 // Workgroups of an unsplit attention call, and of its merge kernel.
-int64_t attn_items(int32_t nseq, int32_t max_rows, int32_t H, int32_t G);
+int64_t attn_items(int32_t nseq, int32_t max_rows, int32_t total, int32_t H, int32_t G, int tile);
 int64_t merge_blocks(int32_t nseq, int32_t max_rows, int32_t Hq, int32_t d);
 // Page ranges per query tile when the caller leaves the choice to the library.
-int32_t auto_splits(int32_t nseq, int32_t max_rows, int32_t max_len, int32_t H, int32_t G, int32_t d,
-                    int32_t cus);
+int32_t auto_splits(int32_t nseq, int32_t max_rows, int32_t max_len, int32_t total, int32_t H, int32_t G,
+                    int32_t d, int tile, int32_t cus);
 // Bytes of workspace of a call of n page ranges: the partial lse [n][total][Hq], then O [n][total][Hq][d].
 int64_t workspace_bytes(int32_t n, int32_t total, int32_t Hq, int32_t d);
 int64_t part_o_offset(int32_t n, int32_t total, int32_t Hq);
+// Workgroups of the other kernels.
 int64_t weigh_items(int32_t nseq, int32_t max_len, int32_t H);
 int64_t append_items(int32_t nseq, int32_t max_rows, int32_t H);
 int64_t gather_items(int32_t nseq, int32_t keep, int32_t H);

@@ -3,7 +3,7 @@
 #include <stdint.h>
 
 #include "cache_launch.h"
-#include "cache_tile.h"
+#include "cache_device.h"
 
 namespace tscache {
 

@@ -12,13 +12,17 @@ namespace {
 int64_t ceil_div(int64_t a, int64_t b) { return a / b + (a % b != 0); }
 }  // namespace
 
-int row_tile(int64_t rows) { return rows <= 16 ? 16 : 32; }
+// Scale 0 is left to the row kernel: with a factor of 0 the tile kernel's masked scores would not vanish.
+int row_tile(int64_t rows, float scale) {
+  return rows <= 16 ? 16 : rows <= 32 || scale == 0.0f ? 32 : kTileRows;
+}
 
-int64_t attn_items(int32_t nseq, int32_t max_rows, int32_t H, int32_t G) {
-  const int64_t rows = (int64_t)max_rows * G;
-  const int64_t tiles = ceil_div(rows, row_tile(rows));
-  // nseq * H * tiles, saturating well above the limit
+int64_t attn_items(int32_t nseq, int32_t max_rows, int32_t total, int32_t H, int32_t G, int tile) {
   const int64_t heads = (int64_t)nseq * H;
+  if (tile == kTileRows)  // sum_s ceil(rows_s / tile) <= (all rows + nseq (tile - 1)) / tile
+    return std::min<int64_t>(4 * kGridLimit / H, ((int64_t)total * G + (int64_t)nseq * (tile - 1)) / tile) * H;
+  const int64_t tiles = ceil_div((int64_t)max_rows * G, tile);
+  // nseq * H * tiles, saturating well above the limit
   return tiles > 0 && heads > 4 * kGridLimit / tiles ? 4 * kGridLimit : heads * tiles;
 }
 
@@ -27,13 +31,22 @@ int64_t merge_blocks(int32_t nseq, int32_t max_rows, int32_t Hq, int32_t d) {
   return per > 0 && nseq > 4 * kGridLimit / per ? 4 * kGridLimit : nseq * per;
 }
 
-int32_t auto_splits(int32_t nseq, int32_t max_rows, int32_t max_len, int32_t H, int32_t G, int32_t,
-                    int32_t cus) {
-  const int64_t items = attn_items(nseq, max_rows, H, G);
-  const int64_t pages = ceil_div(max_len, kPage);
+int32_t auto_splits(int32_t nseq, int32_t max_rows, int32_t max_len, int32_t total, int32_t H, int32_t G,
+                    int32_t d, int tile, int32_t cus) {
+  const int64_t items = attn_items(nseq, max_rows, total, H, G, tile);
   if (items <= 0) return 1;
-  const int64_t want = 4 * (int64_t)cus / items;
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, pages / 4, 64}));
+  if (tile < kTileRows) {
+    const int64_t want = 4 * (int64_t)cus / items;
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, ceil_div(max_len, kPage) / 4, 64}));
+  }
+  const int64_t tiles = ceil_div(max_len, d == 64 ? 2 * kPage : kPage);
+  int32_t best = 1;
+  int64_t best_cost = INT64_MAX;
+  for (int32_t n = 1; n <= 16 && (n == 1 || tiles / n >= 4); ++n) {
+    const int64_t cost = ceil_div(items * n, cus) * (ceil_div(tiles, n) + 4) + (n > 1 ? 6 : 0);
+    if (cost < best_cost) best_cost = cost, best = n;
+  }
+  return best;
 }
 
 int64_t part_o_offset(int32_t n, int32_t total, int32_t Hq) {

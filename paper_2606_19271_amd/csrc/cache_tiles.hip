@@ -1,0 +1,523 @@
+// cache_tiles.hip -- attention of many query rows over the session cache: 256-row tiles on the matrix cores.
+//
+// The schedule is the one of the bf16 kernels (attn_kernels.hip): a workgroup of eight waves owns 256 query
+// rows of one cached head; a wave has 32 of them and alternates between a matrix step (S = K Q^T of one key
+// tile, O += V P of the one before, on 32x32x16 MFMAs) and a vector step (the online softmax), the two waves of
+// a SIMD in opposite steps.  What differs is how the tiles arrive.  A page's bytes cannot go to LDS by DMA,
+// because the MFMA operands are bf16: the vector step's waves load a tile's bytes into registers one step
+// ahead (8 KiB per tile and operand, half of what bf16 takes), widen them (one instruction per two elements,
+// with the page's power of two; exact) and write the bf16 image.  Each element is widened once per workgroup.
+//
+// The registers between memory and LDS are one more stage, so the rings are shorter.  Phases are numbered as in
+// attn_kernels.hip (A's M(j) = 2j, A's V(j) = B's M(j) = 2j + 1, B's V(j) = 2j + 2).  Group A (waves 0-3) writes
+// K_{j+2} in its V(j), phase 2j + 1, over K_{j-1}, whose last reader is B's M(j-1) in phase 2j - 1; its first
+// reader is A itself at the end of V(j+1), phase 2j + 3.  Group B (waves 4-7) writes V_{j+1} in its V(j), phase
+// 2j + 2, over V_{j-1}, last read by B's M(j) in phase 2j + 1, first read by A's M(j+2) in phase 2j + 4.  So K
+// has three stages and V two.
+//
+// The sum of the weights is formed in the vector step from the weights before their rounding (two chains of
+// additions), so that the log-sum-exp is good to fp32, which the cached tokens' weights are formed against.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "attn_tile.h"
+#include "cache_device.h"
+#include "cache_launch.h"
+
+namespace tscache {
+
+template <int D>
+struct TileGeo {
+  using G = Geo<D>;
+  static constexpr int kBN = G::kBN;                     // keys of a tile
+  static constexpr int kPages = kBN / kPage;             // pages of a tile (1 at d = 128, 2 at d = 64)
+  static constexpr int kLoads = kBN * D / 4 / 1024;      // 16-byte loads per lane, tile and operand (4 waves)
+  static constexpr int kVRing = 0, kVStages = 2;
+  static constexpr int kKRing = kVStages * G::kVTile, kKStages = 3;
+  static constexpr int kRings = kKRing + kKStages * G::kKTile;
+  static constexpr int kQBase = kRings;                  // 32 rows of each wave, in the prologue
+  static constexpr int kOBase = kRings;                  // and of O in the epilogue
+  static constexpr int kLds = kRings + kWaves * (G::kQWave > G::kOWave ? G::kQWave : G::kOWave);
+  static_assert(kLoads == 2, "two loads per lane: one page each at d = 64, both of one at d = 128");
+  static_assert(kLds <= 160 * 1024, "LDS of a CU");
+};
+
+// One item: query rows [row0, row0 + 256) of (session, head h) against key tiles [tile_begin, + ntiles).
+struct TileItem {
+  Session se;
+  const int32_t* table;  // the session's pages
+  int h, row0, rows, tile_begin, ntiles, split;
+};
+
+// The session's page numbers and exponents of one operand, in lanes: of the 64 page indexes of a window, the lane
+// has the one that is its own number mod 64.  The window's halves are renewed in turn as the item moves on.  Pages
+// past the session's end are page 0 with no bytes; pages outside the pool are page 0 with the exponent that makes
+// them NaN.
+struct PageWindow {
+  int id, exp;
+
+  __device__ __forceinline__ void load_id(const int32_t* table, int p, int pages) { id = p < pages ? table[p] : 0; }
+  __device__ __forceinline__ void load_exp(const uint8_t* exps, const Pool& pool, int h, int p, int pages) {
+    const bool bad = (unsigned)id >= (unsigned)pool.pages;
+    id = bad ? 0 : id;
+    exp = exps[(int64_t)id * pool.H + h];
+    exp = bad ? 255 : p < pages ? exp : 127;
+  }
+};
+
+// exp2(S c - m_c) of the lane's scores, packed for the PV product; returns the bitwise OR of the packed words
+// (bit 14 set: some weight is 2 or more, or not finite) and adds the weights to sum.
+template <int NT, int kIssue, int kEvery, typename Issue>
+__device__ __forceinline__ unsigned exp_sum_pack(const f32x16 (&s)[NT / 2], bf16x8 (&p)[NT], float m_c, float c,
+                                                 float& sum, Issue&& issue) {
+  unsigned any = 0;
+  float sum0 = 0.0f, sum1 = 0.0f;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+#pragma unroll
+    for (int m = 0; m < 8; m += 2) {
+      const int step = 4 * t + m / 2;
+      if (kIssue > 0 && step % kEvery == 0 && step / kEvery < kIssue) {
+        __builtin_amdgcn_sched_barrier(0);
+        issue(step / kEvery);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      const float x0 = s[t >> 1][8 * (t & 1) + m], x1 = s[t >> 1][8 * (t & 1) + m + 1];
+      const f32x2 e = {__builtin_amdgcn_exp2f(__builtin_fmaf(x0, c, -m_c)),
+                       __builtin_amdgcn_exp2f(__builtin_fmaf(x1, c, -m_c))};
+      sum0 += e[0];
+      sum1 += e[1];
+      // the weights enter the product in 16 bits, its operands' type
+      const bf16x2 pb = __builtin_convertvector(e, bf16x2);
+      p[t][m] = pb[0];
+      p[t][m + 1] = pb[1];
+      any |= __builtin_bit_cast(unsigned, pb);
+    }
+  }
+  sum = sum0 + sum1;
+  // keeps the additions here: sunk behind the test of `any`, they would hold all weights in registers
+  __asm__ volatile("" : "+v"(sum));
+  return any;
+}
+
+struct NoHook {
+  __device__ void operator()(int) const {}
+};
+
+constexpr float kTileBias = 39.0f;  // as kBias of attn_kernels.hip: the largest weight so far is 2^-39
+enum TilePlace { kFirst = 0, kInner = 1, kLast = 2 };
+
+// The online softmax of one tile: as softmax_tile of attn_kernels.hip (the running maximum stays while no weight
+// reaches 2), with the row sum l in the lane (its half of the keys).
+template <int D, int kPlace, int kHooks, int kEvery, typename Issue>
+__device__ __forceinline__ void tile_softmax(f32x16 (&s)[Geo<D>::kBN / 32], bf16x8 (&p)[Geo<D>::kBN / 16],
+                                             float& m_c, float& l, f32x16 (&o)[D / 32], float c, int keys,
+                                             int lane, Issue&& issue) {
+  constexpr int kBN = Geo<D>::kBN;
+  const int hb = lane >> 5;
+  float sum;
+  if (kPlace == kInner) {
+    const unsigned any = exp_sum_pack<kBN / 16, kHooks, kEvery>(s, p, m_c, c, sum, issue);
+    if (__builtin_amdgcn_ballot_w64((any & 0x40004000u) != 0) == 0) {
+      l += sum;
+      return;
+    }
+  }
+  if (kPlace == kLast) {
+#pragma unroll
+    for (int kb = 0; kb < kBN / 32; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (32 * kb + 8 * (r >> 2) + 4 * hb + (r & 3) >= keys) s[kb][r] = -INFINITY;
+  }
+  float mt = s[0][0];
+#pragma unroll
+  for (int kb = 0; kb < kBN / 32; ++kb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mt = fmaxf(mt, s[kb][r]);
+  mt = half_max(mt);
+  const float m_new = fmaxf(m_c, __builtin_fmaf(mt, c, kTileBias));
+  if (kPlace != kFirst) {
+    const float alpha = __builtin_amdgcn_exp2f(m_c - m_new);  // 0 where m_c = -inf
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
+    l *= alpha;
+  }
+  m_c = m_new;
+  if (kPlace == kInner) exp_sum_pack<kBN / 16, 0, 1>(s, p, m_c, c, sum, NoHook{});
+  else exp_sum_pack<kBN / 16, kHooks, kEvery>(s, p, m_c, c, sum, issue);
+  l += sum;
+}
+
+// O = O / l of a wave's 32 rows, through LDS so that whole lines are stored (as write_result of
+// attn_kernels.hip), and the rows' log-sum-exp.
+template <int D, bool kPartial>
+__device__ __forceinline__ void write_rows(const TileItem& it, const RowArgs& a, const f32x16 (&oacc)[D / 32],
+                                           float l, float m_c, int q0, lds_char* stage, int lane) {
+  using G = Geo<D>;
+  const int col = lane & 31, hb = lane >> 5, H = a.pool.H;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const int orow = lane >> 3, ochunk = lane & 7;
+  lds_char* const put = stage + col * G::kORow;
+  const lds_char* const get = stage + orow * G::kORow + ochunk * 16;
+  auto in_order = [] { __asm__ volatile("" ::: "memory"); };
+  const int64_t slab = kPartial ? (int64_t)it.split * a.ss.total * (H * a.G) : 0;
+  int64_t at[4];  // rows that this lane stores
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int r = q0 + orow + 8 * u;
+    at[u] = r < it.rows ? slab + row_of(it.se, r, it.h, H, a.G) : -1;
+  }
+  constexpr int kBlocks = kPartial ? 1 : 2;  // 32-channel blocks of a pass: 128 bytes of each row
+#pragma unroll
+  for (int d0 = 0; d0 < D / 32; d0 += kBlocks) {
+#pragma unroll
+    for (int db = d0; db < d0 + kBlocks; ++db)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4) {
+        const f32x4 x = {oacc[db][4 * g4] * inv, oacc[db][4 * g4 + 1] * inv, oacc[db][4 * g4 + 2] * inv,
+                         oacc[db][4 * g4 + 3] * inv};
+        const int ch = 32 * (db - d0) + 8 * g4 + 4 * hb;
+        if (kPartial) *(lds_u32x4*)(put + ch * 4) = __builtin_bit_cast(u32x4, x);
+        else *(lds_u32x2*)(put + ch * 2) = __builtin_bit_cast(u32x2, __builtin_convertvector(x, bf16x4));
+      }
+    in_order();
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const u32x4 x = *(const lds_u32x4*)(get + 8 * u * G::kORow);
+      if (at[u] >= 0) {
+        if (kPartial) *(u32x4*)((char*)(a.part_o + at[u] * D + 32 * d0) + ochunk * 16) = x;
+        else *(u32x4*)((char*)(a.o + at[u] * D + 32 * d0) + ochunk * 16) = x;
+      }
+    }
+    in_order();
+  }
+  float* const lse = kPartial ? a.part_lse : a.lse;
+  if (lse != nullptr && hb == 0 && q0 + col < it.rows)
+    lse[slab + row_of(it.se, q0 + col, it.h, H, a.G)] = l == 0.0f ? -INFINITY : (m_c + log2f(l)) * kLn2;
+}
+
+// kActive = false: a wave whose rows all lie past the session's: it fetches its share and keeps the barriers.
+template <int D, bool kGroupB, bool kPartial, bool kActive>
+__device__ __forceinline__ void run_tile_group(const TileItem& it, const RowArgs& a, char* smem) {
+  using G = Geo<D>;
+  using T = TileGeo<D>;
+  constexpr int kBN = G::kBN;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int gw = wave & (G::kGroupWaves - 1);
+  const int H = a.pool.H;
+  lds_char* const lds = (lds_char*)smem;
+  auto ktile = [&](int stage) { return lds + T::kKRing + stage * G::kKTile; };
+  auto vtile = [&](int stage) { return lds + T::kVRing + stage * G::kVTile; };
+  const VOffsets<D> vo(lane);
+
+  // ---- fetching
+  const uint8_t* const bytes = (kGroupB ? a.pool.v : a.pool.k) + (int64_t)it.h * (kPage * D);
+  const uint8_t* const exps = kGroupB ? a.pool.v_exp : a.pool.k_exp;
+  const int len = it.se.len, pages = (len + kPage - 1) / kPage;
+  const int first = it.tile_begin * T::kPages;  // page index of the item's first tile
+  int window = first;                           // first page index of the window
+  PageWindow pw;
+  {
+    const int p = window + ((lane - window) & 63);
+    pw.load_id(it.table, p, pages);
+    pw.load_exp(exps, a.pool, it.h, p, pages);
+  }
+  // Tile j's bytes, into registers: load u of a lane covers bytes 1024 n + 16 lane of the tile, n = gw + 4 u;
+  // at d = 128 both lie in the one page, at d = 64 load u in page u.
+  u32x4 raw[T::kLoads];
+  float scale[T::kLoads];
+  auto load = [&](int j, int u) {
+    const int p = (it.tile_begin + j) * T::kPages + (T::kPages == 2 ? u : 0);
+    const int id = __builtin_amdgcn_readlane(pw.id, p & 63), e = __builtin_amdgcn_readlane(pw.exp, p & 63);
+    // tokens of the page (rows past them read as zeros); a scalar, as the descriptor has to be
+    const int n = __builtin_amdgcn_readfirstlane(max(0, min(kPage, len - p * kPage)));
+    __amdgpu_buffer_rsrc_t r = make_rsrc(bytes + (int64_t)id * H * (kPage * D), (uint32_t)(n * D));
+    raw[u] = __builtin_amdgcn_raw_buffer_load_b128(r, 16 * lane + 1024 * (gw + (T::kPages == 2 ? 0 : 4 * u)), 0, 0);
+    scale[u] = __uint_as_float((unsigned)e << 23);
+  };
+  // Half of load u's 16 elements, widened, to its place in the tile's LDS image.
+  const int row0 = (1024 * gw + 16 * lane) / D, chunk0 = lane % (D / 16) * 2;
+  constexpr int kRowStep = 4096 / D;  // rows from load 0 to load 1
+  auto put = [&](lds_char* tile, int u, int half) {
+    const int row = row0 + u * kRowStep;
+    const bf16x8 x = widen8(raw[u][2 * half], raw[u][2 * half + 1], scale[u]);
+    lds_char* const to = kGroupB ? tile + row * G::kVRow + (((chunk0 + half) ^ G::vswz(row)) << 4)
+                                 : tile + row * G::kKRow + ((chunk0 + half) << 4);
+    *(lds_bf16x8*)to = x;
+  };
+  // Renews half of the window when the pages about to be fetched (of tile j) enter its other half: the numbers
+  // first, the exponents that hang on them 16 pages later, 16 pages before they are needed.
+  auto renew = [&](int j) {
+    const int p = (it.tile_begin + j) * T::kPages;
+    if (p == window + 32) {
+      if (((lane - p) & 63) >= 32) pw.load_id(it.table, p + ((lane - p) & 63), pages);
+    } else if (p == window + 48) {
+      window += 32;
+      const int q = window + ((lane - window) & 63);
+      if (q >= window + 32) pw.load_exp(exps, a.pool, it.h, q, pages);
+    }
+  };
+  constexpr int kAhead = kGroupB ? 1 : 2;  // tiles between a vector step and the tile it writes
+
+  // ---- prologue: the first tiles' images, the next one's bytes, the wave's query rows
+  {
+    const int qrow0 = it.row0 + 32 * wave;
+    if constexpr (kActive) {
+      const int last = it.rows - 1, step = H * a.G * D * 2;
+      const int t_last = a.G == 1 ? last : last / a.G;
+      __amdgpu_buffer_rsrc_t rq =
+          make_rsrc(a.q + ((int64_t)it.se.q0 * (H * a.G) + it.h * a.G) * D,
+                    (uint32_t)t_last * (uint32_t)step + (uint32_t)(last - t_last * a.G + 1) * (D * 2));
+#pragma unroll
+      for (int n = 0; n < G::kQWave / 1024; ++n) {
+        const int row = (64 * n + lane) / G::kChunks;
+        const int chunk = (lane % G::kChunks) ^ (D == 128 ? row & 15 : (row >> 1) & 7);
+        const int r = qrow0 + row, t = a.G == 1 ? r : r / a.G;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_void*)(lds + T::kQBase + wave * G::kQWave + 1024 * n), 16,
+                                                 t * step + (r - t * a.G) * (D * 2) + chunk * 16, 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+#pragma unroll
+      for (int u = 0; u < T::kLoads; ++u) load(j, u);
+#pragma unroll
+      for (int u = 0; u < T::kLoads; ++u)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) put(kGroupB ? vtile(j) : ktile(j), u, half);
+    }
+#pragma unroll
+    for (int u = 0; u < T::kLoads; ++u) load(kAhead, u);
+  }
+  bf16x8 qf[D / 16] = {};
+  if constexpr (kActive) {
+    wait_vmem<0>();
+    __asm__ volatile("" ::: "memory");
+    const lds_char* const stage = lds + T::kQBase + wave * G::kQWave;
+    const int row = lane & 31, hb = lane >> 5;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      const u32x4 x = *(const lds_u32x4*)(stage + row * D * 2 +
+                                          (((2 * kk + hb) ^ (D == 128 ? row & 15 : (row >> 1) & 7)) << 4));
+      qf[kk] = __builtin_bit_cast(bf16x8, x ^ u32x4{a.flip, a.flip, a.flip, a.flip});
+    }
+  }
+  wait_lds();
+  block_sync();
+
+  f32x16 oacc[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) oacc[db] = f32x16{};
+  f32x16 s[kBN / 32];
+  bf16x8 p[kBN / 16];
+  bf16x8 kp[kPreReads];
+  f32x4 unused[2] = {};
+  float m_c = -INFINITY, l = 0.0f;
+  const int ntiles = it.ntiles;
+  const int last_keys = min(kBN, len - (it.tile_begin + ntiles - 1) * kBN);
+  if constexpr (kActive) k_preread<D>(ktile(0), kp, lane);
+  if (kGroupB) block_sync();  // group B starts one step behind
+
+  // Vector step j: the softmax of tile j, and in four places of it the image of the tile fetched a step ago (each
+  // a quarter), a load of the next tile's bytes wherever its registers have come free.  `stage`: where the image goes.
+  constexpr int kHooks = 4, kEvery = kBN / 16;
+  auto vstep = [&](int j, int stage, auto place) {
+    constexpr int kPlace = decltype(place)::value;
+    lds_char* const to = kGroupB ? vtile(stage) : ktile(stage);
+    renew(j + kAhead + 1);
+    auto hook = [&](int i) {
+      put(to, i >> 1, i & 1);
+      if (i & 1) load(j + kAhead + 1, i >> 1);
+    };
+    if constexpr (kActive) {
+      tile_softmax<D, kPlace, kHooks, kEvery>(s, p, m_c, l, oacc, a.c, last_keys, lane, hook);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kHooks; ++i) hook(i);
+    }
+    wait_lds();
+    if (kActive && kPlace != kLast) k_preread<D>(ktile((j + 1) % T::kKStages), kp, lane);
+  };
+  using First = std::integral_constant<int, kFirst>;
+  using Inner = std::integral_constant<int, kInner>;
+  using Last = std::integral_constant<int, kLast>;
+  // stages of K_j and of the tile that vector step j writes
+  int ks = 0;
+  auto write_stage = [&](int j) { return kGroupB ? (j + 1) & 1 : ks == 0 ? 2 : ks - 1; };  // (j + 2) % 3
+
+  if constexpr (kActive) {
+    __builtin_amdgcn_s_setprio(1);
+    m_step<D, false, false>(ktile(0), vtile(0), vo, qf, kp, s, p, oacc, bf16x8{}, unused, lane);
+    __builtin_amdgcn_s_setprio(0);
+  }
+  block_sync();
+  auto vector = [&](int j, auto place) { vstep(j, write_stage(j), place); };
+  if (ntiles == 1) vector(0, Last{});
+  else vector(0, First{});
+  auto tile = [&](int j, auto place) {
+    ks = ks == 2 ? 0 : ks + 1;
+    block_sync();  // closes V(j - 1)
+    if constexpr (kActive) {
+      __builtin_amdgcn_s_setprio(1);
+      m_step<D, true, false>(ktile(ks), vtile((j - 1) & 1), vo, qf, kp, s, p, oacc, bf16x8{}, unused, lane);
+      __builtin_amdgcn_s_setprio(0);
+    }
+    block_sync();
+    vector(j, place);
+  };
+  int j = 1;
+  for (; j < ntiles - 1; ++j) tile(j, Inner{});
+  if (j == ntiles - 1) tile(j, Last{});
+  block_sync();  // closes V(ntiles - 1)
+  if constexpr (kActive) pv_tile<D>(vtile((ntiles - 1) & 1), vo, p, oacc);
+  if (!kGroupB) block_sync();  // matches group B's extra barrier at the start
+
+  if constexpr (kActive) {
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    write_rows<D, kPartial>(it, a, oacc, __uint_as_float(r[0]) + __uint_as_float(r[1]), m_c, it.row0 + 32 * wave,
+                            lds + T::kOBase + wave * G::kOWave, lane);
+  }
+}
+
+// The sessions' items, and the one of a workgroup.  Up to 64 sessions are put in order of their lengths by every
+// wave itself, longest first, one per lane, so that a call of unequal sessions ends evenly; more keep their order.
+template <int D>
+__device__ __forceinline__ bool find_item(const RowArgs& a, int chunk, TileItem* it) {
+  const int lane = threadIdx.x & 63, per_tile = a.pool.H * a.n_split;
+  int s, local;
+  auto items_of = [&](const Session& se) {
+    return se.ok ? per_tile * (int)(((int64_t)se.rows * a.G + kBM - 1) / kBM) : 0;
+  };
+  if (a.ss.nseq <= 64) {
+    Session mine{};
+    if (lane < a.ss.nseq) mine = session_of(a.ss, lane);
+    const int count = lane < a.ss.nseq ? items_of(mine) : 0;
+    int before = 0, total = 0;
+    for (int i = 0; i < a.ss.nseq; ++i) {
+      const int li = __builtin_amdgcn_readlane(mine.len, i), ci = __builtin_amdgcn_readlane(count, i);
+      before += li > mine.len || (li == mine.len && i < lane) ? ci : 0;
+      total += ci;
+    }
+    if ((int)blockIdx.x >= total) return false;
+    const int item = remap_block(blockIdx.x, total, chunk);
+    s = __builtin_ctzll(__builtin_amdgcn_ballot_w64(before <= item && item - before < count));
+    local = item - __builtin_amdgcn_readlane(before, s);
+  } else {
+    // Two walks over the sessions, 64 at a time: the items in all, then the one that holds this workgroup's.
+    int total = 0, item = 0;
+    s = -1, local = 0;
+    for (int walk = 0; walk < 2 && s < 0; ++walk) {
+      int base = 0;
+      for (int s0 = 0; s0 < a.ss.nseq && s < 0; s0 += 64) {
+        const int count = s0 + lane < a.ss.nseq ? items_of(session_of(a.ss, s0 + lane)) : 0;
+        int sum = count;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+          const int y = __shfl_up(sum, m);
+          if (lane >= m) sum += y;
+        }
+        const int before = base + sum - count;
+        if (walk == 1) {
+          const unsigned long long hit = __builtin_amdgcn_ballot_w64(before <= item && item - before < count);
+          if (hit != 0) {
+            const int i = __builtin_ctzll(hit);
+            s = s0 + i;
+            local = item - __builtin_amdgcn_readlane(before, i);
+          }
+        }
+        base += __builtin_amdgcn_readlane(sum, 63);
+      }
+      if (walk == 0) {
+        total = base;
+        if ((int)blockIdx.x >= total) return false;
+        item = remap_block(blockIdx.x, total, chunk);
+      }
+    }
+    if (s < 0) return false;
+  }
+  // everything about the item is the same in all lanes: in scalar registers
+  s = __builtin_amdgcn_readfirstlane(s);
+  local = __builtin_amdgcn_readfirstlane(local);
+  it->se = session_of(a.ss, s);
+  it->se.q0 = __builtin_amdgcn_readfirstlane(it->se.q0);
+  it->se.rows = __builtin_amdgcn_readfirstlane(it->se.rows);
+  it->se.len = __builtin_amdgcn_readfirstlane(it->se.len);
+  it->table = a.ss.table + (int64_t)s * a.ss.width;
+  it->rows = it->se.rows * a.G;
+  const int nq = (it->rows + kBM - 1) / kBM, per_head = nq * a.n_split;
+  it->h = __builtin_amdgcn_readfirstlane(small_div(local, per_head));
+  local -= it->h * per_head;
+  it->split = a.n_split == 1 ? 0 : __builtin_amdgcn_readfirstlane(small_div(local, nq));
+  it->row0 = (local - it->split * nq) * kBM;
+  const int tiles = (it->se.len + Geo<D>::kBN - 1) / Geo<D>::kBN;
+  const int per = a.n_split == 1 ? tiles : __builtin_amdgcn_readfirstlane((tiles + a.n_split - 1) / a.n_split);
+  it->tile_begin = it->split * per;
+  it->ntiles = max(0, min(per, tiles - it->tile_begin));
+  return true;
+}
+
+template <int D, bool kPartial>
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+cache_tiles_kernel(RowArgs a, int chunk) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  TileItem it;
+  if (!find_item<D>(a, chunk, &it)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool active = it.row0 + 32 * wave < it.rows;
+  if (it.ntiles <= 0) {  // no keys: zeros, or nothing but the log-sum-exp of an empty range
+    if (!active) return;
+    const int lane = threadIdx.x & 63, r = it.row0 + 32 * wave + (lane & 31);
+    if (r >= it.rows) return;
+    const int64_t row = row_of(it.se, r, it.h, a.pool.H, a.G);
+    if (kPartial) {
+      if (lane < 32) a.part_lse[(int64_t)it.split * a.ss.total * (a.pool.H * a.G) + row] = -INFINITY;
+      return;
+    }
+    for (int c = lane >> 5; c < D / 8; c += 2) *(u32x4*)(a.o + row * D + 8 * c) = u32x4{};
+    if (a.lse != nullptr && lane < 32) a.lse[row] = -INFINITY;
+    return;
+  }
+  if (wave >= kWaves / 2) {
+    if (active) run_tile_group<D, true, kPartial, true>(it, a, smem);
+    else run_tile_group<D, true, kPartial, false>(it, a, smem);
+  } else {
+    if (active) run_tile_group<D, false, kPartial, true>(it, a, smem);
+    else run_tile_group<D, false, kPartial, false>(it, a, smem);
+  }
+}
+
+hipError_t configure_tiles() {
+  const struct {
+    const void* kern;
+    int lds;
+  } all[] = {{(const void*)cache_tiles_kernel<64, false>, TileGeo<64>::kLds},
+             {(const void*)cache_tiles_kernel<64, true>, TileGeo<64>::kLds},
+             {(const void*)cache_tiles_kernel<128, false>, TileGeo<128>::kLds},
+             {(const void*)cache_tiles_kernel<128, true>, TileGeo<128>::kLds}};
+  for (const auto& k : all) {
+    const hipError_t e = hipFuncSetAttribute(k.kern, hipFuncAttributeMaxDynamicSharedMemorySize, k.lds);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <int D>
+static void launch_tiles_d(const RowArgs& r, unsigned grid, int chunk, hipStream_t st) {
+  auto kern = r.n_split > 1 ? cache_tiles_kernel<D, true> : cache_tiles_kernel<D, false>;
+  hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), TileGeo<D>::kLds, st, r, chunk);
+}
+
+// RowArgs' workgroups are 256-row tiles of a session and head here.
+void launch_tiles(const RowArgs& r, int d, unsigned grid, int cus, hipStream_t st) {
+  const int chunk = cus / 8 > 0 ? cus / 8 : 1;  // consecutive items of an XCD
+  if (d == 64) launch_tiles_d<64>(r, grid, chunk, st);
+  else launch_tiles_d<128>(r, grid, chunk, st);
+}
+
+}  // namespace tscache

@@ -178,8 +178,8 @@ int launched(hipError_t e) {
   return TS_ERR_HIP;
 }
 
-int32_t choose_splits(int32_t n, const tscache::Sessions& ss, int32_t H, int32_t G, int32_t d, int32_t cus) {
-  return n > 0 ? n : tscache::auto_splits(ss.nseq, ss.max_rows, ss.max_len, H, G, d, cus);
+int32_t choose_splits(int32_t n, const tscache::Sessions& ss, int32_t H, int32_t G, int32_t d, int tile, int32_t cus) {
+  return n > 0 ? n : tscache::auto_splits(ss.nseq, ss.max_rows, ss.max_len, ss.total, H, G, d, tile, cus);
 }
 
 }  // namespace
@@ -228,7 +228,8 @@ int ts_cache_attn(const ts_cache* cache, const void* q, void* o, float* lse, con
   rc = check_sessions(cache, nseq, width, max_rows, max_len, total, Hq);
   if (rc != TS_OK) return rc;
   const int32_t G = Hq / cache->H;
-  if (tscache::attn_items(nseq, max_rows, cache->H, G) * std::max(1, num_splits) >= tscache::kGridLimit ||
+  const int tile = tscache::row_tile((int64_t)max_rows * G, scale);
+  if (tscache::attn_items(nseq, max_rows, total, cache->H, G, tile) * std::max(1, num_splits) >= tscache::kGridLimit ||
       tscache::merge_blocks(nseq, max_rows, Hq, cache->d) >= tscache::kGridLimit)
     return TS_ERR_SHAPE;
   if (!isfinite(scale)) return TS_ERR_SCALE;
@@ -255,7 +256,7 @@ int ts_cache_attn(const ts_cache* cache, const void* q, void* o, float* lse, con
   if (!st) return rc;
   tscache::AttnArgs a{pool_of(cache), {cu, table, lens, nseq, width, max_rows, max_len, total}, q, o, lse,
                       nullptr, nullptr, cache->d, G, 1, scale, st->cus};
-  a.n_split = choose_splits(num_splits, a.ss, cache->H, G, cache->d, st->cus);
+  a.n_split = choose_splits(num_splits, a.ss, cache->H, G, cache->d, tile, st->cus);
   while (a.n_split > 1 && tscache::workspace_bytes(a.n_split, total, Hq, cache->d) > workspace_bytes) --a.n_split;
   if (a.n_split > 1) {
     a.part_lse = (float*)workspace;
@@ -281,7 +282,8 @@ int64_t ts_cache_attn_workspace(int32_t nseq, int32_t max_rows, int32_t max_len,
     cus = st->cus;
   }
   const tscache::Sessions ss{nullptr, nullptr, nullptr, nseq, 0, max_rows, max_len, total};
-  return tscache::workspace_bytes(choose_splits(num_splits, ss, H, Hq / H, d, cus), total, Hq, d);
+  const int tile = tscache::row_tile((int64_t)max_rows * (Hq / H), 1.0f);
+  return tscache::workspace_bytes(choose_splits(num_splits, ss, H, Hq / H, d, tile, cus), total, Hq, d);
 }
 
 int ts_cache_weigh(const ts_cache* cache, const void* q, const float* lse, const int32_t* cu,

@@ -180,17 +180,21 @@ def attn_bounds(q, pool, cu, table, lens, scale, size, o, lse):
     """How far o and lse may be off.  A score is a sum of d exact products of 16-bit operands in fp32 and one fused
     multiply-add: off by at most (d + 2) 2^-24 of the sum of its terms' magnitudes (S), which shifts ln of a weight by as
     much; exp2 and the sums add a few 2^-23.  The weights are rounded to bfloat16 (half a step, 2^-8) before they
-    meet the values, and the result is rounded once more."""
+    meet the values, and the result is rounded once more.  Weights are formed as 2^-39 of the largest one's size
+    (room for later, larger ones before the maximum is moved), and those under 2^-126, the least normal
+    number, may be lost: n weights of less than 2^-87 each, times the largest value, whose sum the row's total,
+    at least 1, divides."""
     d = q.shape[2]
-    S = np.zeros(lse.shape)
+    S, gone = np.zeros(lse.shape), np.zeros(lse.shape)
     G = q.shape[1] // pool.k.shape[1]
     for s, n in enumerate(lens):
         for hq in range(q.shape[1]):
             if n:
                 k = np.abs(np.nan_to_num(pool.tokens("k", table[s], n, hq // G))).max(0)
                 S[cu[s]:cu[s + 1], hq] = abs(scale) * (np.abs(q[cu[s]:cu[s + 1], hq]) @ k)
+                gone[cu[s]:cu[s + 1], hq] = n * 2.0 ** -87 * np.abs(np.nan_to_num(pool.tokens("v", table[s], n, hq // G))).max()
     shift = (d + 2) * 2.0 ** -24 * S + 2.0 ** -20
-    return (2.0 ** -8 + 2 * shift)[..., None] * size + 2.0 ** -8 * np.abs(o) + 1e-30, shift + 2.0 ** -22 * np.abs(np.nan_to_num(lse, neginf=0))
+    return (2.0 ** -8 + 2 * shift)[..., None] * size + 2.0 ** -8 * np.abs(o) + gone[..., None], shift + 2.0 ** -22 * np.abs(np.nan_to_num(lse, neginf=0))
 
 
 def run_attn(g, rows, lens, H, G, d, scale=None, num_splits=0, max_extra=0):
@@ -270,12 +274,17 @@ def test_attn_rising_scores(d, rows):
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("rows", [2, 290])
 def test_attn_ignores_what_lies_past_a_session(d, rows):
-    """NaN bytes in the slots past the end, and wild page numbers past the last page, change nothing."""
+    """NaN bytes in the slots past the end, wild page numbers past the last page, and pages of other
+    sessions that are NaN (page 0 among them) change nothing."""
     g = torch.Generator().manual_seed(d + rows)
     lens = [97, 64, 500]
     width, pages, H = 9, 14, 2
     cache = make_pool(g, pages, H, d)
-    table, _ = make_table(g, lens, width, pages)
+    table, free = make_table(g, lens, width, pages)
+    if 0 not in free:  # page 0 is nobody's
+        for row in table:
+            row[:] = [free[0] if p == 0 else p for p in row]
+        free[0] = 0
     cu = offsets([rows] * 3)
     q = bf16(normal(g, cu[-1], H, d)).cuda()
     args = (q, cache, ints(cu), rows, ints(table), ints(lens), 512)
@@ -284,6 +293,8 @@ def test_attn_ignores_what_lies_past_a_session(d, rows):
         if n % PAGE:
             for x in (cache.k, cache.v):
                 x.view(torch.uint8)[table[s][n // PAGE], :, n % PAGE:] = 0x7f
+    for p in free:
+        cache.k_exp[p], cache.v_exp[p] = 255, 255
     b = ts.ts_cache_attn(*args, return_lse=True)
     assert torch.equal(a[0].view(torch.int16), b[0].view(torch.int16)) and torch.equal(a[1], b[1])
 
