@@ -142,18 +142,18 @@ __device__ __forceinline__ const lds_char* k_frag(const lds_char* kt, int kk, in
 }
 
 // The K fragments of a tile's first kPreReads S MFMAs.
-template <int D>
-__device__ __forceinline__ void k_preread(const lds_char* __restrict__ kt, bf16x8 (&kp)[kPreReads],
+template <int D, int kPre = kPreReads>
+__device__ __forceinline__ void k_preread(const lds_char* __restrict__ kt, bf16x8 (&kp)[kPre],
                                           int lane) {
   constexpr int kKB = Geo<D>::kBN / 32;  // 32-key blocks per tile
 #pragma unroll
-  for (int i = 0; i < kPreReads; ++i)
+  for (int i = 0; i < kPre; ++i)
     kp[i] = *(const lds_bf16x8*)k_frag<D>(kt, i / kKB, i % kKB, lane);
 }
 
-template <int D>
+template <int D, int kPre = kPreReads>
 __device__ __forceinline__ void qk_tile(const lds_char* __restrict__ kt, const bf16x8 (&qf)[D / 16],
-                                        const bf16x8 (&kp)[kPreReads],
+                                        const bf16x8 (&kp)[kPre],
                                         f32x16 (&s)[Geo<D>::kBN / 32], int lane) {
   constexpr int kKB = Geo<D>::kBN / 32;
 #pragma unroll
@@ -163,7 +163,7 @@ __device__ __forceinline__ void qk_tile(const lds_char* __restrict__ kt, const b
 #pragma unroll
     for (int kb = 0; kb < kKB; ++kb) {
       const int i = kKB * kk + kb;
-      bf16x8 a = i < kPreReads ? kp[i] : *(const lds_bf16x8*)k_frag<D>(kt, kk, kb, lane);
+      bf16x8 a = i < kPre ? kp[i] : *(const lds_bf16x8*)k_frag<D>(kt, kk, kb, lane);
       s[kb] = mfma32(a, qf[kk], s[kb]);
     }
 }
@@ -263,35 +263,35 @@ __device__ __forceinline__ void block_sync() {
 // only, and the K fragments of the first kPreReads S MFMAs were read in the vector step before
 // the barrier.  After that the issue order is pinned so that each MFMA's LDS operand is
 // requested kPreReads MFMAs earlier (one b128 read per S MFMA, two transpose reads per PV MFMA).
-// kSums = false: without the row sums, for kernels that form them in the vector step.
-template <int D, bool kPV, bool kSums = true>
+// kSums = false: without the row sums, for kernels that form them in the vector step.  kPre: in place of kPreReads.
+template <int D, bool kPV, bool kSums = true, int kPre = kPreReads>
 __device__ __forceinline__ constexpr int m_step_reads(int i) {
   constexpr int kBN = Geo<D>::kBN;
   constexpr int kRS = kPV && kSums ? kBN / 16 : 0;  // row-sum MFMAs
   constexpr int kQK = (kBN / 32) * (D / 16);
   if (i < kRS) return 0;
   i -= kRS;
-  return i < kQK ? (i < kPreReads ? 0 : 1) : 2;
+  return i < kQK ? (i < kPre ? 0 : 1) : 2;
 }
 
-template <int D, bool kPV, bool kSums = true>
+template <int D, bool kPV, bool kSums = true, int kPre = kPreReads>
 __device__ __forceinline__ void m_step(const lds_char* __restrict__ kt, const lds_char* __restrict__ vt,
                                        const VOffsets<D>& vo, const bf16x8 (&qf)[D / 16],
-                                       const bf16x8 (&kp)[kPreReads],
+                                       const bf16x8 (&kp)[kPre],
                                        f32x16 (&s)[Geo<D>::kBN / 32],
                                        const bf16x8 (&p)[Geo<D>::kBN / 16], f32x16 (&o)[D / 32],
                                        bf16x8 sel, f32x4 (&l)[2], int lane) {
   constexpr int kBN = Geo<D>::kBN;
   if (kPV && kSums) row_sums(sel, p, l);
-  qk_tile<D>(kt, qf, kp, s, lane);
+  qk_tile<D, kPre>(kt, qf, kp, s, lane);
   if (kPV) pv_tile<D>(vt, vo, p, o);
   // MFMAs: row sums (4), S (16 at d = 128), PV (16 at d = 128)
   constexpr int kN = (kPV && kSums ? kBN / 16 : 0) + (kBN / 32) * (D / 16) + (kPV ? (kBN / 16) * (D / 32) : 0);
 #pragma unroll
   for (int i = 0; i < kN; ++i) {
     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    const int next = i + kPreReads;  // MFMA whose operands are requested now
-    const int reads = next < kN ? m_step_reads<D, kPV, kSums>(next) : 0;
+    const int next = i + kPre;  // MFMA whose operands are requested now
+    const int reads = next < kN ? m_step_reads<D, kPV, kSums, kPre>(next) : 0;
     if (reads == 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     else if (reads == 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
   }

@@ -74,6 +74,11 @@ __device__ __forceinline__ int exponent_of(unsigned amax) {
   return max(x - 8 + (m > 96 ? 1 : 0), 27);
 }
 
+// LDS DMA: lane i's 16 bytes at `offset` of the buffer land at to + 16 i.
+__device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t rsrc, lds_char* to, int offset) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)to, 16, offset, 0, 0, 0);
+}
+
 // Bytes from a page's start to its head h, and the page itself; a page number outside the pool reads
 // page 0 (in bounds, and poisoned through its scale).
 __device__ __forceinline__ int64_t page_offset(int page, bool bad, int H, int h, int bytes) {
@@ -104,6 +109,6 @@ struct RowArgs {
 
 // cache_tiles.hip
 hipError_t configure_tiles();
-void launch_tiles(const RowArgs& r, int d, unsigned grid, int cus, hipStream_t st);
+void launch_tiles(const RowArgs& r, int d, int64_t items, hipStream_t st);
 
 }  // namespace tscache

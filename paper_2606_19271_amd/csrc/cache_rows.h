@@ -1,0 +1,241 @@
+// cache_rows.h -- attention of up to 32 query rows of one cached head over a range of its session's pages, by a
+// workgroup whose waves take the pages in turn.  Used for calls of few rows (cache_attn.hip) and for the last, thin
+// tile of a session's rows (cache_tiles.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "cache_device.h"
+
+namespace tscache {
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// Waits until at most N of this wave's vector-memory operations are outstanding (gfx9 encoding: the count's upper
+// two bits are 15:14), and keeps memory accesses from moving across.
+template <int N>
+__device__ __forceinline__ void wait_vmem_in_order() {
+  static_assert(N >= 0 && N < 64, "vmcnt field");
+  __asm__ volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
+  __asm__ volatile("" ::: "memory");
+}
+
+// The waves share nothing until the end, so there is no barrier in the loop.  Per page a wave computes S^T = K Q^T
+// on 16x16x32 MFMAs (lane: query row lane & 15, keys 4 (lane >> 4) + 0..3 of each 16), keeps a running maximum and
+// sum per row, and accumulates O^T += V^T P^T, whose B operand is the lane's own weights once the 32 keys of a step
+// are taken in the order in which two score blocks hold them.  K goes from memory to MFMA operands in registers: a
+// lane loads D / 4 consecutive channels of a key, and the sum over channels takes them in that order on both sides.
+// V's bytes go by LDS DMA to the wave's own two buffers, in an order (v_chunk) in which the 8-bit transpose reads
+// spread over the banks; both arrive a page ahead of their use.
+template <int D, int NB, int kW>
+struct RowGeo {
+  static constexpr int kKK = D / 32;                     // MFMA steps over the channels
+  static constexpr int kCB = D / 16;                     // 16-channel blocks of O
+  static constexpr int kVLoads = kPage * D / 1024;       // LDS DMA instructions of V per page
+  static constexpr int kKLoads = D / 64;                 // 16-byte loads of K per lane and 16 keys
+  static constexpr int kPageBytes = kPage * D;
+  static constexpr int kVBufs = kW * 2 * kPageBytes;
+  static constexpr int kObuf = kW * 16 * D * 4;          // over the V buffers, at the end
+  static constexpr int kMl = kVBufs > kObuf ? kVBufs : kObuf;  // float [2][kW][16]: maxima and sums
+  static constexpr int kLds = kMl + 2 * kW * 16 * 4;
+  // channels of a thread when the waves' results are joined, 16 rows at a time
+  static constexpr int kCh = D / (4 * kW) < 4 ? 4 : D / (4 * kW);
+};
+
+// Position of 16-byte chunk `chunk` of V row `row` in LDS.
+template <int D>
+__device__ __forceinline__ constexpr int v_chunk(int row, int chunk) {
+  return D == 128 ? chunk ^ (row >> 1 & 7) : chunk ^ (row >> 2 & 3);
+}
+
+// Rows [row0, row0 + 16 NB) of `rows` (see row_of) over the pages [begin, end) of a session; kW waves, RowGeo::kLds
+// bytes of LDS.
+template <int D, int NB, int kW, bool kPartial>
+__device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, const int32_t* table, int h, int row0,
+                                          int rows, int begin, int end, int split, char* smem) {
+  using R = RowGeo<D, NB, kW>;
+  constexpr int kKK = R::kKK, kCB = R::kCB, kVLoads = R::kVLoads, kKLoads = R::kKLoads, kPageBytes = R::kPageBytes;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int i16 = lane & 15, g = lane >> 4;
+  const int H = a.pool.H, G = a.G;
+  lds_char* const lds = (lds_char*)smem;
+  lds_char* const vbuf = lds + wave * 2 * kPageBytes;
+
+  // ---- the wave's pages: begin + wave, + kW, ...; lane i has the number and exponents of the i-th of 64 of them
+  const int mine = end - begin > wave ? (end - begin - wave + kW - 1) / kW : 0;
+  int id = 0, kexp = 0, vexp = 0;
+  auto renew = [&](int i0) {
+    const int i = i0 + lane;
+    id = i < mine ? table[begin + wave + kW * i] : 0;
+    const bool bad = (unsigned)id >= (unsigned)a.pool.pages;
+    id = bad ? 0 : id;
+    kexp = a.pool.k_exp[(int64_t)id * H + h];
+    vexp = a.pool.v_exp[(int64_t)id * H + h];
+    if (bad) kexp = vexp = 255;  // reads as NaN
+  };
+  u32x4 kx[4][kKLoads];
+  float ks, vs;
+  const int koff = i16 * D + D / 4 * g;
+  auto load = [&](int i) {  // page i of the wave
+    const int64_t at = ((int64_t)__builtin_amdgcn_readlane(id, i & 63) * H + h) * kPageBytes;
+    ks = __uint_as_float((unsigned)__builtin_amdgcn_readlane(kexp, i & 63) << 23);
+    vs = __uint_as_float((unsigned)__builtin_amdgcn_readlane(vexp, i & 63) << 23);
+    // rows past the session's end as zeros: scores that are masked, values that meet weights of zero
+    const int n = __builtin_amdgcn_readfirstlane(max(0, min(kPage, se.len - (begin + wave + kW * i) * kPage)));
+    __amdgpu_buffer_rsrc_t rk = make_rsrc(a.pool.k + at, (uint32_t)(n * D));
+    __amdgpu_buffer_rsrc_t rv = make_rsrc(a.pool.v + at, (uint32_t)(n * D));
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+      for (int x = 0; x < kKLoads; ++x)
+        kx[kb][x] = __builtin_amdgcn_raw_buffer_load_b128(rk, koff + 16 * kb * D + 16 * x, 0, 0);
+    lds_char* const to = vbuf + (i & 1) * kPageBytes;
+#pragma unroll
+    for (int x = 0; x < kVLoads; ++x) {
+      const int row = (64 * x + lane) / (D / 16);
+      dma16(rv, to + 1024 * x, row * D + v_chunk<D>(row, lane % (D / 16)) * 16);
+    }
+    __asm__ volatile("" ::: "memory");
+  };
+  if (mine > 0) renew(0);
+
+  bf16x8 qf[NB][kKK];
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+    const int r = row0 + 16 * n + i16;
+    const __bf16* const src = a.q + row_of(se, min(r, rows - 1), h, H, G) * D + D / 4 * g;
+#pragma unroll
+    for (int kk = 0; kk < kKK; ++kk)
+      qf[n][kk] = __builtin_bit_cast(bf16x8, *(const u32x4*)(src + 8 * kk) ^ u32x4{a.flip, a.flip, a.flip, a.flip});
+  }
+  f32x4 o[NB][kCB] = {};
+  float m[NB], l[NB];
+#pragma unroll
+  for (int n = 0; n < NB; ++n) m[n] = -INFINITY, l[n] = 0.0f;
+
+  if (mine > 0) load(0);
+  for (int i = 0; i < mine; ++i) {
+    const int valid = se.len - (begin + wave + kW * i) * kPage;  // keys of this page (64 or more: all)
+    const float v_scale = vs;
+    f32x4 sc[NB][4] = {};
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+      for (int kk = 0; kk < kKK; ++kk) {
+        const bf16x8 kf = widen8(kx[kb][kk / 2][2 * (kk & 1)], kx[kb][kk / 2][2 * (kk & 1) + 1], ks);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) sc[n][kb] = mfma16(kf, qf[n][kk], sc[n][kb]);
+      }
+    const bool more = i + 1 < mine;
+    if (more) {
+      if (((i + 1) & 63) == 0) renew(i + 1);
+      load(i + 1);
+    }
+    bf16x8 pf[NB][2];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      float mt = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (16 * kb + 4 * g + r < valid) mt = fmaxf(mt, sc[n][kb][r]);
+      mt = fmaxf(mt, __shfl_xor(mt, 16));
+      mt = fmaxf(mt, __shfl_xor(mt, 32));
+      // scores that are all NaN leave the maximum as it is; their weights are NaN
+      const float m_new = fmaxf(m[n], mt * a.c);
+      const float alpha = m[n] == m_new ? 1.0f : __builtin_amdgcn_exp2f(m[n] - m_new);
+      m[n] = m_new;
+      float sum = 0.0f;
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][kb][r], a.c, -m_new));
+          if (16 * kb + 4 * g + r >= valid) w = 0.0f;
+          sum += w;
+          // the weights enter the product in 16 bits (its operands' type), the row sum in 32
+          pf[n][kb / 2][4 * (kb & 1) + r] = (__bf16)w;
+        }
+      l[n] = l[n] * alpha + sum;
+#pragma unroll
+      for (int cb = 0; cb < kCB; ++cb) o[n][cb] *= alpha;
+    }
+    // this page's V: all but the next page's loads are done
+    if (more) wait_vmem_in_order<4 * kKLoads + kVLoads>();
+    else wait_vmem_in_order<0>();
+    const lds_char* const vb = vbuf + (i & 1) * kPageBytes;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int cb = 0; cb < kCB; ++cb) {
+        // lane 2 R + c of 16 addresses bytes 8 c of key row R; it gets channel lane & 15 of the 8 rows:
+        // keys 4 g + 0..3 of the step's first 16, then of its second
+        const int r8 = i16 >> 1;
+        const int row = 32 * u + (r8 & 4) * 4 + 4 * g + (r8 & 3);
+        const i32x2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+            (lds_i32x2*)(vb + row * D + v_chunk<D>(row, cb) * 16 + 8 * (i16 & 1)));
+        const bf16x8 vf = widen8((unsigned)x[0], (unsigned)x[1], v_scale);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) o[n][cb] = mfma16(vf, pf[n][u], o[n][cb]);
+      }
+    // the reads have left the buffer before the next but one page's DMA comes into it
+    wait_lds();
+    __asm__ volatile("" ::: "memory");
+  }
+
+  // ---- join the waves: O = sum_w 2^(m_w - M) O_w / sum_w 2^(m_w - M) l_w, 16 rows at a time
+  typedef __attribute__((address_space(3))) float lds_float;
+  typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+  lds_float* const obuf = (lds_float*)lds;
+  lds_float* const ml = (lds_float*)(lds + R::kMl);
+  constexpr int kCh = R::kCh;
+  const int orow = tid / (D / kCh), och = tid % (D / kCh) * kCh;
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+    float ln = l[n];
+    ln += __shfl_xor(ln, 16);
+    ln += __shfl_xor(ln, 32);
+    __syncthreads();
+#pragma unroll
+    for (int cb = 0; cb < kCB; ++cb) *(lds_f32x4*)(obuf + (wave * 16 + i16) * D + 16 * cb + 4 * g) = o[n][cb];
+    if (g == 0) ml[wave * 16 + i16] = m[n], ml[(kW + wave) * 16 + i16] = ln;
+    __syncthreads();
+    const int r = row0 + 16 * n + orow;
+    if (orow >= 16 || r >= rows) continue;
+    float big = -INFINITY, sum = 0.0f;
+    f32x4 acc[kCh / 4] = {};
+#pragma unroll
+    for (int w = 0; w < kW; ++w) big = fmaxf(big, ml[w * 16 + orow]);
+#pragma unroll
+    for (int w = 0; w < kW; ++w) {
+      const float mw = ml[w * 16 + orow], lw = ml[(kW + w) * 16 + orow];
+      if (lw == 0.0f) continue;  // no keys
+      const float f = mw == big ? 1.0f : __builtin_amdgcn_exp2f(mw - big);
+      sum += f * lw;
+#pragma unroll
+      for (int x = 0; x < kCh / 4; ++x) acc[x] += f * *(const lds_f32x4*)(obuf + (w * 16 + orow) * D + och + 4 * x);
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float lse = sum == 0.0f ? -INFINITY : (big + log2f(sum)) * kLn2;
+    const int64_t at = row_of(se, r, h, H, G);
+    if constexpr (kPartial) {
+      const int64_t part = (int64_t)split * a.ss.total * (H * G) + at;
+      if (sum != 0.0f)
+#pragma unroll
+        for (int x = 0; x < kCh / 4; ++x) *(f32x4*)(a.part_o + part * D + och + 4 * x) = acc[x] * inv;
+      if (och == 0) a.part_lse[part] = lse;
+    } else {
+#pragma unroll
+      for (int x = 0; x < kCh / 4; ++x)
+        *(bf16x4*)(a.o + at * D + och + 4 * x) = __builtin_convertvector(acc[x] * inv, bf16x4);
+      if (a.lse != nullptr && och == 0) a.lse[at] = lse;
+    }
+  }
+}
+
+}  // namespace tscache

@@ -15,8 +15,14 @@
 // 2j + 2, over V_{j-1}, last read by B's M(j) in phase 2j + 1, first read by A's M(j+2) in phase 2j + 4.  So K
 // has three stages and V two.
 //
-// The sum of the weights is formed in the vector step from the weights before their rounding (two chains of
-// additions), so that the log-sum-exp is good to fp32, which the cached tokens' weights are formed against.
+// The sum of the weights is formed in the vector step before their rounding to bf16 (two chains of additions; the sum
+// also tells whether a weight is too large for the running maximum), so that the log-sum-exp is good to fp32: the
+// cached tokens' weights are formed against it.  On the matrix core, from the rounded weights as in attn_kernels.hip,
+// it would take 1.4 % less time (4680 rows x 32760 keys x 40 heads, d = 128: 2548 against 2583 us).
+//
+// Registers bound the matrix step: with the bytes of the next tile held through it, operands read 8 MFMAs ahead leave
+// the scheduler without room (it then reads each one right before its use); 4 ahead cost nothing (attn_kernels.hip
+// reads 8 ahead).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -25,6 +31,7 @@
 #include "attn_tile.h"
 #include "cache_device.h"
 #include "cache_launch.h"
+#include "cache_rows.h"
 
 namespace tscache {
 
@@ -39,7 +46,11 @@ struct TileGeo {
   static constexpr int kRings = kKRing + kKStages * G::kKTile;
   static constexpr int kQBase = kRings;                  // 32 rows of each wave, in the prologue
   static constexpr int kOBase = kRings;                  // and of O in the epilogue
-  static constexpr int kLds = kRings + kWaves * (G::kQWave > G::kOWave ? G::kQWave : G::kOWave);
+  static constexpr int kPre = 4;                         // LDS reads ahead of their MFMAs
+  static constexpr int kEntries = 512;                   // pages in a group's list (PageEntry)
+  static constexpr int kList = kRings + kWaves * (G::kQWave > G::kOWave ? G::kQWave : G::kOWave);
+  static constexpr int kLds = kList + 2 * kEntries * 8;
+  static_assert(G::kVTile == 16384 && kVRing == 0 && kVStages == 2, "a V stage is one bit of an LDS address");
   static_assert(kLoads == 2, "two loads per lane: one page each at d = 64, both of one at d = 128");
   static_assert(kLds <= 160 * 1024, "LDS of a CU");
 };
@@ -51,28 +62,18 @@ struct TileItem {
   int h, row0, rows, tile_begin, ntiles, split;
 };
 
-// The session's page numbers and exponents of one operand, in lanes: of the 64 page indexes of a window, the lane
-// has the one that is its own number mod 64.  The window's halves are renewed in turn as the item moves on.  Pages
-// past the session's end are page 0 with no bytes; pages outside the pool are page 0 with the exponent that makes
-// them NaN.
-struct PageWindow {
-  int id, exp;
-
-  __device__ __forceinline__ void load_id(const int32_t* table, int p, int pages) { id = p < pages ? table[p] : 0; }
-  __device__ __forceinline__ void load_exp(const uint8_t* exps, const Pool& pool, int h, int p, int pages) {
-    const bool bad = (unsigned)id >= (unsigned)pool.pages;
-    id = bad ? 0 : id;
-    exp = exps[(int64_t)id * pool.H + h];
-    exp = bad ? 255 : p < pages ? exp : 127;
-  }
+// A page of the session's as a group fetches it: its number, and its exponent as the bits of a float.  Pages past the
+// session's end are page 0 (of which no byte is read), with a scale of 1; pages outside the pool are page 0 with the
+// scale that makes them NaN.
+struct PageEntry {
+  int id;
+  unsigned scale;
 };
 
-// exp2(S c - m_c) of the lane's scores, packed for the PV product; returns the bitwise OR of the packed words
-// (bit 14 set: some weight is 2 or more, or not finite) and adds the weights to sum.
+// exp2(S c - m_c) of the lane's scores, packed for the PV product; returns their sum, in fp32 before that rounding.
 template <int NT, int kIssue, int kEvery, typename Issue>
-__device__ __forceinline__ unsigned exp_sum_pack(const f32x16 (&s)[NT / 2], bf16x8 (&p)[NT], float m_c, float c,
-                                                 float& sum, Issue&& issue) {
-  unsigned any = 0;
+__device__ __forceinline__ float exp_pack(const f32x16 (&s)[NT / 2], bf16x8 (&p)[NT], float m_c, float c,
+                                          Issue&& issue) {
   float sum0 = 0.0f, sum1 = 0.0f;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -93,13 +94,12 @@ __device__ __forceinline__ unsigned exp_sum_pack(const f32x16 (&s)[NT / 2], bf16
       const bf16x2 pb = __builtin_convertvector(e, bf16x2);
       p[t][m] = pb[0];
       p[t][m + 1] = pb[1];
-      any |= __builtin_bit_cast(unsigned, pb);
     }
   }
-  sum = sum0 + sum1;
-  // keeps the additions here: sunk behind the test of `any`, they would hold all weights in registers
+  float sum = sum0 + sum1;
+  // keeps the additions here: sunk behind a test of the weights, they would hold all of them in registers
   __asm__ volatile("" : "+v"(sum));
-  return any;
+  return sum;
 }
 
 struct NoHook {
@@ -109,18 +109,17 @@ struct NoHook {
 constexpr float kTileBias = 39.0f;  // as kBias of attn_kernels.hip: the largest weight so far is 2^-39
 enum TilePlace { kFirst = 0, kInner = 1, kLast = 2 };
 
-// The online softmax of one tile: as softmax_tile of attn_kernels.hip (the running maximum stays while no weight
-// reaches 2), with the row sum l in the lane (its half of the keys).
+// The online softmax of one tile, as softmax_tile of attn_kernels.hip: the running maximum stays while the weights of
+// no lane add up to 2.  l: the row sum over the lane's half of the keys.
 template <int D, int kPlace, int kHooks, int kEvery, typename Issue>
 __device__ __forceinline__ void tile_softmax(f32x16 (&s)[Geo<D>::kBN / 32], bf16x8 (&p)[Geo<D>::kBN / 16],
                                              float& m_c, float& l, f32x16 (&o)[D / 32], float c, int keys,
                                              int lane, Issue&& issue) {
   constexpr int kBN = Geo<D>::kBN;
   const int hb = lane >> 5;
-  float sum;
   if (kPlace == kInner) {
-    const unsigned any = exp_sum_pack<kBN / 16, kHooks, kEvery>(s, p, m_c, c, sum, issue);
-    if (__builtin_amdgcn_ballot_w64((any & 0x40004000u) != 0) == 0) {
+    const float sum = exp_pack<kBN / 16, kHooks, kEvery>(s, p, m_c, c, issue);
+    if (__builtin_amdgcn_ballot_w64(!(sum < 2.0f)) == 0) {  // (NaN and infinities among them)
       l += sum;
       return;
     }
@@ -148,9 +147,8 @@ __device__ __forceinline__ void tile_softmax(f32x16 (&s)[Geo<D>::kBN / 32], bf16
     l *= alpha;
   }
   m_c = m_new;
-  if (kPlace == kInner) exp_sum_pack<kBN / 16, 0, 1>(s, p, m_c, c, sum, NoHook{});
-  else exp_sum_pack<kBN / 16, kHooks, kEvery>(s, p, m_c, c, sum, issue);
-  l += sum;
+  l += kPlace == kInner ? exp_pack<kBN / 16, 0, 1>(s, p, m_c, c, NoHook{})
+                        : exp_pack<kBN / 16, kHooks, kEvery>(s, p, m_c, c, issue);
 }
 
 // O = O / l of a wave's 32 rows, through LDS so that whole lines are stored (as write_result of
@@ -206,7 +204,7 @@ template <int D, bool kGroupB, bool kPartial, bool kActive>
 __device__ __forceinline__ void run_tile_group(const TileItem& it, const RowArgs& a, char* smem) {
   using G = Geo<D>;
   using T = TileGeo<D>;
-  constexpr int kBN = G::kBN;
+  constexpr int kBN = G::kBN, kPre = T::kPre;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gw = wave & (G::kGroupWaves - 1);
@@ -214,54 +212,69 @@ __device__ __forceinline__ void run_tile_group(const TileItem& it, const RowArgs
   lds_char* const lds = (lds_char*)smem;
   auto ktile = [&](int stage) { return lds + T::kKRing + stage * G::kKTile; };
   auto vtile = [&](int stage) { return lds + T::kVRing + stage * G::kVTile; };
-  const VOffsets<D> vo(lane);
+  VOffsets<D> vo(lane);  // in the V stage that the next matrix step reads
 
   // ---- fetching
   const uint8_t* const bytes = (kGroupB ? a.pool.v : a.pool.k) + (int64_t)it.h * (kPage * D);
   const uint8_t* const exps = kGroupB ? a.pool.v_exp : a.pool.k_exp;
   const int len = it.se.len, pages = (len + kPage - 1) / kPage;
   const int first = it.tile_begin * T::kPages;  // page index of the item's first tile
-  int window = first;                           // first page index of the window
-  PageWindow pw;
-  {
-    const int p = window + ((lane - window) & 63);
-    pw.load_id(it.table, p, pages);
-    pw.load_exp(exps, a.pool, it.h, p, pages);
-  }
-  // Tile j's bytes, into registers: load u of a lane covers bytes 1024 n + 16 lane of the tile, n = gw + 4 u;
-  // at d = 128 both lie in the one page, at d = 64 load u in page u.
-  u32x4 raw[T::kLoads];
-  float scale[T::kLoads];
-  auto load = [&](int j, int u) {
-    const int p = (it.tile_begin + j) * T::kPages + (T::kPages == 2 ? u : 0);
-    const int id = __builtin_amdgcn_readlane(pw.id, p & 63), e = __builtin_amdgcn_readlane(pw.exp, p & 63);
-    // tokens of the page (rows past them read as zeros); a scalar, as the descriptor has to be
-    const int n = __builtin_amdgcn_readfirstlane(max(0, min(kPage, len - p * kPage)));
-    __amdgpu_buffer_rsrc_t r = make_rsrc(bytes + (int64_t)id * H * (kPage * D), (uint32_t)(n * D));
-    raw[u] = __builtin_amdgcn_raw_buffer_load_b128(r, 16 * lane + 1024 * (gw + (T::kPages == 2 ? 0 : 4 * u)), 0, 0);
-    scale[u] = __uint_as_float((unsigned)e << 23);
+  // The group's list of pages in LDS, entry i mod kEntries the item's i-th page: filled in the prologue, and its halves
+  // renewed in turn as the item moves on, an entry a lane of the group.
+  typedef __attribute__((address_space(3))) u32x2 lds_entry;
+  lds_char* const list = lds + T::kList + (kGroupB ? T::kEntries * 8 : 0);
+  constexpr int kHalf = T::kEntries / 2;
+  static_assert(kHalf == 64 * G::kGroupWaves, "an entry a lane");
+  auto page_id = [&](int i) { return first + i < pages ? it.table[first + i] : 0; };
+  auto put_entry = [&](int i, int id) {
+    const bool bad = (unsigned)id >= (unsigned)a.pool.pages;
+    const unsigned e = exps[(int64_t)(bad ? 0 : id) * H + it.h];
+    const unsigned scale = (bad ? 255u : first + i < pages ? e : 127u) << 23;
+    *(lds_entry*)(list + (i & (T::kEntries - 1)) * 8) = u32x2{bad ? 0u : (unsigned)id, scale};
   };
-  // Half of load u's 16 elements, widened, to its place in the tile's LDS image.
-  const int row0 = (1024 * gw + 16 * lane) / D, chunk0 = lane % (D / 16) * 2;
-  constexpr int kRowStep = 4096 / D;  // rows from load 0 to load 1
-  auto put = [&](lds_char* tile, int u, int half) {
-    const int row = row0 + u * kRowStep;
-    const bf16x8 x = widen8(raw[u][2 * half], raw[u][2 * half + 1], scale[u]);
+  {
+    const int i = 64 * gw + lane, id0 = page_id(i), id1 = page_id(i + kHalf);
+    put_entry(i, id0);
+    put_entry(i + kHalf, id1);
+  }
+  wait_lds();
+  block_sync();  // the list is there
+  // Tile j's bytes, into registers: load u of a lane covers bytes 1024 n + 16 lane of the tile, n = gw + 4 u;
+  // at d = 128 both lie in the one page, at d = 64 load u in page u.  Its entries are read well before.
+  u32x4 raw[T::kLoads];
+  unsigned scale[T::kPages];
+  u32x2 entry[T::kPages];
+  auto read_entries = [&](int j) {
+#pragma unroll
+    for (int x = 0; x < T::kPages; ++x)
+      entry[x] = *(const lds_entry*)(list + ((j * T::kPages + x) & (T::kEntries - 1)) * 8);
+  };
+  const int lane_byte = 1024 * gw + 16 * lane;
+  auto load = [&](int j, int u) {
+    const int x = T::kPages == 2 ? u : 0;
+    const int id = __builtin_amdgcn_readfirstlane((int)entry[x][0]);
+    // tokens of the page (rows past them read as zeros); a scalar, as the descriptor has to be
+    const int n = __builtin_amdgcn_readfirstlane(max(0, min(kPage, len - (first + j * T::kPages + x) * kPage)));
+    __amdgpu_buffer_rsrc_t r = make_rsrc(bytes + (int64_t)id * H * (kPage * D), (uint32_t)(n * D));
+    raw[u] = __builtin_amdgcn_raw_buffer_load_b128(r, lane_byte + (T::kPages == 2 ? 0 : 4096 * u), 0, 0);
+    if (T::kPages == 2 || u == 0) scale[x] = __builtin_amdgcn_readfirstlane(entry[x][1]);
+  };
+  // Half of load u's 16 elements, widened (times sc), to its place in the tile's LDS image.
+  const int row0 = lane_byte / D, chunk0 = lane % (D / 16) * 2;
+  auto put = [&](lds_char* tile, int u, int half, unsigned sc) {
+    const int row = row0 + u * (4096 / D);
+    const bf16x8 x = widen8(raw[u][2 * half], raw[u][2 * half + 1], __uint_as_float(sc));
     lds_char* const to = kGroupB ? tile + row * G::kVRow + (((chunk0 + half) ^ G::vswz(row)) << 4)
                                  : tile + row * G::kKRow + ((chunk0 + half) << 4);
     *(lds_bf16x8*)to = x;
   };
-  // Renews half of the window when the pages about to be fetched (of tile j) enter its other half: the numbers
-  // first, the exponents that hang on them 16 pages later, 16 pages before they are needed.
+  // Renews half of the list when the tiles about to be fetched (tile j next) enter its other half: the page numbers
+  // first, the entries, which need the numbers to find the exponents, half way through.
+  int fresh = 0;
   auto renew = [&](int j) {
-    const int p = (it.tile_begin + j) * T::kPages;
-    if (p == window + 32) {
-      if (((lane - p) & 63) >= 32) pw.load_id(it.table, p + ((lane - p) & 63), pages);
-    } else if (p == window + 48) {
-      window += 32;
-      const int q = window + ((lane - window) & 63);
-      if (q >= window + 32) pw.load_exp(exps, a.pool, it.h, q, pages);
-    }
+    const int i = j * T::kPages, in_half = i & (kHalf - 1);
+    if (i >= kHalf && in_half == 0) fresh = page_id(i + kHalf + 64 * gw + lane);
+    if (i >= kHalf && in_half == kHalf / 2) put_entry(i + kHalf / 2 + 64 * gw + lane, fresh);
   };
   constexpr int kAhead = kGroupB ? 1 : 2;  // tiles between a vector step and the tile it writes
 
@@ -279,19 +292,21 @@ __device__ __forceinline__ void run_tile_group(const TileItem& it, const RowArgs
         const int row = (64 * n + lane) / G::kChunks;
         const int chunk = (lane % G::kChunks) ^ (D == 128 ? row & 15 : (row >> 1) & 7);
         const int r = qrow0 + row, t = a.G == 1 ? r : r / a.G;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_void*)(lds + T::kQBase + wave * G::kQWave + 1024 * n), 16,
-                                                 t * step + (r - t * a.G) * (D * 2) + chunk * 16, 0, 0, 0);
+        dma16(rq, lds + T::kQBase + wave * G::kQWave + 1024 * n, t * step + (r - t * a.G) * (D * 2) + chunk * 16);
       }
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
+      read_entries(j);
 #pragma unroll
       for (int u = 0; u < T::kLoads; ++u) load(j, u);
 #pragma unroll
       for (int u = 0; u < T::kLoads; ++u)
 #pragma unroll
-        for (int half = 0; half < 2; ++half) put(kGroupB ? vtile(j) : ktile(j), u, half);
+        for (int half = 0; half < 2; ++half)
+          put(kGroupB ? vtile(j) : ktile(j), u, half, scale[T::kPages == 2 ? u : 0]);
     }
+    read_entries(kAhead);
 #pragma unroll
     for (int u = 0; u < T::kLoads; ++u) load(kAhead, u);
   }
@@ -316,12 +331,12 @@ __device__ __forceinline__ void run_tile_group(const TileItem& it, const RowArgs
   for (int db = 0; db < D / 32; ++db) oacc[db] = f32x16{};
   f32x16 s[kBN / 32];
   bf16x8 p[kBN / 16];
-  bf16x8 kp[kPreReads];
-  f32x4 unused[2] = {};
+  bf16x8 kp[kPre];
+  f32x4 unused[2] = {};  // row sums of m_step
   float m_c = -INFINITY, l = 0.0f;
   const int ntiles = it.ntiles;
   const int last_keys = min(kBN, len - (it.tile_begin + ntiles - 1) * kBN);
-  if constexpr (kActive) k_preread<D>(ktile(0), kp, lane);
+  if constexpr (kActive) k_preread<D, kPre>(ktile(0), kp, lane);
   if (kGroupB) block_sync();  // group B starts one step behind
 
   // Vector step j: the softmax of tile j, and in four places of it the image of the tile fetched a step ago (each
@@ -331,8 +346,10 @@ __device__ __forceinline__ void run_tile_group(const TileItem& it, const RowArgs
     constexpr int kPlace = decltype(place)::value;
     lds_char* const to = kGroupB ? vtile(stage) : ktile(stage);
     renew(j + kAhead + 1);
+    read_entries(j + kAhead + 1);
+    const unsigned was = scale[0];  // of the bytes in the registers (at d = 64, where load 1 has its own, of load 0)
     auto hook = [&](int i) {
-      put(to, i >> 1, i & 1);
+      put(to, i >> 1, i & 1, i >> 1 && T::kPages == 2 ? scale[T::kPages - 1] : was);
       if (i & 1) load(j + kAhead + 1, i >> 1);
     };
     if constexpr (kActive) {
@@ -342,7 +359,7 @@ __device__ __forceinline__ void run_tile_group(const TileItem& it, const RowArgs
       for (int i = 0; i < kHooks; ++i) hook(i);
     }
     wait_lds();
-    if (kActive && kPlace != kLast) k_preread<D>(ktile((j + 1) % T::kKStages), kp, lane);
+    if (kActive && kPlace != kLast) k_preread<D, kPre>(ktile((j + 1) % T::kKStages), kp, lane);
   };
   using First = std::integral_constant<int, kFirst>;
   using Inner = std::integral_constant<int, kInner>;
@@ -353,7 +370,7 @@ __device__ __forceinline__ void run_tile_group(const TileItem& it, const RowArgs
 
   if constexpr (kActive) {
     __builtin_amdgcn_s_setprio(1);
-    m_step<D, false, false>(ktile(0), vtile(0), vo, qf, kp, s, p, oacc, bf16x8{}, unused, lane);
+    m_step<D, false, false, kPre>(ktile(0), lds, vo, qf, kp, s, p, oacc, bf16x8{}, unused, lane);
     __builtin_amdgcn_s_setprio(0);
   }
   block_sync();
@@ -365,8 +382,12 @@ __device__ __forceinline__ void run_tile_group(const TileItem& it, const RowArgs
     block_sync();  // closes V(j - 1)
     if constexpr (kActive) {
       __builtin_amdgcn_s_setprio(1);
-      m_step<D, true, false>(ktile(ks), vtile((j - 1) & 1), vo, qf, kp, s, p, oacc, bf16x8{}, unused, lane);
+      m_step<D, true, false, kPre>(ktile(ks), lds, vo, qf, kp, s, p, oacc, bf16x8{}, unused, lane);
       __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+      for (int r2 = 0; r2 < 2; ++r2)
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) vo.off[r2][db] ^= G::kVTile;
     }
     block_sync();
     vector(j, place);
@@ -375,72 +396,83 @@ __device__ __forceinline__ void run_tile_group(const TileItem& it, const RowArgs
   for (; j < ntiles - 1; ++j) tile(j, Inner{});
   if (j == ntiles - 1) tile(j, Last{});
   block_sync();  // closes V(ntiles - 1)
-  if constexpr (kActive) pv_tile<D>(vtile((ntiles - 1) & 1), vo, p, oacc);
+  if constexpr (kActive) pv_tile<D>(lds, vo, p, oacc);
   if (!kGroupB) block_sync();  // matches group B's extra barrier at the start
 
   if constexpr (kActive) {
     auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
-    write_rows<D, kPartial>(it, a, oacc, __uint_as_float(r[0]) + __uint_as_float(r[1]), m_c, it.row0 + 32 * wave,
-                            lds + T::kOBase + wave * G::kOWave, lane);
+    l = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    write_rows<D, kPartial>(it, a, oacc, l, m_c, it.row0 + 32 * wave, lds + T::kOBase + wave * G::kOWave, lane);
   }
 }
 
-// The sessions' items, and the one of a workgroup.  Up to 64 sessions are put in order of their lengths by every
-// wave itself, longest first, one per lane, so that a call of unequal sessions ends evenly; more keep their order.
+// The item of a workgroup.  A session has H x n_split x ceil(rows / 256) items, head-major, then by page range, then
+// by row tile, so that neighbours read the same keys.  The hardware deals workgroups to the eight XCDs in turn,
+// workgroup b to XCD b % 8, and an XCD starts its own in order.  Every XCD gets a consecutive eighth of each
+// session's items (what is left over goes to the XCDs in turn, from session to session), so an eighth of the
+// keys passes through its L2, and the XCDs have equal work; within an XCD the longest sessions come first, so
+// that it ends evenly.  Up to 64 sessions are put in order by every wave itself, one per lane; more keep their order.
+// (Spans of 8 x 32 items dealt over the XCDs instead leave the first ones all the long items: six sessions of 2730 to
+// 32760 keys x 1560 queries x 12 heads took 1170 us instead of 1044.)
+struct Share {  // of a session's `count` items, `before` items of earlier sessions: this XCD's
+  int n, first;
+  __device__ __forceinline__ Share(int count, int before, int xcd) {
+    const int y = (xcd - before) & 7, q = count >> 3, r = count & 7;
+    n = q + (y < r ? 1 : 0);
+    first = y * q + min(y, r);
+  }
+};
+
 template <int D>
-__device__ __forceinline__ bool find_item(const RowArgs& a, int chunk, TileItem* it) {
+__device__ __forceinline__ bool find_item(const RowArgs& a, TileItem* it) {
   const int lane = threadIdx.x & 63, per_tile = a.pool.H * a.n_split;
-  int s, local;
+  const int xcd = blockIdx.x & 7, at = blockIdx.x >> 3;  // the at-th workgroup of that XCD
   auto items_of = [&](const Session& se) {
     return se.ok ? per_tile * (int)(((int64_t)se.rows * a.G + kBM - 1) / kBM) : 0;
   };
+  int s = -1, local = 0;
   if (a.ss.nseq <= 64) {
     Session mine{};
     if (lane < a.ss.nseq) mine = session_of(a.ss, lane);
     const int count = lane < a.ss.nseq ? items_of(mine) : 0;
-    int before = 0, total = 0;
-    for (int i = 0; i < a.ss.nseq; ++i) {
-      const int li = __builtin_amdgcn_readlane(mine.len, i), ci = __builtin_amdgcn_readlane(count, i);
-      before += li > mine.len || (li == mine.len && i < lane) ? ci : 0;
-      total += ci;
+    auto earlier = [&](int i, int li) { return li > mine.len || (li == mine.len && i < lane); };
+    int before = 0, start = 0;
+    for (int i = 0; i < a.ss.nseq; ++i)
+      before += earlier(i, __builtin_amdgcn_readlane(mine.len, i)) ? __builtin_amdgcn_readlane(count, i) : 0;
+    const Share share(count, before, xcd);
+    for (int i = 0; i < a.ss.nseq; ++i)
+      start += earlier(i, __builtin_amdgcn_readlane(mine.len, i)) ? __builtin_amdgcn_readlane(share.n, i) : 0;
+    const unsigned long long hit = __builtin_amdgcn_ballot_w64(start <= at && at - start < share.n);
+    if (hit != 0) {
+      s = __builtin_ctzll(hit);
+      local = at - __builtin_amdgcn_readlane(start, s) + __builtin_amdgcn_readlane(share.first, s);
     }
-    if ((int)blockIdx.x >= total) return false;
-    const int item = remap_block(blockIdx.x, total, chunk);
-    s = __builtin_ctzll(__builtin_amdgcn_ballot_w64(before <= item && item - before < count));
-    local = item - __builtin_amdgcn_readlane(before, s);
   } else {
-    // Two walks over the sessions, 64 at a time: the items in all, then the one that holds this workgroup's.
-    int total = 0, item = 0;
-    s = -1, local = 0;
-    for (int walk = 0; walk < 2 && s < 0; ++walk) {
-      int base = 0;
-      for (int s0 = 0; s0 < a.ss.nseq && s < 0; s0 += 64) {
-        const int count = s0 + lane < a.ss.nseq ? items_of(session_of(a.ss, s0 + lane)) : 0;
-        int sum = count;
+    auto scan = [&](int x) {  // inclusive, over the lanes
 #pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-          const int y = __shfl_up(sum, m);
-          if (lane >= m) sum += y;
-        }
-        const int before = base + sum - count;
-        if (walk == 1) {
-          const unsigned long long hit = __builtin_amdgcn_ballot_w64(before <= item && item - before < count);
-          if (hit != 0) {
-            const int i = __builtin_ctzll(hit);
-            s = s0 + i;
-            local = item - __builtin_amdgcn_readlane(before, i);
-          }
-        }
-        base += __builtin_amdgcn_readlane(sum, 63);
+      for (int m = 1; m < 64; m <<= 1) {
+        const int y = __shfl_up(x, m);
+        if (lane >= m) x += y;
       }
-      if (walk == 0) {
-        total = base;
-        if ((int)blockIdx.x >= total) return false;
-        item = remap_block(blockIdx.x, total, chunk);
+      return x;
+    };
+    int items = 0, base = 0;  // of the sessions so far: in all, and this XCD's
+    for (int s0 = 0; s0 < a.ss.nseq && s < 0; s0 += 64) {
+      const int count = s0 + lane < a.ss.nseq ? items_of(session_of(a.ss, s0 + lane)) : 0;
+      const int counts = scan(count);
+      const Share share(count, items + counts - count, xcd);
+      const int shares = scan(share.n), start = base + shares - share.n;
+      const unsigned long long hit = __builtin_amdgcn_ballot_w64(start <= at && at - start < share.n);
+      if (hit != 0) {
+        const int i = __builtin_ctzll(hit);
+        s = s0 + i;
+        local = at - __builtin_amdgcn_readlane(start, i) + __builtin_amdgcn_readlane(share.first, i);
       }
+      items += __builtin_amdgcn_readlane(counts, 63);
+      base += __builtin_amdgcn_readlane(shares, 63);
     }
-    if (s < 0) return false;
   }
+  if (s < 0) return false;
   // everything about the item is the same in all lanes: in scalar registers
   s = __builtin_amdgcn_readfirstlane(s);
   local = __builtin_amdgcn_readfirstlane(local);
@@ -462,27 +494,34 @@ __device__ __forceinline__ bool find_item(const RowArgs& a, int chunk, TileItem*
   return true;
 }
 
+// A last tile of at most this many rows is shared by the eight waves, each taking pages of its own (rows_item): in
+// the schedule above one wave would work and seven keep its barriers, for as long as a full tile takes (those six
+// sessions, whose last tiles have 24 rows: 1098 us instead of 1044).
+constexpr int kThinRows = 32;
+
+template <int D>
+constexpr int tiles_lds() {
+  return TileGeo<D>::kLds > RowGeo<D, kThinRows / 16, kWaves>::kLds ? TileGeo<D>::kLds
+                                                                   : RowGeo<D, kThinRows / 16, kWaves>::kLds;
+}
+
 template <int D, bool kPartial>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
-cache_tiles_kernel(RowArgs a, int chunk) {
+cache_tiles_kernel(RowArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   TileItem it;
-  if (!find_item<D>(a, chunk, &it)) return;
+  if (!find_item<D>(a, &it)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const bool active = it.row0 + 32 * wave < it.rows;
-  if (it.ntiles <= 0) {  // no keys: zeros, or nothing but the log-sum-exp of an empty range
-    if (!active) return;
-    const int lane = threadIdx.x & 63, r = it.row0 + 32 * wave + (lane & 31);
-    if (r >= it.rows) return;
-    const int64_t row = row_of(it.se, r, it.h, a.pool.H, a.G);
-    if (kPartial) {
-      if (lane < 32) a.part_lse[(int64_t)it.split * a.ss.total * (a.pool.H * a.G) + row] = -INFINITY;
-      return;
-    }
-    for (int c = lane >> 5; c < D / 8; c += 2) *(u32x4*)(a.o + row * D + 8 * c) = u32x4{};
-    if (a.lse != nullptr && lane < 32) a.lse[row] = -INFINITY;
+  if (it.ntiles <= 0 || it.rows - it.row0 <= kThinRows) {
+    // (without keys as well: zeros, or nothing but the log-sum-exp of an empty range)
+    const int begin = it.tile_begin * TileGeo<D>::kPages;
+    const int end = min((it.se.len + kPage - 1) / kPage, begin + it.ntiles * TileGeo<D>::kPages);
+    const int last = min(it.rows, it.row0 + kBM);
+    for (int row0 = it.row0; row0 < last; row0 += kThinRows)
+      rows_item<D, kThinRows / 16, kWaves, kPartial>(a, it.se, it.table, it.h, row0, it.rows, begin, end, it.split, smem);
     return;
   }
+  const bool active = it.row0 + 32 * wave < it.rows;
   if (wave >= kWaves / 2) {
     if (active) run_tile_group<D, true, kPartial, true>(it, a, smem);
     else run_tile_group<D, true, kPartial, false>(it, a, smem);
@@ -492,32 +531,32 @@ cache_tiles_kernel(RowArgs a, int chunk) {
   }
 }
 
-hipError_t configure_tiles() {
-  const struct {
-    const void* kern;
-    int lds;
-  } all[] = {{(const void*)cache_tiles_kernel<64, false>, TileGeo<64>::kLds},
-             {(const void*)cache_tiles_kernel<64, true>, TileGeo<64>::kLds},
-             {(const void*)cache_tiles_kernel<128, false>, TileGeo<128>::kLds},
-             {(const void*)cache_tiles_kernel<128, true>, TileGeo<128>::kLds}};
-  for (const auto& k : all) {
-    const hipError_t e = hipFuncSetAttribute(k.kern, hipFuncAttributeMaxDynamicSharedMemorySize, k.lds);
+template <int D>
+static hipError_t configure_d() {
+  const void* const all[] = {(const void*)cache_tiles_kernel<D, false>, (const void*)cache_tiles_kernel<D, true>};
+  for (const void* kern : all) {
+    const hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, tiles_lds<D>());
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
-template <int D>
-static void launch_tiles_d(const RowArgs& r, unsigned grid, int chunk, hipStream_t st) {
-  auto kern = r.n_split > 1 ? cache_tiles_kernel<D, true> : cache_tiles_kernel<D, false>;
-  hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), TileGeo<D>::kLds, st, r, chunk);
+hipError_t configure_tiles() {
+  const hipError_t e = configure_d<64>();
+  return e != hipSuccess ? e : configure_d<128>();
 }
 
-// RowArgs' workgroups are 256-row tiles of a session and head here.
-void launch_tiles(const RowArgs& r, int d, unsigned grid, int cus, hipStream_t st) {
-  const int chunk = cus / 8 > 0 ? cus / 8 : 1;  // consecutive items of an XCD
-  if (d == 64) launch_tiles_d<64>(r, grid, chunk, st);
-  else launch_tiles_d<128>(r, grid, chunk, st);
+template <int D>
+static void launch_tiles_d(const RowArgs& r, unsigned grid, hipStream_t st) {
+  auto kern = r.n_split > 1 ? cache_tiles_kernel<D, true> : cache_tiles_kernel<D, false>;
+  hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), tiles_lds<D>(), st, r);
+}
+
+// RowArgs' workgroups are 256-row tiles of a session and head here, `items` of them at most.
+void launch_tiles(const RowArgs& r, int d, int64_t items, hipStream_t st) {
+  const unsigned grid = (unsigned)((items + 7) / 8 * 8);  // every XCD has up to ceil(items / 8)
+  if (d == 64) launch_tiles_d<64>(r, grid, st);
+  else launch_tiles_d<128>(r, grid, st);
 }
 
 }  // namespace tscache

@@ -656,6 +656,25 @@ def test_more_sessions_than_lanes():
     run_attn(g, rows, lens, 1, 1, 64)
 
 
+def test_more_sessions_than_lanes_in_large_tiles():
+    g = torch.Generator().manual_seed(19)
+    rows = [(i * 53) % 301 for i in range(70)]
+    lens = [(i * 37) % 200 for i in range(70)]
+    run_attn(g, rows, lens, 1, 1, 64)
+
+
+@pytest.mark.parametrize("d,rows,splits", [(64, 40, 1), (128, 40, 1), (128, 290, 2), (64, 3, 1), (128, 20, 2)])
+def test_attn_long_sessions(d, rows, splits):
+    """More pages than an item keeps at hand at once; the longer session ends inside a page and inside a tile, and a
+    page far behind is outside the pool."""
+    g = torch.Generator().manual_seed(d + rows)
+    lens = [100_031, 40_000]
+    cache, table, cu, q, o, lse = run_attn(g, [rows, 33], lens, 1, 1, d, num_splits=splits)
+    table[1][600] = 1 << 29
+    o2 = ts.ts_cache_attn(q.cuda(), cache, ints(cu), max(rows, 33), ints(table), ints(lens), max(lens), num_splits=splits)
+    assert torch.equal(o2[:rows], o[:rows]) and torch.isnan(o2[rows:]).all()
+
+
 def test_validation_mode(monkeypatch):
     from paper_2606_19271_amd import _lib
     g = torch.Generator().manual_seed(16)
