@@ -14,7 +14,7 @@ SOURCES = [os.path.join(CSRC, "attn_kernels.hip"), os.path.join(CSRC, "state_cop
 
 CACHE_LIB = os.path.join(HERE, "libts_cache.so")
 CACHE_SOURCES = [os.path.join(CSRC, "cache_attn.hip"), os.path.join(CSRC, "cache_tiles.hip"),
-                 os.path.join(CSRC, "cache_pages.hip"),
+                 os.path.join(CSRC, "cache_weigh.hip"), os.path.join(CSRC, "cache_pages.hip"),
                  os.path.join(CSRC, "cache_plan.cpp"), os.path.join(CSRC, "ts_cache.cpp")]
 
 SCHED_LIB = os.path.join(HERE, "libts_sched.so")

@@ -1,5 +1,5 @@
-// cache_attn.hip -- gfx950 kernels that read the session cache's pages: attention, and the weight that
-// its queries give to each cached token.
+// cache_attn.hip -- attention over the session cache's pages: the kernel for few query rows, the merge of split
+// calls, and the choice between the kernels.
 //
 // For every session s, query row t of it, query head hq (of cached head h = hq / G):
 //   O[t,hq,:] = softmax_j(scale <Q[t,hq,:], K[j,h,:]>) V[j,h,:]   over the session's cached tokens j.
@@ -73,79 +73,6 @@ __global__ void __launch_bounds__(kMergeThreads) cache_merge_kernel(RowArgs a, i
   if (a.lse != nullptr && ch == 0) a.lse[row] = sum == 0.0f ? -INFINITY : big + log2f(sum) * kLn2;
 }
 
-// ---- the weight that the queries give to each cached token: column sums of the softmax, one workgroup
-// per (session, page, head).  A wave holds the page's keys as MFMA operands and takes every fourth tile of 32
-// query rows: S^T = K Q^T on 32x32x16 MFMAs (lane: query row lane & 31), weights against the rows' lse, and
-// their sums over the rows in the lane, across the lanes at the end.
-template <int D>
-__global__ void __launch_bounds__(kRowThreads)
-cache_weigh_kernel(Pool pool, Sessions ss, const __bf16* __restrict__ q, const float* __restrict__ lse,
-                   float* __restrict__ out, int G, int page_slots, float c, unsigned flip) {
-  constexpr int kKK = D / 16;
-  __shared__ float sums[kRowWaves][kPage];
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int col = lane & 31, hb = lane >> 5;
-  const int H = pool.H;
-  int b = blockIdx.x;
-  const int p = b % page_slots;
-  b /= page_slots;
-  const int h = b % H, s = b / H;
-  const Session se = session_of(ss, s);
-  if (!se.ok || p * kPage >= se.len) return;
-  const int page = ss.table[(int64_t)s * ss.width + p];
-  if ((unsigned)page >= (unsigned)pool.pages) return;
-  const int64_t ph = (int64_t)page * H + h;
-  const float ks = scale_of(pool.k_exp[ph], false);
-  bf16x8 kf[2][kKK];
-#pragma unroll
-  for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-    for (int x = 0; x < kKK / 2; ++x) {
-      const u32x4 y = *(const u32x4*)(pool.k + ph * (kPage * D) + (32 * kb + col) * D + D / 2 * hb + 16 * x);
-      kf[kb][2 * x] = widen8(y[0], y[1], ks);
-      kf[kb][2 * x + 1] = widen8(y[2], y[3], ks);
-    }
-  const int rows = se.rows * G;
-  f32x16 acc[2] = {};
-  for (int r0 = 32 * wave; r0 < rows; r0 += 32 * kRowWaves) {
-    const int r = r0 + col;
-    const int64_t at = row_of(se, min(r, rows - 1), h, H, G);
-    const float ls = r < rows ? lse[at] * kLog2e : INFINITY;  // rows past the end weigh nothing
-    f32x16 sc[2] = {};
-#pragma unroll
-    for (int kk = 0; kk < kKK; ++kk) {
-      const bf16x8 qf = __builtin_bit_cast(
-          bf16x8, *(const u32x4*)(q + at * D + D / 2 * hb + 8 * kk) ^ u32x4{flip, flip, flip, flip});
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) sc[kb] = mfma32(kf[kb][kk], qf, sc[kb]);
-    }
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kb][i], c, -ls));
-        acc[kb][i] += r < rows ? w : 0.0f;
-      }
-  }
-#pragma unroll
-  for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float x = acc[kb][i];
-#pragma unroll
-      for (int m = 1; m < 32; m <<= 1) x += __shfl_xor(x, m);
-      if (col == 0) sums[wave][32 * kb + 8 * (i >> 2) + 4 * hb + (i & 3)] = x;
-    }
-  __syncthreads();
-  if (tid < kPage && p * kPage + tid < se.len) {
-    float x = pool.weight[ph * kPage + tid];
-#pragma unroll
-    for (int w = 0; w < kRowWaves; ++w) x += sums[w][tid];
-    out[ph * kPage + tid] = x;
-  }
-}
-
 // ---------------------------------------------------------------------------------------------
 // host-side launchers
 
@@ -175,15 +102,6 @@ static hipError_t launch_attn_d(const AttnArgs& a, hipStream_t st) {
 
 hipError_t launch_attn(const AttnArgs& a, hipStream_t st) {
   return a.d == 64 ? launch_attn_d<64>(a, st) : launch_attn_d<128>(a, st);
-}
-
-hipError_t launch_weigh(const WeighArgs& a, hipStream_t st) {
-  const int64_t items = weigh_items(a.ss.nseq, a.ss.max_len, a.pool.H);
-  auto kern = a.d == 64 ? cache_weigh_kernel<64> : cache_weigh_kernel<128>;
-  hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(kRowThreads), 0, st, a.pool, a.ss, (const __bf16*)a.q,
-                     a.lse, a.out, a.G, (a.ss.max_len + kPage - 1) / kPage, fabsf(a.scale) * kLog2e,
-                     a.scale < 0.0f ? 0x80008000u : 0u);
-  return hipGetLastError();
 }
 
 hipError_t configure_kernels() { return configure_tiles(); }

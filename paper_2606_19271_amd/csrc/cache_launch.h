@@ -86,6 +86,10 @@ int32_t auto_splits(int32_t nseq, int32_t max_rows, int32_t max_len, int32_t tot
 int64_t workspace_bytes(int32_t n, int32_t total, int32_t Hq, int32_t d);
 int64_t part_o_offset(int32_t n, int32_t total, int32_t Hq);
 // Workgroups of the other kernels.
+// weigh: a page to a workgroup where there are few, else four pages of a head, in 8 XCDs x nseq sessions x weigh_share
+// workgroups, at most weigh_items.
+bool weigh_few(int32_t nseq, int32_t max_len, int32_t H, int32_t cus);
+int64_t weigh_share(int32_t max_len, int32_t H);
 int64_t weigh_items(int32_t nseq, int32_t max_len, int32_t H);
 int64_t append_items(int32_t nseq, int32_t max_rows, int32_t H);
 int64_t gather_items(int32_t nseq, int32_t keep, int32_t H);

@@ -57,9 +57,15 @@ int64_t workspace_bytes(int32_t n, int32_t total, int32_t Hq, int32_t d) {
   return n > 1 ? part_o_offset(n, total, Hq) + (int64_t)n * total * Hq * d * 4 : 0;
 }
 
+bool weigh_few(int32_t nseq, int32_t max_len, int32_t H, int32_t cus) {
+  return (int64_t)nseq * H * ceil_div(max_len, 4 * kPage) <= 2 * (int64_t)cus;
+}
+
+int64_t weigh_share(int32_t max_len, int32_t H) { return ceil_div((int64_t)H * ceil_div(max_len, 4 * kPage), 8); }
+
 int64_t weigh_items(int32_t nseq, int32_t max_len, int32_t H) {
-  const int64_t pages = ceil_div(max_len, kPage), heads = (int64_t)nseq * H;
-  return pages > 0 && heads > 4 * kGridLimit / pages ? 4 * kGridLimit : heads * pages;
+  const int64_t share = weigh_share(max_len, H);
+  return share > 0 && nseq > kGridLimit / share ? 4 * kGridLimit : 8 * nseq * share;
 }
 
 int64_t append_items(int32_t nseq, int32_t max_rows, int32_t H) {

@@ -375,6 +375,42 @@ def test_weigh(rows, lens, H, G, d, scale):
     assert abs(after[live].sum() - before - given) <= 1e-4 * max(given, before, 1)
 
 
+@pytest.mark.parametrize("d,G,rows,lens", [(128, 1, [70, 1, 0], [60_000, 30_001, 5_000]), (64, 3, [200, 3, 64], [50_000, 999, 60_064]),
+                                           (128, 5, [13, 300], [64_000, 20_000])])
+def test_weigh_many_keys(d, G, rows, lens):
+    """Enough keys for several groups of pages to a workgroup, sessions of unequal length, a bad page among them."""
+    g = torch.Generator().manual_seed(d + G)
+    H = 2
+    width = -(-max(lens) // PAGE)
+    pages = sum(-(-n // PAGE) for n in lens) + 2
+    cache = make_pool(g, pages, H, d)
+    table, _ = make_table(g, lens, width, pages)
+    table[0][100] = pages + 7
+    cu = offsets(rows)
+    q = bf16(normal(g, cu[-1], H * G, d))
+    lse = (10 + normal(g, cu[-1], H * G)).cuda()
+    pool = R.Pool.of(cache)
+    scale = float(np.float32(1 / math.sqrt(d)))
+    with np.errstate(invalid="ignore"):
+        want = R.weigh(pool, q.double().numpy(), lse.double().cpu().numpy(), cu, table, lens, scale)
+    out = torch.full_like(cache.weight, 5.0)
+    ts.ts_cache_weigh(q.cuda(), lse, cache, ints(cu), max(rows), ints(table), ints(lens), max(lens), out=out)
+    got = out.double().cpu().numpy()
+    live = np.zeros(want.shape, bool)
+    for s, n in enumerate(lens):
+        for j in range(0, n, PAGE):
+            if table[s][j // PAGE] < pages:
+                live[table[s][j // PAGE], :, :min(PAGE, n - j)] = True
+    assert np.all(got[~live] == 5)
+    most = abs(scale) * float((q.float().abs().sum(2).max())) * 64
+    rel = (d + 2) * 2.0 ** -24 * most + (max(rows) * G + 8) * 2.0 ** -24 + 2.0 ** -20
+    # (an lse that is not these rows' own lets single weights pass the largest float32: those are infinite)
+    over = live & (want > np.finfo(np.float32).max)
+    assert np.all(np.isinf(got[over]))
+    live &= ~over
+    assert (np.abs(got - want)[live] / want[live]).max() <= rel
+
+
 def test_weigh_bad_sessions_and_pages():
     g = torch.Generator().manual_seed(3)
     H, d = 2, 64
