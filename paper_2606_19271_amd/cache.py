@@ -17,12 +17,13 @@ import os
 from typing import NamedTuple
 
 import torch
+from torch import Tensor
 
-from . import _lib
-from .attention import _call, _check_offsets, _check_tensor, _scale
+from .attention import _call, _scale
 from .build import CACHE_LIB
 
 PAGE = 64
+_E4M3, _U8, _I32, _F32, _BF16 = torch.float8_e4m3fn, torch.uint8, torch.int32, torch.float32, torch.bfloat16
 
 _cache_lib = None
 
@@ -75,81 +76,107 @@ def load_cache():
     return lib
 
 
+def _not(t, dtype, dim, index):
+    """Whether t is anything but a contiguous `dim`-dimensional tensor of this type on GPU `index`."""
+    return (not isinstance(t, Tensor) or t.dtype is not dtype or t.dim() != dim or t.get_device() != index
+            or not t.is_contiguous())
+
+
 def _pool(cache, need_weight=False):
-    """(struct ts_cache, device) of a SessionCache, whose tensors have to fit each other."""
+    """(struct ts_cache, device, its index) of a SessionCache, whose tensors have to fit each other."""
     k, v, k_exp, v_exp, weight = cache
-    for name, t, dtype in (("k", k, torch.float8_e4m3fn), ("v", v, torch.float8_e4m3fn), ("k_exp", k_exp, torch.uint8),
-                           ("v_exp", v_exp, torch.uint8)):
-        if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
-            raise ValueError("cache.%s must be a contiguous %s GPU tensor" % (name, dtype))
-    shape = k.shape
-    if len(shape) != 4 or shape[2] != PAGE or v.shape != shape or k_exp.shape != shape[:2] or v_exp.shape != shape[:2]:
-        raise ValueError("a cache is k, v [pages, H, %d, d] and k_exp, v_exp [pages, H]" % PAGE)
+    if not isinstance(k, Tensor) or not k.is_cuda:
+        raise ValueError("cache.k must be a contiguous float8_e4m3fn GPU tensor")
     dev = k.device
-    if v.device != dev or k_exp.device != dev or v_exp.device != dev:
-        raise ValueError("a cache's tensors must be on one device")
+    index = dev.index
+    for name, t, dtype, dim in (("k", k, _E4M3, 4), ("v", v, _E4M3, 4), ("k_exp", k_exp, _U8, 2), ("v_exp", v_exp, _U8, 2)):
+        if _not(t, dtype, dim, index):
+            raise ValueError("cache.%s must be a contiguous %s tensor with %d dims on one GPU" % (name, dtype, dim))
+    shape = k.shape
+    pages, H, rows, d = shape
+    if rows != PAGE or v.shape != shape or k_exp.shape != (pages, H) or v_exp.shape != (pages, H):
+        raise ValueError("a cache is k, v [pages, H, %d, d] and k_exp, v_exp [pages, H]" % PAGE)
     if weight is not None:
-        _check_weight("cache.weight", weight, shape, dev)
+        _check_weight("cache.weight", weight, shape, index)
     elif need_weight:
         raise ValueError("this call needs the cache's weight")
-    pages, H, _, d = shape
-    _lib.i32s(pages=pages, H=H, d=d)
+    _i32s("pages, H, d", pages, H, d)
     return _Pool(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
-                 None if weight is None else weight.data_ptr(), pages, H, d), dev
+                 None if weight is None else weight.data_ptr(), pages, H, d), dev, index
 
 
-def _check_weight(name, t, shape, dev):
-    if (not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or t.shape != shape[:3] or t.device != dev
-            or not t.is_contiguous()):
+def _i32s(names, *values):
+    """The sizes as C int32 arguments (ctypes would silently wrap a larger one)."""
+    values = [int(x) for x in values]
+    if min(values) < -(1 << 31) or max(values) >= 1 << 31:
+        raise ValueError("%s = %s do not fit the C ABI's int32" % (names, values))
+    return values
+
+
+def _check_weight(name, t, shape, index):
+    if _not(t, _F32, 3, index) or t.shape != shape[:3]:
         raise ValueError("%s must be a contiguous float32 [pages, H, %d] tensor on the cache's device" % (name, PAGE))
 
 
-def _check_ints(name, t, dim, dev):
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.dim() != dim or t.device != dev or not t.is_contiguous():
+def _check_ints(name, t, dim, index):
+    if _not(t, _I32, dim, index):
         raise ValueError("%s must be a contiguous int32 tensor with %d dims on the cache's device" % (name, dim))
 
 
-def _sessions(table, lens, dev):
-    """(nseq, width)"""
-    _check_ints("table", table, 2, dev)
-    _check_ints("lens", lens, 1, dev)
-    if table.shape[0] != lens.shape[0]:
+def _sessions(cu, table, lens, index):
+    """(nseq, width); cu, the sessions' rows, is None for a call without rows."""
+    _check_ints("table", table, 2, index)
+    _check_ints("lens", lens, 1, index)
+    nseq, width = table.shape
+    if lens.numel() != nseq:
         raise ValueError("table and lens must have one row per session")
-    return table.shape
+    if cu is not None:
+        _check_ints("cu_seqlens", cu, 1, index)
+        if cu.numel() != nseq + 1:
+            raise ValueError("cu_seqlens must have one more entry than there are sessions")
+    return nseq, width
 
 
-def _rows(name, t, H, d, dev, groups=False):
-    _check_tensor(name, t, 3)
-    if t.device != dev or t.shape[2] != d or (t.shape[1] % H if groups else t.shape[1] != H) or t.shape[1] == 0:
-        raise ValueError("%s must be [rows, %s, %d] on the cache's device" % (name, "a multiple of %d" % H if groups else H, d))
+def _rows(name, t, H, d, index, groups=False):
+    if not isinstance(t, Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if _not(t, _BF16, 3, index):
+        raise ValueError("%s must be a contiguous bfloat16 tensor with 3 dims on the cache's device" % name)
+    _, heads, channels = t.shape
+    if channels != d or (heads % H if groups else heads != H) or heads == 0:
+        raise ValueError("%s must be [rows, %s, %d]" % (name, "a multiple of %d" % H if groups else H, d))
 
 
-def _cu(cu, nseq, dev):
-    _check_offsets("cu_seqlens", cu, dev)
-    if cu.numel() != nseq + 1:
-        raise ValueError("cu_seqlens must have one more entry than there are sessions")
+def _lens_out(out, lens, index):
+    if out is None:
+        return torch.empty_like(lens)
+    _check_ints("out", out, 1, index)
+    if out.shape != lens.shape:
+        raise ValueError("out must match lens")
+    return out
+
+
+def _check_lse(lse, T, Hq, index):
+    if _not(lse, _F32, 2, index) or lse.shape != (T, Hq):
+        raise ValueError("lse must be a contiguous float32 [T, Hq] tensor on the cache's device")
 
 
 def ts_cache_append(cache, k, v, cu_seqlens, max_seqlen, table, lens, out=None):
     """Appends each session's new tokens to its pages: k, v are bfloat16 [T, H, d], session s's rows
     [cu_seqlens[s], cu_seqlens[s+1]), at most max_seqlen of them, becoming its tokens lens[s], lens[s] + 1, ...
     of the pages table[s] (int32 [nseq, width]).  Returns the new lengths (int32 [nseq], or `out`)."""
-    pool, dev = _pool(cache)
-    nseq, width = _sessions(table, lens, dev)
-    _rows("k", k, pool.H, pool.d, dev)
-    _rows("v", v, pool.H, pool.d, dev)
-    if v.shape != k.shape:
+    pool, dev, index = _pool(cache)
+    nseq, width = _sessions(cu_seqlens, table, lens, index)
+    H, d = pool.H, pool.d
+    _rows("k", k, H, d, index)
+    _rows("v", v, H, d, index)
+    T = k.shape[0]
+    if v.shape[0] != T:
         raise ValueError("k and v must have one shape")
-    _cu(cu_seqlens, nseq, dev)
-    if out is None:
-        out = torch.empty_like(lens)
-    else:
-        _check_ints("out", out, 1, dev)
-        if out.shape != lens.shape:
-            raise ValueError("out must match lens")
+    out = _lens_out(out, lens, index)
     _call(load_cache().ts_cache_append, dev, ctypes.addressof(pool), k.data_ptr(), v.data_ptr(), cu_seqlens.data_ptr(),
           table.data_ptr(), lens.data_ptr(), out.data_ptr(),
-          *_lib.i32s(nseq=nseq, width=width, max_seqlen=max_seqlen, T=k.shape[0]))
+          *_i32s("nseq, width, max_seqlen, T", nseq, width, max_seqlen, T))
     return out
 
 
@@ -160,39 +187,35 @@ def ts_cache_attn(q, cache, cu_seqlens, max_seqlen, table, lens, max_len, scale=
     [cu_seqlens[s], cu_seqlens[s+1]), at most max_seqlen of them, over its lens[s] <= max_len tokens.  Returns o
     [T, Hq, d], or (o, lse) with lse float32 [T, Hq] when return_lse is set or an lse tensor is passed.
     num_splits: 0 lets the library choose, 1..64 forces that many page ranges per query tile."""
-    pool, dev = _pool(cache)
-    nseq, width = _sessions(table, lens, dev)
-    _rows("q", q, pool.H, pool.d, dev, groups=True)
-    _cu(cu_seqlens, nseq, dev)
+    pool, dev, index = _pool(cache)
+    nseq, width = _sessions(cu_seqlens, table, lens, index)
+    _rows("q", q, pool.H, pool.d, index, groups=True)
     T, Hq, d = q.shape
     if out is None:
         out = torch.empty_like(q)
     else:
-        _check_tensor("out", out, 3)
-        if out.shape != q.shape or out.device != dev:
+        if _not(out, _BF16, 3, index) or out.shape != q.shape:
             raise ValueError("out must match q")
     if lse is None and return_lse:
-        lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
-    if lse is not None:
-        _check_lse(lse, T, Hq, dev)
-    sizes = _lib.i32s(nseq=nseq, width=width, max_seqlen=max_seqlen, max_len=max_len, T=T, Hq=Hq)
-    num_splits = _lib.i32("num_splits", num_splits)
+        lse = q.new_empty((T, Hq), dtype=_F32)
+    elif lse is not None:
+        _check_lse(lse, T, Hq, index)
+    sizes = _i32s("nseq, width, max_seqlen, max_len, T, Hq, num_splits", nseq, width, max_seqlen, max_len, T, Hq, num_splits)
+    num_splits = sizes.pop()
     lib = load_cache()
-    with torch.cuda.device(dev):
-        need = lib.ts_cache_attn_workspace(nseq, sizes[2], sizes[3], T, pool.H, Hq, d, num_splits)
+    asked = nseq, sizes[2], sizes[3], T, pool.H, Hq, d, num_splits
+    if torch.cuda.current_device() == index:
+        need = lib.ts_cache_attn_workspace(*asked)
+    else:
+        with torch.cuda.device(dev):
+            need = lib.ts_cache_attn_workspace(*asked)
     # from torch's allocator: the memory goes back to the current stream's pool (or, while a graph is
     # captured, the graph's own) when the call is enqueued, so no other work meets it
-    work = torch.empty(need, dtype=torch.uint8, device=dev) if need > 0 else None
+    work = q.new_empty(need, dtype=_U8) if need > 0 else None
     _call(lib.ts_cache_attn, dev, ctypes.addressof(pool), q.data_ptr(), out.data_ptr(),
           None if lse is None else lse.data_ptr(), cu_seqlens.data_ptr(), table.data_ptr(), lens.data_ptr(),
           *sizes, _scale(scale, d), num_splits, None if work is None else work.data_ptr(), max(need, 0))
     return (out, lse) if lse is not None else out
-
-
-def _check_lse(lse, T, Hq, dev):
-    if (not isinstance(lse, torch.Tensor) or lse.dtype != torch.float32 or lse.shape != (T, Hq) or lse.device != dev
-            or not lse.is_contiguous()):
-        raise ValueError("lse must be a contiguous float32 [T, Hq] tensor on the cache's device")
 
 
 def ts_cache_weigh(q, lse, cache, cu_seqlens, max_seqlen, table, lens, max_len, scale=None, out=None):
@@ -200,19 +223,18 @@ def ts_cache_weigh(q, lse, cache, cu_seqlens, max_seqlen, table, lens, max_len, 
     each query row and head, exp(scale <q, k> - lse), with lse as ts_cache_attn returned it for these queries.
     In place, or into `out` (float32 [pages, H, 64], of which only the sessions' tokens are written); returns
     what it wrote to."""
-    pool, dev = _pool(cache, need_weight=True)
-    nseq, width = _sessions(table, lens, dev)
-    _rows("q", q, pool.H, pool.d, dev, groups=True)
-    _cu(cu_seqlens, nseq, dev)
+    pool, dev, index = _pool(cache, need_weight=True)
+    nseq, width = _sessions(cu_seqlens, table, lens, index)
+    _rows("q", q, pool.H, pool.d, index, groups=True)
     T, Hq, d = q.shape
-    _check_lse(lse, T, Hq, dev)
+    _check_lse(lse, T, Hq, index)
     if out is None:
         out = cache[4]
     else:
-        _check_weight("out", out, cache[0].shape, dev)
+        _check_weight("out", out, cache[0].shape, index)
     _call(load_cache().ts_cache_weigh, dev, ctypes.addressof(pool), q.data_ptr(), lse.data_ptr(), cu_seqlens.data_ptr(),
           table.data_ptr(), lens.data_ptr(), out.data_ptr(),
-          *_lib.i32s(nseq=nseq, width=width, max_seqlen=max_seqlen, max_len=max_len, T=T, Hq=Hq), _scale(scale, d))
+          *_i32s("nseq, width, max_seqlen, max_len, T, Hq", nseq, width, max_seqlen, max_len, T, Hq), _scale(scale, d))
     return out
 
 
@@ -221,25 +243,21 @@ def ts_cache_evict(cache, table, lens, max_len, new_table, keep, first=0, last=0
     64 * width' >= keep): the first `first`, the last `last`, and of the others those with the largest
     weight (the earlier one of equals), in order.  Sessions of up to `keep` tokens keep them all.  Returns
     (new lengths int32 [nseq], kept positions int32 [nseq, H, keep], -1 past a session's new length)."""
-    pool, dev = _pool(cache, need_weight=True)
-    nseq, width = _sessions(table, lens, dev)
-    _check_ints("new_table", new_table, 2, dev)
-    keep = _lib.i32("keep", keep)
-    if new_table.shape[0] != nseq:
+    pool, dev, index = _pool(cache, need_weight=True)
+    nseq, width = _sessions(None, table, lens, index)
+    _check_ints("new_table", new_table, 2, index)
+    rows, new_width = new_table.shape
+    if rows != nseq:
         raise ValueError("new_table must have one row per session")
-    if out is None:
-        out = torch.empty_like(lens)
-    else:
-        _check_ints("out", out, 1, dev)
-        if out.shape != lens.shape:
-            raise ValueError("out must match lens")
+    sizes = _i32s("nseq, width, new_width, max_len, keep, first, last", nseq, width, new_width, max_len, keep, first, last)
+    keep = sizes[4]
+    out = _lens_out(out, lens, index)
     if kept is None:
-        kept = torch.empty((nseq, pool.H, max(keep, 0)), dtype=torch.int32, device=dev)
+        kept = lens.new_empty((nseq, pool.H, max(keep, 0)))
     else:
-        _check_ints("kept", kept, 3, dev)
+        _check_ints("kept", kept, 3, index)
         if kept.shape != (nseq, pool.H, keep):
             raise ValueError("kept must be [nseq, H, keep]")
     _call(load_cache().ts_cache_evict, dev, ctypes.addressof(pool), table.data_ptr(), lens.data_ptr(), new_table.data_ptr(),
-          out.data_ptr(), kept.data_ptr(),
-          *_lib.i32s(nseq=nseq, width=width, new_width=new_table.shape[1], max_len=max_len, keep=keep, first=first, last=last))
+          out.data_ptr(), kept.data_ptr(), *sizes)
     return out, kept

@@ -30,19 +30,19 @@ cache_rows_kernel(RowArgs a) {
   const int tile = b % a.tiles;
   b /= a.tiles;
   const int h = b % a.pool.H, s = b / a.pool.H;
+  const int32_t* const table = a.ss.table + (int64_t)s * a.ss.width;
+  const int id = first_ids<kRowWaves>(table, a.ss.width, split, a.n_split);
   const Session se = session_of(a.ss, s);
   const int rows = se.rows * a.G, row0 = tile * 16 * NB;
   if (!se.ok || row0 >= rows) return;
-  const int pages = (se.len + kPage - 1) / kPage;
-  const int per = (pages + a.n_split - 1) / a.n_split;
-  const int begin = __builtin_amdgcn_readfirstlane(min(pages, split * per));
-  const int end = __builtin_amdgcn_readfirstlane(min(pages, begin + per));
-  rows_item<D, NB, kRowWaves, kPartial>(a, se, a.ss.table + (int64_t)s * a.ss.width, h, row0, rows, begin, end, split,
-                                        smem);
+  const PageRange range{split, a.n_split, (se.len + kPage - 1) / kPage};
+  rows_item<D, NB, kRowWaves, kPartial>(a, se, table, h, row0, rows, range, id, split, smem);
 }
 
 // Joins the page ranges of a split call: O = sum_i exp(lse_i - lse) O_i with lse = ln sum_i exp(lse_i).  One
 // thread per 8 channels of a row, per_session workgroups to a session.
+constexpr int kMergeBatch = 8;  // ranges whose results are loaded at once
+
 template <int D>
 __global__ void __launch_bounds__(kMergeThreads) cache_merge_kernel(RowArgs a, int per_session) {
   constexpr int kChunks = D / 8;
@@ -52,18 +52,32 @@ __global__ void __launch_bounds__(kMergeThreads) cache_merge_kernel(RowArgs a, i
   if (!se.ok || i / kChunks >= (int64_t)se.rows * Hq) return;
   const int64_t row = (int64_t)se.q0 * Hq + i / kChunks, all = (int64_t)a.ss.total * Hq;
   const int ch = (int)(i % kChunks) * 8;
-  float big = -INFINITY;
-  for (int n = 0; n < a.n_split; ++n) big = fmaxf(big, a.part_lse[n * all + row]);
+  float big = -INFINITY, sum = 0.0f;
   f32x4 x = {}, y = {};
-  float sum = 0.0f;
-  for (int n = 0; n < a.n_split; ++n) {
-    const float e = a.part_lse[n * all + row];
-    if (e == -INFINITY) continue;  // a range without keys has no O
-    const float w = e == big ? 1.0f : __builtin_amdgcn_exp2f((e - big) * kLog2e);
-    const f32x4* const src = (const f32x4*)(a.part_o + (n * all + row) * D + ch);
-    sum += w;
-    x += w * src[0];
-    y += w * src[1];
+  for (int n0 = 0; n0 < a.n_split; n0 += kMergeBatch) {
+    float e[kMergeBatch];
+    f32x4 px[kMergeBatch], py[kMergeBatch];
+#pragma unroll
+    for (int k = 0; k < kMergeBatch; ++k) {  // (past the last range: that one's again, with no weight)
+      const int64_t at = min(n0 + k, a.n_split - 1) * all + row;
+      const float part = a.part_lse[at];
+      e[k] = n0 + k < a.n_split ? part : -INFINITY;
+      const f32x4* const src = (const f32x4*)(a.part_o + at * D + ch);
+      px[k] = src[0], py[k] = src[1];
+    }
+    float top = big;
+#pragma unroll
+    for (int k = 0; k < kMergeBatch; ++k) top = fmaxf(top, e[k]);
+    const float old = big == top ? 1.0f : __builtin_amdgcn_exp2f((big - top) * kLog2e);
+    big = top, sum *= old, x *= old, y *= old;
+#pragma unroll
+    for (int k = 0; k < kMergeBatch; ++k) {
+      const bool none = e[k] == -INFINITY;  // a range without keys has no O
+      const float w = none ? 0.0f : e[k] == big ? 1.0f : __builtin_amdgcn_exp2f((e[k] - big) * kLog2e);
+      sum += w;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) x[c] += none ? 0.0f : w * px[k][c], y[c] += none ? 0.0f : w * py[k][c];
+    }
   }
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   bf16x8 r;

@@ -51,11 +51,25 @@ __device__ __forceinline__ constexpr int v_chunk(int row, int chunk) {
   return D == 128 ? chunk ^ (row >> 1 & 7) : chunk ^ (row >> 2 & 3);
 }
 
-// Rows [row0, row0 + 16 NB) of `rows` (see row_of) over the pages [begin, end) of a session; kW waves, RowGeo::kLds
+// A range of a session's pages: first, first + step, ... < end.  Wave w of kW takes the pages number w, w + kW, ...
+struct PageRange {
+  int first, step, end;
+  __device__ __forceinline__ int page(int i) const { return first + step * i; }
+};
+
+// The first table entries of a wave's pages, one a lane.  Asked for before the session's length is known, they arrive
+// with it: entries past the last page are read (inside the table) and not used.
+template <int kW>
+__device__ __forceinline__ int first_ids(const int32_t* table, int width, int first, int step) {
+  const int p = first + step * ((int)(threadIdx.x >> 6) + kW * (int)(threadIdx.x & 63));
+  return p < width ? table[p] : 0;
+}
+
+// Rows [row0, row0 + 16 NB) of `rows` (see row_of) over a range of pages, `id` its first_ids; kW waves, RowGeo::kLds
 // bytes of LDS.
 template <int D, int NB, int kW, bool kPartial>
 __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, const int32_t* table, int h, int row0,
-                                          int rows, int begin, int end, int split, char* smem) {
+                                          int rows, const PageRange& range, int id, int split, char* smem) {
   using R = RowGeo<D, NB, kW>;
   constexpr int kKK = R::kKK, kCB = R::kCB, kVLoads = R::kVLoads, kKLoads = R::kKLoads, kPageBytes = R::kPageBytes;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -65,12 +79,11 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
   lds_char* const lds = (lds_char*)smem;
   lds_char* const vbuf = lds + wave * 2 * kPageBytes;
 
-  // ---- the wave's pages: begin + wave, + kW, ...; lane i has the number and exponents of the i-th of 64 of them
-  const int mine = end - begin > wave ? (end - begin - wave + kW - 1) / kW : 0;
-  int id = 0, kexp = 0, vexp = 0;
-  auto renew = [&](int i0) {
-    const int i = i0 + lane;
-    id = i < mine ? table[begin + wave + kW * i] : 0;
+  // ---- the wave's pages; lane i has the number and exponents of the i-th of 64 of them
+  const int left = range.end - range.page(wave), apart = kW * range.step;
+  const int mine = left > 0 ? (left + apart - 1) / apart : 0;
+  int kexp = 0, vexp = 0;
+  auto exponents = [&] {
     const bool bad = (unsigned)id >= (unsigned)a.pool.pages;
     id = bad ? 0 : id;
     kexp = a.pool.k_exp[(int64_t)id * H + h];
@@ -82,10 +95,8 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
   const int koff = i16 * D + D / 4 * g;
   auto load = [&](int i) {  // page i of the wave
     const int64_t at = ((int64_t)__builtin_amdgcn_readlane(id, i & 63) * H + h) * kPageBytes;
-    ks = __uint_as_float((unsigned)__builtin_amdgcn_readlane(kexp, i & 63) << 23);
-    vs = __uint_as_float((unsigned)__builtin_amdgcn_readlane(vexp, i & 63) << 23);
     // rows past the session's end as zeros: scores that are masked, values that meet weights of zero
-    const int n = __builtin_amdgcn_readfirstlane(max(0, min(kPage, se.len - (begin + wave + kW * i) * kPage)));
+    const int n = __builtin_amdgcn_readfirstlane(max(0, min(kPage, se.len - range.page(wave + kW * i) * kPage)));
     __amdgpu_buffer_rsrc_t rk = make_rsrc(a.pool.k + at, (uint32_t)(n * D));
     __amdgpu_buffer_rsrc_t rv = make_rsrc(a.pool.v + at, (uint32_t)(n * D));
 #pragma unroll
@@ -100,8 +111,11 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
       dma16(rv, to + 1024 * x, row * D + v_chunk<D>(row, lane % (D / 16)) * 16);
     }
     __asm__ volatile("" ::: "memory");
+    // (after the loads: the first page's need not wait for its exponents)
+    ks = __uint_as_float((unsigned)__builtin_amdgcn_readlane(kexp, i & 63) << 23);
+    vs = __uint_as_float((unsigned)__builtin_amdgcn_readlane(vexp, i & 63) << 23);
   };
-  if (mine > 0) renew(0);
+  if (mine > 0) exponents();
 
   bf16x8 qf[NB][kKK];
 #pragma unroll
@@ -119,7 +133,7 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
 
   if (mine > 0) load(0);
   for (int i = 0; i < mine; ++i) {
-    const int valid = se.len - (begin + wave + kW * i) * kPage;  // keys of this page (64 or more: all)
+    const int valid = se.len - range.page(wave + kW * i) * kPage;  // keys of this page (64 or more: all)
     const float v_scale = vs;
     f32x4 sc[NB][4] = {};
 #pragma unroll
@@ -132,7 +146,10 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
       }
     const bool more = i + 1 < mine;
     if (more) {
-      if (((i + 1) & 63) == 0) renew(i + 1);
+      if (((i + 1) & 63) == 0) {
+        id = i + 1 + lane < mine ? table[range.page(wave + kW * (i + 1 + lane))] : 0;
+        exponents();
+      }
       load(i + 1);
     }
     bf16x8 pf[NB][2];

@@ -517,8 +517,10 @@ cache_tiles_kernel(RowArgs a) {
     const int begin = it.tile_begin * TileGeo<D>::kPages;
     const int end = min((it.se.len + kPage - 1) / kPage, begin + it.ntiles * TileGeo<D>::kPages);
     const int last = min(it.rows, it.row0 + kBM);
+    const int id = first_ids<kWaves>(it.table, a.ss.width, begin, 1);
     for (int row0 = it.row0; row0 < last; row0 += kThinRows)
-      rows_item<D, kThinRows / 16, kWaves, kPartial>(a, it.se, it.table, it.h, row0, it.rows, begin, end, it.split, smem);
+      rows_item<D, kThinRows / 16, kWaves, kPartial>(a, it.se, it.table, it.h, row0, it.rows, {begin, 1, end}, id, it.split,
+                                                     smem);
     return;
   }
   const bool active = it.row0 + 32 * wave < it.rows;
