@@ -118,6 +118,9 @@ hipError_t launch_attn(const AttnArgs& a, hipStream_t st) {
   return a.d == 64 ? launch_attn_d<64>(a, st) : launch_attn_d<128>(a, st);
 }
 
-hipError_t configure_kernels() { return configure_tiles(); }
+hipError_t configure_kernels() {
+  const hipError_t e = configure_tiles();
+  return e != hipSuccess ? e : configure_pages();
+}
 
 }  // namespace tscache

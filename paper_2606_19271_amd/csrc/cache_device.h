@@ -109,6 +109,7 @@ struct RowArgs {
 
 // cache_tiles.hip
 hipError_t configure_tiles();
+hipError_t configure_pages();
 void launch_tiles(const RowArgs& r, int d, int64_t items, hipStream_t st);
 
 }  // namespace tscache

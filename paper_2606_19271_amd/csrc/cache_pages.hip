@@ -118,11 +118,17 @@ cache_append_kernel(Pool pool, Sessions ss, const __bf16* __restrict__ k, const 
 // ---- evict, first kernel: which tokens stay.  One workgroup per (session, head).
 //
 // The tokens of the middle (neither the first nor the last protected ones) are ranked by their weight as an
-// ordered integer.  Three passes over 11, 11 and 10 bits find the m-th largest, threshold, each narrowing the
-// prefix by a histogram in LDS; then a pass counts what every wave keeps and one writes the positions.
+// ordered integer, read once into LDS (as many as fit: kCachedMax; further ones are read again in every pass).  Four
+// passes over 8 bits find the m-th largest, threshold, each narrowing the prefix by a histogram in LDS; then a pass
+// counts what every wave keeps and one writes the positions.  A histogram has 16 copies, one to a bank or two: weights
+// share their exponents, and lanes that count in one bin of one copy do so one after the other.  200 workgroups of 32760
+// tokens take 42 us (85 us with one histogram of 2048 bins and the weights read again in each of five passes).
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectWaves = kSelectThreads / 64;
-constexpr int kBins = 2048;
+constexpr int kBins = 256, kCopies = 16;
+constexpr int kHistBytes = kBins * kCopies * 4;
+constexpr int kCachedMax = 575 * kPage;  // with the histogram and the scans' words within the 160 KiB of a CU
+constexpr int kAhead = 8;                // pages of weights that a wave has in flight
 
 // Monotone in the weight: -infinity (and NaN) lowest, -0 equal to 0.
 __device__ __forceinline__ unsigned rank_bits(float w) {
@@ -134,12 +140,14 @@ __device__ __forceinline__ unsigned rank_bits(float w) {
 
 __global__ void __launch_bounds__(kSelectThreads)
 cache_select_kernel(Pool pool, Sessions ss, int32_t* __restrict__ new_lens, int32_t* __restrict__ kept,
-                    int keep, int first, int last) {
-  __shared__ unsigned hist[kBins];
+                    int keep, int first, int last, int cached) {
+  extern __shared__ __attribute__((aligned(16))) unsigned select_lds[];
   __shared__ unsigned wave_a[kSelectWaves], wave_b[kSelectWaves];
   __shared__ unsigned found[2];
+  unsigned* const hist = select_lds;                    // [kBins][kCopies]
+  unsigned* const ranks = select_lds + kBins * kCopies; // of the first `cached` tokens
   const int h = blockIdx.x % pool.H, s = blockIdx.x / pool.H;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Session se = session_of(ss, s);
   int32_t* const out = kept + (int64_t)blockIdx.x * keep;
   if (h == 0 && tid == 0) new_lens[s] = se.ok ? min(se.len, keep) : se.len;
@@ -149,42 +157,61 @@ cache_select_kernel(Pool pool, Sessions ss, int32_t* __restrict__ new_lens, int3
   }
   const int begin = first, end = se.len - last;  // the middle; begin < end since len > keep >= first + last
   const int32_t* const table = ss.table + (int64_t)s * ss.width;
-  auto rank_at = [&](int i) -> unsigned {
-    const int page = table[i / kPage];
+  auto weight_of = [&](int page, int slot) {  // tokens of pages outside the pool rank lowest
     const bool bad = (unsigned)page >= (unsigned)pool.pages;
-    const float w = pool.weight[page_offset(page, bad, pool.H, h, kPage) + i % kPage];
-    return rank_bits(bad ? -INFINITY : w);
+    const float w = pool.weight[page_offset(page, bad, pool.H, h, kPage) + slot];
+    return bad ? -INFINITY : w;
+  };
+  auto rank_at = [&](int i) -> unsigned {
+    return i < cached ? ranks[i] : rank_bits(weight_of(table[i / kPage], i % kPage));
   };
   unsigned want = (unsigned)(keep - first - last);  // tokens of the middle that stay
   unsigned prefix = 0, mask = 0;
-  bool none = want == 0;
-  for (int pass = 0; pass < 3 && !none; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
-    for (int i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
+  const bool none = want == 0;
+  if (!none) {
+    // wave w reads the pages w, w + kSelectWaves, ...; lane i has the number of the i-th of 64 of them
+    const int pages = min((se.len + kPage - 1) / kPage, cached / kPage);
+    for (int p0 = wave; p0 < pages; p0 += kSelectWaves * 64) {
+      const int mine = min(64, (pages - p0 + kSelectWaves - 1) / kSelectWaves);
+      const int id = lane < mine ? table[p0 + kSelectWaves * lane] : 0;
+      for (int k = 0; k < mine; k += kAhead) {
+        float w[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) w[u] = weight_of(__builtin_amdgcn_readlane(id, min(k + u, mine - 1)), lane);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+          if (k + u < mine) ranks[(p0 + kSelectWaves * (k + u)) * kPage + lane] = rank_bits(w[u]);
+      }
+    }
+  }
+  for (int shift = 24; shift >= 0 && !none; shift -= 8) {
+    *(u32x4*)(hist + 4 * tid) = u32x4{};
     __syncthreads();
     for (int i = begin + tid; i < end; i += kSelectThreads) {
       const unsigned u = rank_at(i);
-      if ((u & mask) == prefix) atomicAdd(&hist[u >> shift & (bins - 1)], 1u);
+      if ((u & mask) == prefix) atomicAdd(&hist[(u >> shift & (kBins - 1)) * kCopies + (lane & (kCopies - 1))], 1u);
     }
     __syncthreads();
-    // the bin that holds the want-th largest: suffix sums of two bins a thread, from the top
-    const int b1 = bins - 1 - 2 * tid, b0 = b1 - 1;
-    const unsigned c1 = b1 >= 0 ? hist[b1] : 0, c0 = b0 >= 0 ? hist[b0] : 0;
-    unsigned sum = c1 + c0;
+    // the bin that holds the want-th largest: suffix sums, four lanes to a bin, from the top
+    const int bin = kBins - 1 - tid / 4;
+    const u32x4 part = *(const u32x4*)(hist + bin * kCopies + tid % 4 * 4);
+    unsigned here = (part[0] + part[1]) + (part[2] + part[3]);
+    here += (unsigned)__shfl_xor((int)here, 1);
+    here += (unsigned)__shfl_xor((int)here, 2);
+    unsigned sum = here;
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
+    for (int m = 4; m < 64; m <<= 1) {
       const unsigned y = (unsigned)__shfl_up((int)sum, m);
       if (lane >= m) sum += y;
     }
     if (lane == 63) wave_a[wave] = sum;
     __syncthreads();
-    unsigned before = sum - (c1 + c0);
+    unsigned before = sum - here;
     for (int w = 0; w < wave; ++w) before += wave_a[w];
-    if (before < want && before + c1 >= want) found[0] = (unsigned)b1, found[1] = before;
-    if (before + c1 < want && before + c1 + c0 >= want) found[0] = (unsigned)b0, found[1] = before + c1;
+    if (before < want && before + here >= want && tid % 4 == 0) found[0] = (unsigned)bin, found[1] = before;
     __syncthreads();
     prefix |= found[0] << shift;
-    mask |= (unsigned)(bins - 1) << shift;
+    mask |= (unsigned)(kBins - 1) << shift;
     want -= found[1];
   }
   // kept of the middle: every rank above prefix, and of those equal to it the first `want`
@@ -305,9 +332,15 @@ hipError_t launch_append(const AppendArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+hipError_t configure_pages() {
+  return hipFuncSetAttribute((const void*)cache_select_kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
+                             kHistBytes + kCachedMax * 4);
+}
+
 hipError_t launch_evict(const EvictArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(cache_select_kernel, dim3((unsigned)(a.ss.nseq * a.pool.H)), dim3(kSelectThreads), 0,
-                     st, a.pool, a.ss, a.new_lens, a.kept, a.keep, a.first, a.last);
+  const int cached = min((a.ss.max_len + kPage - 1) / kPage * kPage, kCachedMax);
+  hipLaunchKernelGGL(cache_select_kernel, dim3((unsigned)(a.ss.nseq * a.pool.H)), dim3(kSelectThreads),
+                     kHistBytes + cached * 4, st, a.pool, a.ss, a.new_lens, a.kept, a.keep, a.first, a.last, cached);
   const hipError_t e = hipGetLastError();
   const int64_t items = gather_items(a.ss.nseq, a.keep, a.pool.H);
   if (e != hipSuccess || items == 0) return e;
