@@ -86,11 +86,12 @@ int ts_cache_append(const ts_cache* cache, const void* k, const void* v, const i
  *   lse[t,hq] = ln sum_j exp(scale * <q[t,hq,:], k[j,hq/G,:]>)
  * q, o bfloat16 [total][Hq][d] (16-byte aligned); lse float32 [total][Hq] or NULL.  A session without
  * tokens gets o = 0 and lse = -infinity.  scale: any finite float.
- *  num_splits  0: chosen by the library; n in 1..TS_CACHE_MAX_SPLITS: the keys of every query tile are
- *              split into n ranges of pages, joined by a second kernel through float32 partial results in
+ *  num_splits  0: the library divides the work, by the sessions' lengths where there are many rows; n in
+ *              1..TS_CACHE_MAX_SPLITS: the keys of every query tile are split into n ranges of pages.  What
+ *              is divided is joined by a second kernel, through float32 partial results in
  *  workspace   (DEVICE, 256-byte aligned, of this call alone until it is done): ts_cache_attn_workspace
- *              bytes.  With num_splits = 0 a smaller one, or NULL, lowers n to what fits; a forced n that does
- *              not fit returns TS_ERR_SCRATCH.
+ *              bytes.  With num_splits = 0 a smaller one, or NULL, divides less or not at all; a forced n
+ *              that does not fit returns TS_ERR_SCRATCH.
  * o, lse and workspace must not overlap each other or any input (TS_ERR_ALIAS).
  */
 #define TS_CACHE_MAX_SPLITS 64

@@ -36,7 +36,7 @@ cache_rows_kernel(RowArgs a) {
   const int rows = se.rows * a.G, row0 = tile * 16 * NB;
   if (!se.ok || row0 >= rows) return;
   const PageRange range{split, a.n_split, (se.len + kPage - 1) / kPage};
-  rows_item<D, NB, kRowWaves, kPartial>(a, se, table, h, row0, rows, range, id, split, smem);
+  rows_item<D, NB, kRowWaves, kPartial ? kSlab : kResult>(a, se, table, h, row0, rows, range, id, split, smem);
 }
 
 // Joins the page ranges of a split call: O = sum_i exp(lse_i - lse) O_i with lse = ln sum_i exp(lse_i).  One
@@ -52,39 +52,7 @@ __global__ void __launch_bounds__(kMergeThreads) cache_merge_kernel(RowArgs a, i
   if (!se.ok || i / kChunks >= (int64_t)se.rows * Hq) return;
   const int64_t row = (int64_t)se.q0 * Hq + i / kChunks, all = (int64_t)a.ss.total * Hq;
   const int ch = (int)(i % kChunks) * 8;
-  float big = -INFINITY, sum = 0.0f;
-  f32x4 x = {}, y = {};
-  for (int n0 = 0; n0 < a.n_split; n0 += kMergeBatch) {
-    float e[kMergeBatch];
-    f32x4 px[kMergeBatch], py[kMergeBatch];
-#pragma unroll
-    for (int k = 0; k < kMergeBatch; ++k) {  // (past the last range: that one's again, with no weight)
-      const int64_t at = min(n0 + k, a.n_split - 1) * all + row;
-      const float part = a.part_lse[at];
-      e[k] = n0 + k < a.n_split ? part : -INFINITY;
-      const f32x4* const src = (const f32x4*)(a.part_o + at * D + ch);
-      px[k] = src[0], py[k] = src[1];
-    }
-    float top = big;
-#pragma unroll
-    for (int k = 0; k < kMergeBatch; ++k) top = fmaxf(top, e[k]);
-    const float old = big == top ? 1.0f : __builtin_amdgcn_exp2f((big - top) * kLog2e);
-    big = top, sum *= old, x *= old, y *= old;
-#pragma unroll
-    for (int k = 0; k < kMergeBatch; ++k) {
-      const bool none = e[k] == -INFINITY;  // a range without keys has no O
-      const float w = none ? 0.0f : e[k] == big ? 1.0f : __builtin_amdgcn_exp2f((e[k] - big) * kLog2e);
-      sum += w;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) x[c] += none ? 0.0f : w * px[k][c], y[c] += none ? 0.0f : w * py[k][c];
-    }
-  }
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  bf16x8 r;
-#pragma unroll
-  for (int c = 0; c < 4; ++c) r[c] = (__bf16)(x[c] * inv), r[4 + c] = (__bf16)(y[c] * inv);
-  *(bf16x8*)(a.o + row * D + ch) = r;
-  if (a.lse != nullptr && ch == 0) a.lse[row] = sum == 0.0f ? -INFINITY : big + log2f(sum) * kLn2;
+  join_parts<D, kMergeBatch>(a, a.n_split, [&](int n) { return n * all + row; }, row, ch);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -100,7 +68,7 @@ template <int D>
 static hipError_t launch_attn_d(const AttnArgs& a, hipStream_t st) {
   const int64_t rows = (int64_t)a.ss.max_rows * a.G;
   const int tile = row_tile(rows, a.scale);
-  RowArgs r{a.pool, a.ss, (const __bf16*)a.q, (__bf16*)a.o, a.lse, a.part_o, a.part_lse, a.G, a.n_split,
+  RowArgs r{a.pool, a.ss, (const __bf16*)a.q, (__bf16*)a.o, a.lse, a.part_o, a.part_lse, a.G, a.n_split, a.shares,
             (int)((rows + tile - 1) / tile), fabsf(a.scale) * kLog2e, a.scale < 0.0f ? 0x80008000u : 0u};
   const int64_t items = attn_items(a.ss.nseq, a.ss.max_rows, a.ss.total, a.pool.H, a.G, tile) * a.n_split;
   if (tile == kTileRows) launch_tiles(r, D, items, st);

@@ -79,6 +79,14 @@ __device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t rsrc, lds_char* to,
   __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)to, 16, offset, 0, 0, 0);
 }
 
+// threadIdx.x, of which nothing is derived ahead of the call: what a loop over items would keep in registers through
+// all of them is formed for each anew.
+__device__ __forceinline__ int thread_anew() {
+  int t = threadIdx.x;
+  __asm__ volatile("" : "+v"(t));
+  return t;
+}
+
 // Bytes from a page's start to its head h, and the page itself; a page number outside the pool reads
 // page 0 (in bounds, and poisoned through its scale).
 __device__ __forceinline__ int64_t page_offset(int page, bool bad, int H, int h, int bytes) {
@@ -102,10 +110,54 @@ struct RowArgs {
   float* part_o;
   float* part_lse;
   int G, n_split;
+  int shares;     // equal shares of the work (cache_tiles_kernel), or 0
   int tiles;      // row tiles of a session at most (cache_rows_kernel)
   float c;        // |scale| log2(e)
   unsigned flip;  // sign bits of Q to invert (negative scales)
 };
+
+// What becomes of an item's rows: they are the result, or one of n_split ranges' part of it (part_o[n_split][total][Hq]),
+// or the part of it that a share of the work has (part_o[slots][256], kTileRows rows each).
+enum Out { kResult, kSlab, kSlot };
+
+// The 8 channels from `ch` on of a row whose n parts lie at rows part(0) .. part(n - 1) of part_o and part_lse:
+// O = sum_i exp(lse_i - lse) O_i with lse = ln sum_i exp(lse_i), kBatch parts loaded at once.
+template <int D, int kBatch, typename Part>
+__device__ __forceinline__ void join_parts(const RowArgs& a, int n, Part&& part, int64_t row, int ch) {
+  float big = -INFINITY, sum = 0.0f;
+  f32x4 x = {}, y = {};
+  for (int n0 = 0; n0 < n; n0 += kBatch) {
+    float e[kBatch];
+    f32x4 px[kBatch], py[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {  // (past the last part: that one's again, with no weight)
+      const int64_t at = part(min(n0 + k, n - 1));
+      const float l = a.part_lse[at];
+      e[k] = n0 + k < n ? l : -INFINITY;
+      const f32x4* const src = (const f32x4*)(a.part_o + at * D + ch);
+      px[k] = src[0], py[k] = src[1];
+    }
+    float top = big;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) top = fmaxf(top, e[k]);
+    const float old = big == top ? 1.0f : __builtin_amdgcn_exp2f((big - top) * kLog2e);
+    big = top, sum *= old, x *= old, y *= old;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const bool none = e[k] == -INFINITY;  // a part without keys has no O
+      const float w = none ? 0.0f : e[k] == big ? 1.0f : __builtin_amdgcn_exp2f((e[k] - big) * kLog2e);
+      sum += w;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) x[c] += none ? 0.0f : w * px[k][c], y[c] += none ? 0.0f : w * py[k][c];
+    }
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  bf16x8 r;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) r[c] = (__bf16)(x[c] * inv), r[4 + c] = (__bf16)(y[c] * inv);
+  *(bf16x8*)(a.o + row * D + ch) = r;
+  if (a.lse != nullptr && ch == 0) a.lse[row] = sum == 0.0f ? -INFINITY : big + log2f(sum) * kLn2;
+}
 
 // cache_tiles.hip
 hipError_t configure_tiles();

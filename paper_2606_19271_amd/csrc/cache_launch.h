@@ -35,11 +35,10 @@ struct AttnArgs {
   const void* q;
   void* o;
   float* lse;       // or null
-  float* part_o;    // [n_split][total][Hq][d] (n_split > 1)
-  float* part_lse;  // [n_split][total][Hq]
-  int32_t d, G, n_split;
+  float* part_o;    // [n_split][total][Hq][d] (n_split > 1), [2 shares][256][d] (shares > 0)
+  float* part_lse;  // the same without d
+  int32_t d, G, n_split, shares;
   float scale;
-  int32_t cus;
 };
 
 struct WeighArgs {
@@ -79,12 +78,19 @@ int row_tile(int64_t rows, float scale);
 // Workgroups of an unsplit attention call, and of its merge kernel.
 int64_t attn_items(int32_t nseq, int32_t max_rows, int32_t total, int32_t H, int32_t G, int tile);
 int64_t merge_blocks(int32_t nseq, int32_t max_rows, int32_t Hq, int32_t d);
-// Page ranges per query tile when the caller leaves the choice to the library.
-int32_t auto_splits(int32_t nseq, int32_t max_rows, int32_t max_len, int32_t total, int32_t H, int32_t G,
-                    int32_t d, int tile, int32_t cus);
-// Bytes of workspace of a call of n page ranges: the partial lse [n][total][Hq], then O [n][total][Hq][d].
-int64_t workspace_bytes(int32_t n, int32_t total, int32_t Hq, int32_t d);
-int64_t part_o_offset(int32_t n, int32_t total, int32_t Hq);
+// How the keys of an attention call are dealt out, and its workspace of partial results.  Calls of few rows are split
+// into n_split ranges of pages, as many as fill the device; 256-row tiles into `shares` equal shares of the work.
+// A workspace that is too small makes them fewer or none.
+struct Parts {
+  int32_t n_split, shares;
+  int64_t o_offset, bytes;  // the partial log-sum-exps lie first, then O
+};
+Parts attn_parts(const Sessions& ss, int32_t H, int32_t G, int32_t d, int tile, int32_t num_splits, int64_t workspace,
+                 int32_t cus);
+// Equal shares (Work in cache_tiles.hip), costs in key tiles: what an item costs beside its tiles, the least share, the
+// least part of an item.  With kEvenItems row tiles a CU and more, whole ones end evenly enough.
+constexpr int kStartCost = 4, kShareMin = 12, kCutMin = 4;
+constexpr int kEvenItems = 2;
 // Workgroups of the other kernels.
 // weigh: a page to a workgroup where there are few, else four pages of a head, in 8 XCDs x nseq sessions x weigh_share
 // workgroups, at most weigh_items.

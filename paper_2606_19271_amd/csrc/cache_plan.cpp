@@ -31,30 +31,33 @@ int64_t merge_blocks(int32_t nseq, int32_t max_rows, int32_t Hq, int32_t d) {
   return per > 0 && nseq > 4 * kGridLimit / per ? 4 * kGridLimit : nseq * per;
 }
 
-int32_t auto_splits(int32_t nseq, int32_t max_rows, int32_t max_len, int32_t total, int32_t H, int32_t G,
-                    int32_t d, int tile, int32_t cus) {
-  const int64_t items = attn_items(nseq, max_rows, total, H, G, tile);
-  if (items <= 0) return 1;
-  if (tile < kTileRows) {
-    const int64_t want = 4 * (int64_t)cus / items;
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, ceil_div(max_len, kPage) / 4, 64}));
-  }
-  const int64_t tiles = ceil_div(max_len, d == 64 ? 2 * kPage : kPage);
-  int32_t best = 1;
-  int64_t best_cost = INT64_MAX;
-  for (int32_t n = 1; n <= 16 && (n == 1 || tiles / n >= 4); ++n) {
-    const int64_t cost = ceil_div(items * n, cus) * (ceil_div(tiles, n) + 4) + (n > 1 ? 6 : 0);
-    if (cost < best_cost) best_cost = cost, best = n;
-  }
-  return best;
+namespace {
+Parts parts(int32_t n_split, int32_t shares, int64_t rows, int32_t d) {
+  const int64_t o_offset = (rows * 4 + 255) / 256 * 256;
+  return {n_split, shares, o_offset, rows > 0 ? o_offset + rows * d * 4 : 0};
 }
-
-int64_t part_o_offset(int32_t n, int32_t total, int32_t Hq) {
-  return ((int64_t)n * total * Hq * 4 + 255) / 256 * 256;
+Parts ranges(int32_t n, int32_t total, int32_t Hq, int32_t d) {
+  return parts(n, 0, n > 1 ? (int64_t)n * total * Hq : 0, d);
 }
+}  // namespace
 
-int64_t workspace_bytes(int32_t n, int32_t total, int32_t Hq, int32_t d) {
-  return n > 1 ? part_o_offset(n, total, Hq) + (int64_t)n * total * Hq * d * 4 : 0;
+Parts attn_parts(const Sessions& ss, int32_t H, int32_t G, int32_t d, int tile, int32_t num_splits, int64_t workspace,
+                 int32_t cus) {
+  int32_t n = std::max(1, num_splits);
+  if (num_splits == 0) {
+    const int64_t items = std::max<int64_t>(1, attn_items(ss.nseq, ss.max_rows, ss.total, H, G, tile));
+    if (tile < kTileRows) {
+      const int64_t want = 4 * (int64_t)cus / items;
+      n = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, ceil_div(ss.max_len, kPage) / 4, 64}));
+      while (n > 1 && ranges(n, ss.total, H * G, d).bytes > workspace) --n;
+    } else if (items < kEvenItems * (int64_t)cus) {
+      const int64_t cost = items * (ceil_div(ss.max_len, d == 64 ? 2 * kPage : kPage) + kStartCost);  // at most
+      const int64_t shares = std::min<int64_t>(cus, ceil_div(cost, kShareMin));
+      const Parts p = parts(1, (int32_t)shares, 2 * shares * kTileRows, d);
+      if (shares > 1 && p.bytes <= workspace) return p;
+    }
+  }
+  return ranges(n, ss.total, H * G, d);
 }
 
 bool weigh_few(int32_t nseq, int32_t max_len, int32_t H, int32_t cus) {

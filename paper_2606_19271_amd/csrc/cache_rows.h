@@ -45,6 +45,13 @@ struct RowGeo {
   static constexpr int kCh = D / (4 * kW) < 4 ? 4 : D / (4 * kW);
 };
 
+// f over the lanes that differ in bits 4 and 5.
+template <typename F>
+__device__ __forceinline__ float across(float x, F&& f) {
+  x = f(x, __shfl_xor(x, 16));
+  return f(x, __shfl_xor(x, 32));
+}
+
 // Position of 16-byte chunk `chunk` of V row `row` in LDS.
 template <int D>
 __device__ __forceinline__ constexpr int v_chunk(int row, int chunk) {
@@ -61,18 +68,18 @@ struct PageRange {
 // with it: entries past the last page are read (inside the table) and not used.
 template <int kW>
 __device__ __forceinline__ int first_ids(const int32_t* table, int width, int first, int step) {
-  const int p = first + step * ((int)(threadIdx.x >> 6) + kW * (int)(threadIdx.x & 63));
+  const int tid = thread_anew(), p = first + step * ((tid >> 6) + kW * (tid & 63));
   return p < width ? table[p] : 0;
 }
 
 // Rows [row0, row0 + 16 NB) of `rows` (see row_of) over a range of pages, `id` its first_ids; kW waves, RowGeo::kLds
-// bytes of LDS.
-template <int D, int NB, int kW, bool kPartial>
+// bytes of LDS.  `to`: of kSlab the range's number; of kSlot the slot, row0 its first row, or -1 for a result.
+template <int D, int NB, int kW, Out kOut>
 __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, const int32_t* table, int h, int row0,
-                                          int rows, const PageRange& range, int id, int split, char* smem) {
+                                          int rows, const PageRange& range, int id, int to, char* smem) {
   using R = RowGeo<D, NB, kW>;
   constexpr int kKK = R::kKK, kCB = R::kCB, kVLoads = R::kVLoads, kKLoads = R::kKLoads, kPageBytes = R::kPageBytes;
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = thread_anew(), lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i16 = lane & 15, g = lane >> 4;
   const int H = a.pool.H, G = a.G;
@@ -161,8 +168,7 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           if (16 * kb + 4 * g + r < valid) mt = fmaxf(mt, sc[n][kb][r]);
-      mt = fmaxf(mt, __shfl_xor(mt, 16));
-      mt = fmaxf(mt, __shfl_xor(mt, 32));
+      mt = across(mt, [](float x, float y) { return fmaxf(x, y); });
       // scores that are all NaN leave the maximum as it is; their weights are NaN
       const float m_new = fmaxf(m[n], mt * a.c);
       const float alpha = m[n] == m_new ? 1.0f : __builtin_amdgcn_exp2f(m[n] - m_new);
@@ -214,9 +220,7 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
   const int orow = tid / (D / kCh), och = tid % (D / kCh) * kCh;
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
-    float ln = l[n];
-    ln += __shfl_xor(ln, 16);
-    ln += __shfl_xor(ln, 32);
+    const float ln = across(l[n], [](float x, float y) { return x + y; });
     __syncthreads();
 #pragma unroll
     for (int cb = 0; cb < kCB; ++cb) *(lds_f32x4*)(obuf + (wave * 16 + i16) * D + 16 * cb + 4 * g) = o[n][cb];
@@ -238,10 +242,10 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
       for (int x = 0; x < kCh / 4; ++x) acc[x] += f * *(const lds_f32x4*)(obuf + (w * 16 + orow) * D + och + 4 * x);
     }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    const float lse = sum == 0.0f ? -INFINITY : (big + log2f(sum)) * kLn2;
+    const float lse = sum == 0.0f ? -INFINITY : (big + __builtin_amdgcn_logf(sum)) * kLn2;
     const int64_t at = row_of(se, r, h, H, G);
-    if constexpr (kPartial) {
-      const int64_t part = (int64_t)split * a.ss.total * (H * G) + at;
+    if (kOut == kSlab || (kOut == kSlot && to >= 0)) {
+      const int64_t part = kOut == kSlot ? (int64_t)to * kTileRows + (r - row0) : (int64_t)to * a.ss.total * (H * G) + at;
       if (sum != 0.0f)
 #pragma unroll
         for (int x = 0; x < kCh / 4; ++x) *(f32x4*)(a.part_o + part * D + och + 4 * x) = acc[x] * inv;

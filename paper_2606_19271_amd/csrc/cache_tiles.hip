@@ -52,7 +52,7 @@ struct TileGeo {
   static constexpr int kLds = kList + 2 * kEntries * 8;
   static_assert(G::kVTile == 16384 && kVRing == 0 && kVStages == 2, "a V stage is one bit of an LDS address");
   static_assert(kLoads == 2, "two loads per lane: one page each at d = 64, both of one at d = 128");
-  static_assert(kLds <= 160 * 1024, "LDS of a CU");
+  static_assert(kLds + 32 <= 160 * 1024, "LDS of a CU");
 };
 
 // One item: query rows [row0, row0 + 256) of (session, head h) against key tiles [tile_begin, + ntiles).
@@ -60,6 +60,7 @@ struct TileItem {
   Session se;
   const int32_t* table;  // the session's pages
   int h, row0, rows, tile_begin, ntiles, split;
+  int slot;  // where a piece of the item goes that kEven's shares have cut, or -1
 };
 
 // A page of the session's as a group fetches it: its number, and its exponent as the bits of a float.  Pages past the
@@ -153,7 +154,7 @@ __device__ __forceinline__ void tile_softmax(f32x16 (&s)[Geo<D>::kBN / 32], bf16
 
 // O = O / l of a wave's 32 rows, through LDS so that whole lines are stored (as write_result of
 // attn_kernels.hip), and the rows' log-sum-exp.
-template <int D, bool kPartial>
+template <int D, Out kOut>
 __device__ __forceinline__ void write_rows(const TileItem& it, const RowArgs& a, const f32x16 (&oacc)[D / 32],
                                            float l, float m_c, int q0, lds_char* stage, int lane) {
   using G = Geo<D>;
@@ -163,12 +164,16 @@ __device__ __forceinline__ void write_rows(const TileItem& it, const RowArgs& a,
   lds_char* const put = stage + col * G::kORow;
   const lds_char* const get = stage + orow * G::kORow + ochunk * 16;
   auto in_order = [] { __asm__ volatile("" ::: "memory"); };
-  const int64_t slab = kPartial ? (int64_t)it.split * a.ss.total * (H * a.G) : 0;
+  constexpr bool kPartial = kOut != kResult;
+  const int64_t slab = kOut == kSlab ? (int64_t)it.split * a.ss.total * (H * a.G) : 0;
+  auto place = [&](int r) {
+    return kOut == kSlot ? (int64_t)it.slot * kBM + (r - it.row0) : slab + row_of(it.se, r, it.h, H, a.G);
+  };
   int64_t at[4];  // rows that this lane stores
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const int r = q0 + orow + 8 * u;
-    at[u] = r < it.rows ? slab + row_of(it.se, r, it.h, H, a.G) : -1;
+    at[u] = r < it.rows ? place(r) : -1;
   }
   constexpr int kBlocks = kPartial ? 1 : 2;  // 32-channel blocks of a pass: 128 bytes of each row
 #pragma unroll
@@ -196,16 +201,20 @@ __device__ __forceinline__ void write_rows(const TileItem& it, const RowArgs& a,
   }
   float* const lse = kPartial ? a.part_lse : a.lse;
   if (lse != nullptr && hb == 0 && q0 + col < it.rows)
-    lse[slab + row_of(it.se, q0 + col, it.h, H, a.G)] = l == 0.0f ? -INFINITY : (m_c + log2f(l)) * kLn2;
+    lse[place(q0 + col)] = l == 0.0f ? -INFINITY : (m_c + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // kActive = false: a wave whose rows all lie past the session's: it fetches its share and keeps the barriers.
-template <int D, bool kGroupB, bool kPartial, bool kActive>
+// How the work is dealt to workgroups: an item each (find_item), whole or in n_split ranges of keys; or equal shares of it
+// (Work below).
+enum Mode { kWhole, kSplit, kEven };
+
+template <int D, bool kGroupB, Mode kMode, bool kActive>
 __device__ __forceinline__ void run_tile_group(const TileItem& it, const RowArgs& a, char* smem) {
   using G = Geo<D>;
   using T = TileGeo<D>;
   constexpr int kBN = G::kBN, kPre = T::kPre;
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = thread_anew(), lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gw = wave & (G::kGroupWaves - 1);
   const int H = a.pool.H;
@@ -402,7 +411,11 @@ __device__ __forceinline__ void run_tile_group(const TileItem& it, const RowArgs
   if constexpr (kActive) {
     auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    write_rows<D, kPartial>(it, a, oacc, l, m_c, it.row0 + 32 * wave, lds + T::kOBase + wave * G::kOWave, lane);
+    const int q0 = it.row0 + 32 * wave;
+    lds_char* const stage = lds + T::kOBase + wave * G::kOWave;
+    if constexpr (kMode != kEven) write_rows<D, kMode == kSplit ? kSlab : kResult>(it, a, oacc, l, m_c, q0, stage, lane);
+    else if (it.slot < 0) write_rows<D, kResult>(it, a, oacc, l, m_c, q0, stage, lane);
+    else write_rows<D, kSlot>(it, a, oacc, l, m_c, q0, stage, lane);
   }
 }
 
@@ -413,7 +426,7 @@ __device__ __forceinline__ void run_tile_group(const TileItem& it, const RowArgs
 // keys passes through its L2, and the XCDs have equal work; within an XCD the longest sessions come first, so
 // that it ends evenly.  Up to 64 sessions are put in order by every wave itself, one per lane; more keep their order.
 // (Spans of 8 x 32 items dealt over the XCDs instead leave the first ones all the long items: six sessions of 2730 to
-// 32760 keys x 1560 queries x 12 heads took 1170 us instead of 1044.)
+// 32760 keys x 1560 queries x 12 heads took 1.12 times as long.)
 struct Share {  // of a session's `count` items, `before` items of earlier sessions: this XCD's
   int n, first;
   __device__ __forceinline__ Share(int count, int before, int xcd) {
@@ -495,8 +508,8 @@ __device__ __forceinline__ bool find_item(const RowArgs& a, TileItem* it) {
 }
 
 // A last tile of at most this many rows is shared by the eight waves, each taking pages of its own (rows_item): in
-// the schedule above one wave would work and seven keep its barriers, for as long as a full tile takes (those six
-// sessions, whose last tiles have 24 rows: 1098 us instead of 1044).
+// the schedule above one wave would work and seven keep its barriers, for three quarters of a full tile's time (32768
+// keys, d = 128: 206 us for 24 rows this way, 568 for 100, 713 for 256).
 constexpr int kThinRows = 32;
 
 template <int D>
@@ -505,13 +518,133 @@ constexpr int tiles_lds() {
                                                                    : RowGeo<D, kThinRows / 16, kWaves>::kLds;
 }
 
-template <int D, bool kPartial>
-__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
-cache_tiles_kernel(RowArgs a) {
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  TileItem it;
-  if (!find_item<D>(a, &it)) return;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+constexpr int kStateBytes = 32;  // where a share stands (kEven)
+
+// Equal shares.  Items as they come, the sessions' in their order and of each head-major, cost kStartCost and their tiles,
+// less where the last rows leave waves idle; share i of P has [i S, (i + 1) S) of their sum, S = sum / P but at least
+// kShareMin: whole items, and the parts of those that a border cuts.  A cut is at a tile, and none within kCutMin tiles
+// of an item's ends (it moves there).  What a share has of a cut item goes to
+// one of its two slots: 2 i, if the item began in an earlier share, else 2 i + 1; cache_join_kernel joins them.
+// Consecutive eighths of the shares go to the XCDs.  Against whole row tiles, or as many ranges of each as fill the device
+// when all sessions have the stated length: 257 .. 640 odd rows x 777 .. 20011 keys x 12 heads x 2, d = 64, 152 -> 119 us; six
+// sessions of 2730 to 32760 keys 961 -> 923; one of 32760 keys x 1560 rows x 12 heads, which three ranges fill exactly,
+// 294 -> 302 (the workgroups of an XCD then read the same keys at one time, and shares do not).
+struct Spot {
+  int s, h, tile, t;  // session, head, row tile, key tile of it (0 unless the spot is inside an item)
+  int64_t from;       // where its item begins
+  __device__ __forceinline__ bool before(const Spot& o) const {
+    if (s != o.s) return s < o.s;
+    if (h != o.h) return h < o.h;
+    return tile != o.tile ? tile < o.tile : t < o.t;
+  }
+};
+
+__device__ __forceinline__ void next_item(Spot& p, int nq, int H) {
+  p.t = 0;
+  if (++p.tile < nq) return;
+  p.tile = 0;
+  if (++p.h < H) return;
+  p.h = 0, ++p.s;
+}
+
+// The share of a workgroup: consecutive eighths to the XCDs (workgroup b runs on XCD b % 8).
+__device__ __forceinline__ int share_of_block() {
+  return (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+}
+
+// The kernel's arguments, read from memory at this point.
+__device__ __forceinline__ RowArgs args_anew() {
+  typedef __attribute__((address_space(4))) const uint64_t const_word;
+  struct Words {
+    uint64_t w[sizeof(RowArgs) / 8];
+  } x;
+  uintptr_t p = (uintptr_t)__builtin_amdgcn_kernarg_segment_ptr();
+  __asm__ volatile("" : "+s"(p));
+#pragma unroll
+  for (unsigned i = 0; i < sizeof(x) / 8; ++i) x.w[i] = ((const_word*)p)[i];
+  return __builtin_bit_cast(RowArgs, x);
+}
+
+template <int D>
+struct Work {
+  const RowArgs& a;
+  int64_t sum, share;
+
+  struct Shape {  // of a session: key tiles, row tiles, costs of a row tile, of the last one, and of a head
+    int tiles, nq;
+    int part;  // 20ths of a full tile's time that the last one takes: 24, 100 and 256 rows measured
+    int cost, last;
+    int64_t head;
+    __device__ __forceinline__ Shape(const Session& se, int G) {
+      const int rows = se.rows * G;
+      tiles = (se.len + Geo<D>::kBN - 1) / Geo<D>::kBN;
+      nq = (rows + kBM - 1) / kBM;
+      cost = tiles + kStartCost;
+      const int active = (rows - (nq - 1) * kBM + 31) / 32;  // waves
+      part = active == 1 ? 9 : 12 + active;
+      last = (int)((int64_t)tiles * part / 20) + kStartCost;
+      head = (int64_t)(nq - 1) * cost + last;
+    }
+    // the tile at which a border `in` past the item's start cuts it: 0 and `tiles` are its ends
+    __device__ __forceinline__ int cut(int tile, int in) const {
+      const int t = tile == nq - 1 ? (int)((int64_t)(in - kStartCost) * 20 / part) : in - kStartCost;
+      return t < kCutMin ? 0 : tiles - t < kCutMin ? tiles : t;
+    }
+  };
+  __device__ __forceinline__ int64_t cost_of(int s) const {
+    if (s >= a.ss.nseq) return 0;
+    const Session se = session_of(a.ss, s);
+    return se.rows > 0 ? Shape(se, a.G).head * a.pool.H : 0;
+  }
+  static __device__ __forceinline__ int64_t scan(int64_t x, int lane) {  // inclusive, over the lanes
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const int64_t y = __shfl_up(x, m);
+      if (lane >= m) x += y;
+    }
+    return x;
+  }
+  __device__ __forceinline__ Work(const RowArgs& args) : a(args) {
+    const int lane = threadIdx.x & 63;
+    int64_t x = 0;
+    for (int s = lane; s < a.ss.nseq; s += 64) x += cost_of(s);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
+    sum = x;
+    const int64_t each = (sum + a.shares - 1) / a.shares;
+    share = each > kShareMin ? each : kShareMin;
+  }
+  __device__ __forceinline__ Spot at(int64_t x) const {
+    const int lane = threadIdx.x & 63;
+    Spot p{a.ss.nseq, 0, 0, 0, sum};
+    int64_t base = 0;
+    if (x >= sum) return p;
+    for (int s0 = 0; s0 < a.ss.nseq; s0 += 64) {
+      const int64_t cost = cost_of(s0 + lane), to = base + scan(cost, lane);
+      const unsigned long long hit = __builtin_amdgcn_ballot_w64(x < to);
+      if (hit != 0) {
+        const int i = __builtin_ctzll(hit);  // the first that ends past x
+        p.s = s0 + i, p.from = __shfl(to - cost, i);
+        break;
+      }
+      base = __shfl(to, 63);
+    }
+    const Shape sh(session_of(a.ss, p.s), a.G);
+    p.h = (int)((x - p.from) / sh.head);
+    p.from += p.h * sh.head;
+    const int64_t tile = (x - p.from) / sh.cost;
+    p.tile = tile < sh.nq ? (int)tile : sh.nq - 1;
+    p.from += (int64_t)p.tile * sh.cost;
+    p.t = sh.cut(p.tile, (int)(x - p.from));
+    if (p.t > 0 && p.t == sh.tiles) next_item(p, sh.nq, a.pool.H);
+    return p;
+  }
+};
+
+template <int D, Mode kMode>
+__device__ __forceinline__ void run_item(const TileItem& it, const RowArgs& a, char* smem) {
+  constexpr Out kOut = kMode == kEven ? kSlot : kMode == kSplit ? kSlab : kResult;
+  const int wave = __builtin_amdgcn_readfirstlane(thread_anew() >> 6);
   if (it.ntiles <= 0 || it.rows - it.row0 <= kThinRows) {
     // (without keys as well: zeros, or nothing but the log-sum-exp of an empty range)
     const int begin = it.tile_begin * TileGeo<D>::kPages;
@@ -519,25 +652,114 @@ cache_tiles_kernel(RowArgs a) {
     const int last = min(it.rows, it.row0 + kBM);
     const int id = first_ids<kWaves>(it.table, a.ss.width, begin, 1);
     for (int row0 = it.row0; row0 < last; row0 += kThinRows)
-      rows_item<D, kThinRows / 16, kWaves, kPartial>(a, it.se, it.table, it.h, row0, it.rows, {begin, 1, end}, id, it.split,
-                                                     smem);
+      rows_item<D, kThinRows / 16, kWaves, kOut>(a, it.se, it.table, it.h, row0, it.rows, {begin, 1, end}, id,
+                                                 kMode == kEven ? it.slot : it.split, smem);
     return;
   }
   const bool active = it.row0 + 32 * wave < it.rows;
   if (wave >= kWaves / 2) {
-    if (active) run_tile_group<D, true, kPartial, true>(it, a, smem);
-    else run_tile_group<D, true, kPartial, false>(it, a, smem);
+    if (active) run_tile_group<D, true, kMode, true>(it, a, smem);
+    else run_tile_group<D, true, kMode, false>(it, a, smem);
   } else {
-    if (active) run_tile_group<D, false, kPartial, true>(it, a, smem);
-    else run_tile_group<D, false, kPartial, false>(it, a, smem);
+    if (active) run_tile_group<D, false, kMode, true>(it, a, smem);
+    else run_tile_group<D, false, kMode, false>(it, a, smem);
+  }
+}
+
+template <int D, Mode kMode>
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+cache_tiles_kernel(RowArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  if constexpr (kMode != kEven) {
+    TileItem it;
+    if (find_item<D>(a, &it)) run_item<D, kMode>(it, a, smem);
+    return;
+  }
+  // Between items the share's place is in LDS and the arguments are read again: held in scalar registers through the
+  // items, they leave the scheduler without room (the matrix step's reads then wait for each other).
+  typedef __attribute__((address_space(3))) int lds_int;
+  lds_int* const state = (lds_int*)((lds_char*)smem + tiles_lds<D>());  // Spot p, Spot end
+  {
+    const Work<D> work(a);
+    const int64_t x = share_of_block() * work.share;
+    if (x >= work.sum) return;
+    const Spot p = work.at(x), end = work.at(x + work.share);
+    if (threadIdx.x == 0) {
+      state[0] = p.s, state[1] = p.h, state[2] = p.tile, state[3] = p.t;
+      state[4] = end.s, state[5] = end.h, state[6] = end.tile, state[7] = end.t;
+    }
+  }
+  for (;;) {
+    __syncthreads();  // the state is there, and every wave is done with the last item's LDS
+    int base = (int)(uintptr_t)state;
+    __asm__ volatile("" : "+v"(base));
+    auto word = [&](int n) { return __builtin_amdgcn_readfirstlane(*(lds_int*)(uintptr_t)(unsigned)(base + 4 * n)); };
+    Spot p{word(0), word(1), word(2), word(3), 0};
+    const Spot end{word(4), word(5), word(6), word(7), 0};
+    if (!p.before(end)) return;
+    const RowArgs b = args_anew();
+    TileItem it;
+    it.se = session_of(b.ss, p.s);
+    it.se.q0 = __builtin_amdgcn_readfirstlane(it.se.q0);
+    it.se.rows = __builtin_amdgcn_readfirstlane(it.se.rows);
+    it.se.len = __builtin_amdgcn_readfirstlane(it.se.len);
+    it.rows = it.se.rows * b.G;
+    const int tiles = (it.se.len + Geo<D>::kBN - 1) / Geo<D>::kBN;
+    const bool last = p.s == end.s && p.h == end.h && p.tile == end.tile;
+    it.table = b.ss.table + (int64_t)p.s * b.ss.width;
+    it.h = p.h, it.row0 = p.tile * kBM, it.split = 0;
+    it.tile_begin = p.t, it.ntiles = (last ? end.t : tiles) - p.t;
+    it.slot = it.ntiles == tiles ? -1 : 2 * share_of_block() + (p.t > 0 ? 0 : 1);
+    const int nq = (it.rows + kBM - 1) / kBM;
+    const bool none = it.se.rows == 0;
+    if (none) p = {p.s + 1, 0, 0, 0, 0};
+    else if (last) p = end;
+    else next_item(p, nq, b.pool.H);
+    __syncthreads();  // every wave has read the state
+    if (threadIdx.x == 0) state[0] = p.s, state[1] = p.h, state[2] = p.tile, state[3] = p.t;
+    if (!none) run_item<D, kEven>(it, b, smem);
+  }
+}
+
+// Joins the parts of the items that the shares have cut: kJoinBlocks workgroups to a border between shares, the first of
+// those inside its item.
+constexpr int kJoinBlocks = 8;
+
+template <int D>
+__global__ void __launch_bounds__(kMergeThreads) cache_join_kernel(RowArgs a) {
+  const Work<D> work(a);
+  const int b = blockIdx.x / kJoinBlocks + 1;
+  if (b * work.share >= work.sum) return;
+  const Spot p = work.at(b * work.share);
+  if (p.t == 0) return;
+  const Session se = session_of(a.ss, p.s);
+  const typename Work<D>::Shape sh(se, a.G);
+  const int rows = se.rows * a.G, row0 = p.tile * kBM;
+  const int64_t cost = p.tile == sh.nq - 1 ? sh.last : sh.cost;
+  auto inside = [&](int j) {  // whether border j cuts this item
+    const int64_t in = j * work.share - p.from;
+    if (in < 0 || in >= cost) return false;
+    const int t = sh.cut(p.tile, (int)in);
+    return t > 0 && t < sh.tiles;
+  };
+  if (inside(b - 1)) return;
+  int n = 2;
+  while (inside(b + n - 1)) ++n;
+  constexpr int kChunks = D / 8;
+  for (int e = blockIdx.x % kJoinBlocks * kMergeThreads + threadIdx.x; e < kBM * kChunks; e += kJoinBlocks * kMergeThreads) {
+    const int r = e / kChunks, ch = e % kChunks * 8;
+    if (row0 + r >= rows) return;
+    auto part = [&](int k) { return (int64_t)(2 * (b + k) - (k == 0 ? 1 : 2)) * kBM + r; };
+    join_parts<D, 4>(a, n, part, row_of(se, row0 + r, p.h, a.pool.H, a.G), ch);
   }
 }
 
 template <int D>
 static hipError_t configure_d() {
-  const void* const all[] = {(const void*)cache_tiles_kernel<D, false>, (const void*)cache_tiles_kernel<D, true>};
+  const void* const all[] = {(const void*)cache_tiles_kernel<D, kWhole>, (const void*)cache_tiles_kernel<D, kSplit>,
+                             (const void*)cache_tiles_kernel<D, kEven>};
   for (const void* kern : all) {
-    const hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, tiles_lds<D>());
+    const hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, tiles_lds<D>() + kStateBytes);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -549,16 +771,21 @@ hipError_t configure_tiles() {
 }
 
 template <int D>
-static void launch_tiles_d(const RowArgs& r, unsigned grid, hipStream_t st) {
-  auto kern = r.n_split > 1 ? cache_tiles_kernel<D, true> : cache_tiles_kernel<D, false>;
+static void launch_tiles_d(const RowArgs& r, int64_t items, hipStream_t st) {
+  if (r.shares > 0) {
+    hipLaunchKernelGGL((cache_tiles_kernel<D, kEven>), dim3((r.shares + 7) / 8 * 8), dim3(kThreads), tiles_lds<D>() + kStateBytes, st, r);
+    hipLaunchKernelGGL(cache_join_kernel<D>, dim3((r.shares - 1) * kJoinBlocks), dim3(kMergeThreads), 0, st, r);
+    return;
+  }
+  const unsigned grid = (unsigned)((items + 7) / 8 * 8);  // every XCD has up to ceil(items / 8)
+  auto kern = r.n_split > 1 ? cache_tiles_kernel<D, kSplit> : cache_tiles_kernel<D, kWhole>;
   hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), tiles_lds<D>(), st, r);
 }
 
 // RowArgs' workgroups are 256-row tiles of a session and head here, `items` of them at most.
 void launch_tiles(const RowArgs& r, int d, int64_t items, hipStream_t st) {
-  const unsigned grid = (unsigned)((items + 7) / 8 * 8);  // every XCD has up to ceil(items / 8)
-  if (d == 64) launch_tiles_d<64>(r, grid, st);
-  else launch_tiles_d<128>(r, grid, st);
+  if (d == 64) launch_tiles_d<64>(r, items, st);
+  else launch_tiles_d<128>(r, items, st);
 }
 
 }  // namespace tscache

@@ -178,10 +178,6 @@ int launched(hipError_t e) {
   return TS_ERR_HIP;
 }
 
-int32_t choose_splits(int32_t n, const tscache::Sessions& ss, int32_t H, int32_t G, int32_t d, int tile, int32_t cus) {
-  return n > 0 ? n : tscache::auto_splits(ss.nseq, ss.max_rows, ss.max_len, ss.total, H, G, d, tile, cus);
-}
-
 }  // namespace
 
 extern "C" {
@@ -249,19 +245,14 @@ int ts_cache_attn(const ts_cache* cache, const void* q, void* o, float* lse, con
                        {table, (int64_t)nseq * width * 4},
                        {lens, (int64_t)nseq * 4}};
   if (aliased(written, read)) return TS_ERR_ALIAS;
-  if (num_splits > 0 && tscache::workspace_bytes(num_splits, total, Hq, cache->d) > workspace_bytes)
-    return TS_ERR_SCRATCH;
   const hipStream_t s = (hipStream_t)stream;
   DeviceState* st = current_device(&rc, s);
   if (!st) return rc;
-  tscache::AttnArgs a{pool_of(cache), {cu, table, lens, nseq, width, max_rows, max_len, total}, q, o, lse,
-                      nullptr, nullptr, cache->d, G, 1, scale, st->cus};
-  a.n_split = choose_splits(num_splits, a.ss, cache->H, G, cache->d, tile, st->cus);
-  while (a.n_split > 1 && tscache::workspace_bytes(a.n_split, total, Hq, cache->d) > workspace_bytes) --a.n_split;
-  if (a.n_split > 1) {
-    a.part_lse = (float*)workspace;
-    a.part_o = (float*)((char*)workspace + tscache::part_o_offset(a.n_split, total, Hq));
-  }
+  const tscache::Sessions ss{cu, table, lens, nseq, width, max_rows, max_len, total};
+  const tscache::Parts parts = tscache::attn_parts(ss, cache->H, G, cache->d, tile, num_splits, workspace_bytes, st->cus);
+  if (parts.bytes > workspace_bytes) return TS_ERR_SCRATCH;  // (ranges that the caller has asked for)
+  const tscache::AttnArgs a{pool_of(cache), ss, q, o, lse, (float*)((char*)workspace + parts.o_offset), (float*)workspace,
+                            cache->d, G, parts.n_split, parts.shares, scale};
   if (validate_mode() && !capturing(s) &&
       (rc = validate(a.ss, cache->pages, false, nullptr, 0, 0, s)) != TS_OK)
     return rc;
@@ -283,7 +274,7 @@ int64_t ts_cache_attn_workspace(int32_t nseq, int32_t max_rows, int32_t max_len,
   }
   const tscache::Sessions ss{nullptr, nullptr, nullptr, nseq, 0, max_rows, max_len, total};
   const int tile = tscache::row_tile((int64_t)max_rows * (Hq / H), 1.0f);
-  return tscache::workspace_bytes(choose_splits(num_splits, ss, H, Hq / H, d, tile, cus), total, Hq, d);
+  return tscache::attn_parts(ss, H, Hq / H, d, tile, num_splits, INT64_MAX, cus).bytes;
 }
 
 int ts_cache_weigh(const ts_cache* cache, const void* q, const float* lse, const int32_t* cu,

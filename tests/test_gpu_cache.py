@@ -250,6 +250,42 @@ def test_attn_splits(n, rows, lens, d):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows,lens,H,G", [
+    ([280], [8000], 1, 1), ([512], [16_000], 1, 1), ([257, 40], [6001, 5999], 2, 1),  # items cut several times
+    ([70, 300, 0, 33, 1], [5000, 900, 4000, 17_000, 0], 1, 2), ([35], [20_001], 2, 3),
+    ([40, 1] * 40, [300, 700] * 40, 1, 1), ([33], [63], 1, 1), ([600], [0], 1, 1)])
+def test_attn_equal_shares(rows, lens, H, G, d):
+    """Many rows whose work is dealt out in equal shares, wherever those cut a row tile's keys: twice the same result,
+    and the row tiles' own without a workspace."""
+    g = torch.Generator().manual_seed(sum(rows) + sum(lens) + d)
+    cache, table, cu, q, o, lse = run_attn(g, rows, lens, H, G, d)
+    def call(**kw):
+        return ts.ts_cache_attn(q.cuda(), cache, ints(cu), max(rows), ints(table), ints(lens), max(max(lens), 1),
+                                return_lse=True, **kw)
+    for x, y in zip(call(), (o, lse)):
+        assert torch.equal(x, y)
+
+
+def test_attn_takes_a_smaller_workspace(monkeypatch):
+    """The library's own choice falls back to whole row tiles, and to fewer ranges, as the caller's memory goes."""
+    g = torch.Generator().manual_seed(3)
+    lib = ts.load_cache()
+    for rows, n in ((300, 3000), (3, 3000)):
+        cache, table, cu, q, o, lse = run_attn(g, [rows], [n], 1, 1, 128)
+        def call(size, **kw):
+            with monkeypatch.context() as m:
+                m.setattr(lib, "ts_cache_attn_workspace", lambda *a: size)
+                return ts.ts_cache_attn(q.cuda(), cache, ints(cu), rows, ints(table), ints([n]), n, **kw)
+        whole = ts.ts_cache_attn(q.cuda(), cache, ints(cu), rows, ints(table), ints([n]), n, num_splits=1)
+        need = lib.ts_cache_attn_workspace(1, rows, n, rows, 1, 1, 128, 0)
+        assert need > 0 and torch.equal(call(need), o) and torch.equal(call(0), whole)
+        if rows == 300:
+            assert torch.equal(call(need - 1), whole)
+        with pytest.raises(RuntimeError):
+            call(0, num_splits=2)
+
+
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("rows", [3, 300])
 def test_attn_rising_scores(d, rows):
     """Keys that grow along the session, so that the running maximum moves in every page, by far at the end."""
@@ -300,7 +336,7 @@ def test_attn_ignores_what_lies_past_a_session(d, rows):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("rows,splits", [(2, 0), (2, 5), (300, 1), (300, 3)])
+@pytest.mark.parametrize("rows,splits", [(2, 0), (2, 5), (300, 0), (300, 1), (300, 3)])
 def test_attn_bad_sessions_and_pages(d, rows, splits):
     """Sessions that break the rules leave their rows; pages outside the pool, and pages of exponent 255, make
     theirs NaN; the others are as without them."""
