@@ -51,10 +51,16 @@ Parts attn_parts(const Sessions& ss, int32_t H, int32_t G, int32_t d, int tile, 
       n = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, ceil_div(ss.max_len, kPage) / 4, 64}));
       while (n > 1 && ranges(n, ss.total, H * G, d).bytes > workspace) --n;
     } else if (items < kEvenItems * (int64_t)cus) {
-      const int64_t cost = items * (ceil_div(ss.max_len, d == 64 ? 2 * kPage : kPage) + kStartCost);  // at most
+      const int64_t tiles = ceil_div(ss.max_len, d == 64 ? 2 * kPage : kPage), cost = items * (tiles + kStartCost);  // at most
+      // One session has the stated length, so ranges that fill the device can be told from here; costs in key tiles.
+      int64_t best = INT64_MAX;
+      for (int32_t i = 1; ss.nseq == 1 && i <= 16 && (i == 1 || tiles / i >= kCutMin); ++i) {
+        const int64_t c = ceil_div(items * i, cus) * (ceil_div(tiles, i) + kStartCost) + (i > 1 ? 6 : 0);
+        if (c < best && ranges(i, ss.total, H * G, d).bytes <= workspace) best = c, n = i;
+      }
       const int64_t shares = std::min<int64_t>(cus, ceil_div(cost, kShareMin));
       const Parts p = parts(1, (int32_t)shares, 2 * shares * kTileRows, d);
-      if (shares > 1 && p.bytes <= workspace) return p;
+      if (shares > 1 && p.bytes <= workspace && ceil_div(cost, shares) * 7 / 6 + 14 < best) return p;
     }
   }
   return ranges(n, ss.total, H * G, d);

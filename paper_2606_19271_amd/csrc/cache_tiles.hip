@@ -527,8 +527,9 @@ constexpr int kStateBytes = 32;  // where a share stands (kEven)
 // one of its two slots: 2 i, if the item began in an earlier share, else 2 i + 1; cache_join_kernel joins them.
 // Consecutive eighths of the shares go to the XCDs.  Against whole row tiles, or as many ranges of each as fill the device
 // when all sessions have the stated length: 257 .. 640 odd rows x 777 .. 20011 keys x 12 heads x 2, d = 64, 152 -> 119 us; six
-// sessions of 2730 to 32760 keys 961 -> 923; one of 32760 keys x 1560 rows x 12 heads, which three ranges fill exactly,
-// 294 -> 302 (the workgroups of an XCD then read the same keys at one time, and shares do not).
+// sessions of 2730 to 32760 keys 961 -> 923.  But the workgroups of an XCD no longer read the same keys at one time: one session
+// of 32760 keys x 1560 rows x 12 heads, whose row tiles in three ranges just fill the device, took 302 us instead of 294,
+// so a call of one session takes shares only where ranges leave a sixth idle (attn_parts).
 struct Spot {
   int s, h, tile, t;  // session, head, row tile, key tile of it (0 unless the spot is inside an item)
   int64_t from;       // where its item begins

@@ -270,16 +270,17 @@ def test_attn_takes_a_smaller_workspace(monkeypatch):
     """The library's own choice falls back to whole row tiles, and to fewer ranges, as the caller's memory goes."""
     g = torch.Generator().manual_seed(3)
     lib = ts.load_cache()
-    for rows, n in ((300, 3000), (3, 3000)):
-        cache, table, cu, q, o, lse = run_attn(g, [rows], [n], 1, 1, 128)
+    for rows, lens in (([300], [3000]), ([3], [3000]), ([300, 40], [3000, 500])):
+        cache, table, cu, q, o, lse = run_attn(g, rows, lens, 1, 1, 128)
+        args = (q.cuda(), cache, ints(cu), max(rows), ints(table), ints(lens), max(lens))
         def call(size, **kw):
             with monkeypatch.context() as m:
                 m.setattr(lib, "ts_cache_attn_workspace", lambda *a: size)
-                return ts.ts_cache_attn(q.cuda(), cache, ints(cu), rows, ints(table), ints([n]), n, **kw)
-        whole = ts.ts_cache_attn(q.cuda(), cache, ints(cu), rows, ints(table), ints([n]), n, num_splits=1)
-        need = lib.ts_cache_attn_workspace(1, rows, n, rows, 1, 1, 128, 0)
+                return ts.ts_cache_attn(*args, **kw)
+        whole = ts.ts_cache_attn(*args, num_splits=1)
+        need = lib.ts_cache_attn_workspace(len(rows), max(rows), max(lens), cu[-1], 1, 1, 128, 0)
         assert need > 0 and torch.equal(call(need), o) and torch.equal(call(0), whole)
-        if rows == 300:
+        if len(rows) == 2:
             assert torch.equal(call(need - 1), whole)
         with pytest.raises(RuntimeError):
             call(0, num_splits=2)
