@@ -89,12 +89,13 @@ def _pool(cache, need_weight=False):
         raise ValueError("cache.k must be a contiguous float8_e4m3fn GPU tensor")
     dev = k.device
     index = dev.index
-    for name, t, dtype, dim in (("k", k, _E4M3, 4), ("v", v, _E4M3, 4), ("k_exp", k_exp, _U8, 2), ("v_exp", v_exp, _U8, 2)):
-        if _not(t, dtype, dim, index):
-            raise ValueError("cache.%s must be a contiguous %s tensor with %d dims on one GPU" % (name, dtype, dim))
-    shape = k.shape
+    shape, scales = k.shape, k_exp.shape if isinstance(k_exp, Tensor) else None
+    if _not(k, _E4M3, 4, index) or _not(v, _E4M3, 4, index):
+        raise ValueError("cache.k and v must be contiguous float8_e4m3fn tensors [pages, H, %d, d] on one GPU" % PAGE)
+    if _not(k_exp, _U8, 2, index) or _not(v_exp, _U8, 2, index):
+        raise ValueError("cache.k_exp and v_exp must be contiguous uint8 tensors [pages, H] on the cache's GPU")
     pages, H, rows, d = shape
-    if rows != PAGE or v.shape != shape or k_exp.shape != (pages, H) or v_exp.shape != (pages, H):
+    if rows != PAGE or v.shape != shape or scales != shape[:2] or v_exp.shape != scales:
         raise ValueError("a cache is k, v [pages, H, %d, d] and k_exp, v_exp [pages, H]" % PAGE)
     if weight is not None:
         _check_weight("cache.weight", weight, shape, index)

@@ -245,12 +245,15 @@ int ts_cache_attn(const ts_cache* cache, const void* q, void* o, float* lse, con
                        {table, (int64_t)nseq * width * 4},
                        {lens, (int64_t)nseq * 4}};
   if (aliased(written, read)) return TS_ERR_ALIAS;
+  const tscache::Sessions ss{cu, table, lens, nseq, width, max_rows, max_len, total};
+  auto parts_on = [&](int32_t cus) {
+    return tscache::attn_parts(ss, cache->H, G, cache->d, tile, num_splits, workspace_bytes, cus);
+  };
+  if (num_splits > 0 && parts_on(1).bytes > workspace_bytes) return TS_ERR_SCRATCH;  // (as asked for, on any device)
   const hipStream_t s = (hipStream_t)stream;
   DeviceState* st = current_device(&rc, s);
   if (!st) return rc;
-  const tscache::Sessions ss{cu, table, lens, nseq, width, max_rows, max_len, total};
-  const tscache::Parts parts = tscache::attn_parts(ss, cache->H, G, cache->d, tile, num_splits, workspace_bytes, st->cus);
-  if (parts.bytes > workspace_bytes) return TS_ERR_SCRATCH;  // (ranges that the caller has asked for)
+  const tscache::Parts parts = parts_on(st->cus);
   const tscache::AttnArgs a{pool_of(cache), ss, q, o, lse, (float*)((char*)workspace + parts.o_offset), (float*)workspace,
                             cache->d, G, parts.n_split, parts.shares, scale};
   if (validate_mode() && !capturing(s) &&
