@@ -570,6 +570,7 @@ template <int D>
 struct Work {
   const RowArgs& a;
   int64_t sum, share;
+  int64_t cost, to;  // of up to 64 sessions, one a lane: its cost, and where it ends
 
   struct Shape {  // of a session: key tiles, row tiles, costs of a row tile, of the last one, and of a head
     int tiles, nq;
@@ -597,6 +598,10 @@ struct Work {
     const Session se = session_of(a.ss, s);
     return se.rows > 0 ? Shape(se, a.G).head * a.pool.H : 0;
   }
+  // of numbers that are not negative; most fit 32 bits, in which the division takes a fourth of the time
+  static __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
+    return (uint64_t)(x | y) >> 32 == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+  }
   static __device__ __forceinline__ int64_t scan(int64_t x, int lane) {  // inclusive, over the lanes
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) {
@@ -607,33 +612,40 @@ struct Work {
   }
   __device__ __forceinline__ Work(const RowArgs& args) : a(args) {
     const int lane = threadIdx.x & 63;
-    int64_t x = 0;
-    for (int s = lane; s < a.ss.nseq; s += 64) x += cost_of(s);
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
-    sum = x;
-    const int64_t each = (sum + a.shares - 1) / a.shares;
+    sum = 0;
+    for (int s0 = 0; s0 < a.ss.nseq; s0 += 64) {
+      cost = cost_of(s0 + lane);
+      to = sum + scan(cost, lane);
+      sum = __shfl(to, 63);
+    }
+    const int64_t each = quotient(sum + a.shares - 1, a.shares);
     share = each > kShareMin ? each : kShareMin;
   }
   __device__ __forceinline__ Spot at(int64_t x) const {
     const int lane = threadIdx.x & 63;
     Spot p{a.ss.nseq, 0, 0, 0, sum};
-    int64_t base = 0;
     if (x >= sum) return p;
-    for (int s0 = 0; s0 < a.ss.nseq; s0 += 64) {
-      const int64_t cost = cost_of(s0 + lane), to = base + scan(cost, lane);
+    auto find = [&](int s0, int64_t cost, int64_t to) {
       const unsigned long long hit = __builtin_amdgcn_ballot_w64(x < to);
-      if (hit != 0) {
-        const int i = __builtin_ctzll(hit);  // the first that ends past x
-        p.s = s0 + i, p.from = __shfl(to - cost, i);
-        break;
+      if (hit == 0) return false;
+      const int i = __builtin_ctzll(hit);  // the first that ends past x
+      p.s = s0 + i, p.from = __shfl(to - cost, i);
+      return true;
+    };
+    if (a.ss.nseq <= 64) {
+      find(0, cost, to);
+    } else {
+      int64_t base = 0;
+      for (int s0 = 0; s0 < a.ss.nseq; s0 += 64) {
+        const int64_t c = cost_of(s0 + lane), t = base + scan(c, lane);
+        if (find(s0, c, t)) break;
+        base = __shfl(t, 63);
       }
-      base = __shfl(to, 63);
     }
     const Shape sh(session_of(a.ss, p.s), a.G);
-    p.h = (int)((x - p.from) / sh.head);
+    p.h = (int)quotient(x - p.from, sh.head);
     p.from += p.h * sh.head;
-    const int64_t tile = (x - p.from) / sh.cost;
+    const int64_t tile = quotient(x - p.from, sh.cost);
     p.tile = tile < sh.nq ? (int)tile : sh.nq - 1;
     p.from += (int64_t)p.tile * sh.cost;
     p.t = sh.cut(p.tile, (int)(x - p.from));
