@@ -74,7 +74,7 @@ int64_t weigh_share(int32_t max_len, int32_t H) { return ceil_div((int64_t)H * c
 
 int64_t weigh_items(int32_t nseq, int32_t max_len, int32_t H) {
   const int64_t share = weigh_share(max_len, H);
-  return share > 0 && nseq > kGridLimit / share ? 4 * kGridLimit : 8 * nseq * share;
+  return share > 0 && nseq > kGridLimit / share ? 4 * kGridLimit : 8 * (int64_t)nseq * share;
 }
 
 int64_t append_items(int32_t nseq, int32_t max_rows, int32_t H) {
