@@ -19,7 +19,7 @@ namespace tscache {
 constexpr int kRowThreads = 256;
 constexpr int kRowWaves = kRowThreads / 64;
 
-template <int D, int NB, bool kPartial>
+template <int D, int NB, Out kOut>
 __global__ void __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 cache_rows_kernel(RowArgs a) {
   __shared__ __attribute__((aligned(16))) char smem[RowGeo<D, NB, kRowWaves>::kLds];
@@ -36,7 +36,7 @@ cache_rows_kernel(RowArgs a) {
   const int rows = se.rows * a.G, row0 = tile * 16 * NB;
   if (!se.ok || row0 >= rows) return;
   const PageRange range{split, a.n_split, (se.len + kPage - 1) / kPage};
-  rows_item<D, NB, kRowWaves, kPartial ? kSlab : kResult>(a, se, table, h, row0, rows, range, id, split, smem);
+  rows_item<D, NB, kRowWaves, kOut>(a, se, table, h, row0, rows, range, id, split, smem);
 }
 
 // Joins the page ranges of a split call: O = sum_i exp(lse_i - lse) O_i with lse = ln sum_i exp(lse_i).  One
@@ -58,9 +58,9 @@ __global__ void __launch_bounds__(kMergeThreads) cache_merge_kernel(RowArgs a, i
 // ---------------------------------------------------------------------------------------------
 // host-side launchers
 
-template <int D, bool kPartial>
+template <int D, Out kOut>
 static void launch_rows(const RowArgs& r, int tile, unsigned grid, hipStream_t st) {
-  auto kern = tile == 16 ? cache_rows_kernel<D, 1, kPartial> : cache_rows_kernel<D, 2, kPartial>;
+  auto kern = tile == 16 ? cache_rows_kernel<D, 1, kOut> : cache_rows_kernel<D, 2, kOut>;
   hipLaunchKernelGGL(kern, dim3(grid), dim3(kRowThreads), 0, st, r);
 }
 
@@ -72,8 +72,8 @@ static hipError_t launch_attn_d(const AttnArgs& a, hipStream_t st) {
             (int)((rows + tile - 1) / tile), fabsf(a.scale) * kLog2e, a.scale < 0.0f ? 0x80008000u : 0u};
   const int64_t items = attn_items(a.ss.nseq, a.ss.max_rows, a.ss.total, a.pool.H, a.G, tile) * a.n_split;
   if (tile == kTileRows) launch_tiles(r, D, items, st);
-  else if (a.n_split > 1) launch_rows<D, true>(r, tile, (unsigned)items, st);
-  else launch_rows<D, false>(r, tile, (unsigned)items, st);
+  else if (a.n_split > 1) launch_rows<D, kSlab>(r, tile, (unsigned)items, st);
+  else launch_rows<D, kResult>(r, tile, (unsigned)items, st);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_split == 1) return e;
   const int64_t blocks = merge_blocks(a.ss.nseq, a.ss.max_rows, a.pool.H * a.G, D);

@@ -47,8 +47,11 @@ Parts attn_parts(const Sessions& ss, int32_t H, int32_t G, int32_t d, int tile, 
   if (num_splits == 0) {
     const int64_t items = std::max<int64_t>(1, attn_items(ss.nseq, ss.max_rows, ss.total, H, G, tile));
     if (tile < kTileRows) {
+      // Four workgroups a CU, and a page at least to each of their four waves.  Up to 768 tokens one workgroup is done
+      // as soon as ranges and their merge are, and takes one launch (9.0 against 10.0 us at 512 tokens, 10.8 and 10.9 at
+      // 768, 12.8 and 11.3 at 1024).
       const int64_t want = 4 * (int64_t)cus / items;
-      n = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, ceil_div(ss.max_len, kPage) / 4, 64}));
+      if (ss.max_len > 768) n = (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, ceil_div(ss.max_len, kPage) / 4, 64}));
       while (n > 1 && ranges(n, ss.total, H * G, d).bytes > workspace) --n;
     } else if (items < kEvenItems * (int64_t)cus) {
       const int64_t tiles = ceil_div(ss.max_len, d == 64 ? 2 * kPage : kPage), cost = items * (tiles + kStartCost);  // at most

@@ -37,6 +37,7 @@ struct RowGeo {
   static constexpr int kVLoads = kPage * D / 1024;       // LDS DMA instructions of V per page
   static constexpr int kKLoads = D / 64;                 // 16-byte loads of K per lane and 16 keys
   static constexpr int kPageBytes = kPage * D;
+  static constexpr bool kEarly = D * NB < 256;           // room for two pages' keys in registers
   static constexpr int kVBufs = kW * 2 * kPageBytes;
   static constexpr int kObuf = kW * 16 * D * 4;          // over the V buffers, at the end
   static constexpr int kMl = kVBufs > kObuf ? kVBufs : kObuf;  // float [2][kW][16]: maxima and sums
@@ -97,13 +98,13 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
     vexp = a.pool.v_exp[(int64_t)id * H + h];
     if (bad) kexp = vexp = 255;  // reads as NaN
   };
-  u32x4 kx[4][kKLoads];
-  float ks, vs;
+  typedef u32x4 Keys[4][kKLoads];
   const int koff = i16 * D + D / 4 * g;
-  auto load = [&](int i) {  // page i of the wave
+  int i0 = 0, now = min(mine, 64);  // the pages whose numbers the lanes have: i0, ... i0 + now - 1 of the wave's
+  auto load = [&](int i, Keys& kx, lds_char* to) {  // page i0 + i; past the last of them, nothing
     const int64_t at = ((int64_t)__builtin_amdgcn_readlane(id, i & 63) * H + h) * kPageBytes;
     // rows past the session's end as zeros: scores that are masked, values that meet weights of zero
-    const int n = __builtin_amdgcn_readfirstlane(max(0, min(kPage, se.len - range.page(wave + kW * i) * kPage)));
+    const int n = __builtin_amdgcn_readfirstlane(i < now ? min(kPage, se.len - range.page(wave + kW * (i0 + i)) * kPage) : 0);
     __amdgpu_buffer_rsrc_t rk = make_rsrc(a.pool.k + at, (uint32_t)(n * D));
     __amdgpu_buffer_rsrc_t rv = make_rsrc(a.pool.v + at, (uint32_t)(n * D));
 #pragma unroll
@@ -111,37 +112,47 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
 #pragma unroll
       for (int x = 0; x < kKLoads; ++x)
         kx[kb][x] = __builtin_amdgcn_raw_buffer_load_b128(rk, koff + 16 * kb * D + 16 * x, 0, 0);
-    lds_char* const to = vbuf + (i & 1) * kPageBytes;
 #pragma unroll
     for (int x = 0; x < kVLoads; ++x) {
       const int row = (64 * x + lane) / (D / 16);
       dma16(rv, to + 1024 * x, row * D + v_chunk<D>(row, lane % (D / 16)) * 16);
     }
     __asm__ volatile("" ::: "memory");
-    // (after the loads: the first page's need not wait for its exponents)
-    ks = __uint_as_float((unsigned)__builtin_amdgcn_readlane(kexp, i & 63) << 23);
-    vs = __uint_as_float((unsigned)__builtin_amdgcn_readlane(vexp, i & 63) << 23);
   };
   if (mine > 0) exponents();
 
-  bf16x8 qf[NB][kKK];
+  u32x4 qraw[NB][kKK];
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
     const int r = row0 + 16 * n + i16;
     const __bf16* const src = a.q + row_of(se, min(r, rows - 1), h, H, G) * D + D / 4 * g;
 #pragma unroll
-    for (int kk = 0; kk < kKK; ++kk)
-      qf[n][kk] = __builtin_bit_cast(bf16x8, *(const u32x4*)(src + 8 * kk) ^ u32x4{a.flip, a.flip, a.flip, a.flip});
+    for (int kk = 0; kk < kKK; ++kk) qraw[n][kk] = *(const u32x4*)(src + 8 * kk);
   }
+  lds_char *const v0 = vbuf, *const v1 = vbuf + kPageBytes;
+  Keys k0, k1;
+  if (mine > 0) load(0, k0, v0);  // before the queries are waited for
+  bf16x8 qf[NB][kKK];
+#pragma unroll
+  for (int n = 0; n < NB; ++n)
+#pragma unroll
+    for (int kk = 0; kk < kKK; ++kk)
+      qf[n][kk] = __builtin_bit_cast(bf16x8, qraw[n][kk] ^ u32x4{a.flip, a.flip, a.flip, a.flip});
   f32x4 o[NB][kCB] = {};
   float m[NB], l[NB];
 #pragma unroll
   for (int n = 0; n < NB; ++n) m[n] = -INFINITY, l[n] = 0.0f;
 
-  if (mine > 0) load(0);
-  for (int i = 0; i < mine; ++i) {
-    const int valid = se.len - range.page(wave + kW * i) * kPage;  // keys of this page (64 or more: all)
-    const float v_scale = vs;
+  // Page i0 + i, its keys in kx; the next page's go to `next`, before this one's are waited for (R::kEarly) or once they are used.
+  // `from` holds the page's values, `to` takes the next page's: told that they are apart, the compiler does not have the
+  // transpose reads wait for every DMA in flight.
+  auto page = [&](int i, Keys& kx, Keys& next, lds_char* __restrict to, const lds_char* __restrict from) {
+    const int valid = se.len - range.page(wave + kW * (i0 + i)) * kPage;  // keys of this page (64 or more: all)
+    if (R::kEarly) load(i + 1, next, to);
+    // (after those loads: the first page's exponents may still be on their way)
+    const float ks = __uint_as_float((unsigned)__builtin_amdgcn_readlane(kexp, i) << 23);
+    const float v_scale = __uint_as_float((unsigned)__builtin_amdgcn_readlane(vexp, i) << 23);
+    if (R::kEarly) __builtin_amdgcn_sched_barrier(0);  // the products stay behind those loads
     f32x4 sc[NB][4] = {};
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb)
@@ -151,14 +162,7 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
 #pragma unroll
         for (int n = 0; n < NB; ++n) sc[n][kb] = mfma16(kf, qf[n][kk], sc[n][kb]);
       }
-    const bool more = i + 1 < mine;
-    if (more) {
-      if (((i + 1) & 63) == 0) {
-        id = i + 1 + lane < mine ? table[range.page(wave + kW * (i + 1 + lane))] : 0;
-        exponents();
-      }
-      load(i + 1);
-    }
+    if (!R::kEarly) load(i + 1, next, to);
     bf16x8 pf[NB][2];
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
@@ -189,9 +193,7 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
       for (int cb = 0; cb < kCB; ++cb) o[n][cb] *= alpha;
     }
     // this page's V: all but the next page's loads are done
-    if (more) wait_vmem_in_order<4 * kKLoads + kVLoads>();
-    else wait_vmem_in_order<0>();
-    const lds_char* const vb = vbuf + (i & 1) * kPageBytes;
+    wait_vmem_in_order<4 * kKLoads + kVLoads>();
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -201,7 +203,7 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
         const int r8 = i16 >> 1;
         const int row = 32 * u + (r8 & 4) * 4 + 4 * g + (r8 & 3);
         const i32x2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-            (lds_i32x2*)(vb + row * D + v_chunk<D>(row, cb) * 16 + 8 * (i16 & 1)));
+            (lds_i32x2*)(from + row * D + v_chunk<D>(row, cb) * 16 + 8 * (i16 & 1)));
         const bf16x8 vf = widen8((unsigned)x[0], (unsigned)x[1], v_scale);
 #pragma unroll
         for (int n = 0; n < NB; ++n) o[n][cb] = mfma16(vf, pf[n][u], o[n][cb]);
@@ -209,6 +211,23 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
     // the reads have left the buffer before the next but one page's DMA comes into it
     wait_lds();
     __asm__ volatile("" ::: "memory");
+  };
+  for (; i0 < mine; i0 += 64) {
+    if (i0 > 0) {
+      now = min(mine - i0, 64);
+      id = lane < now ? table[range.page(wave + kW * (i0 + lane))] : 0;
+      exponents();
+      load(0, k0, v0);
+    }
+    if constexpr (R::kEarly) {
+      for (int i = 0; i < now; i += 2) {
+        page(i, k0, k1, v1, v0);
+        if (i + 1 < now) page(i + 1, k1, k0, v0, v1);
+      }
+    } else {
+      for (int i = 0; i < now; ++i) page(i, k0, k0, i & 1 ? v0 : v1, i & 1 ? v1 : v0);
+    }
+    wait_vmem_in_order<0>();  // (nothing lands in the buffers any more)
   }
 
   // ---- join the waves: O = sum_w 2^(m_w - M) O_w / sum_w 2^(m_w - M) l_w, 16 rows at a time
