@@ -509,7 +509,7 @@ __device__ __forceinline__ bool find_item(const RowArgs& a, TileItem* it) {
 
 // A last tile of at most this many rows is shared by the eight waves, each taking pages of its own (rows_item): in
 // the schedule above one wave would work and seven keep its barriers, for three quarters of a full tile's time (32768
-// keys, d = 128: 206 us for 24 rows this way, 568 for 100, 713 for 256).
+// keys, d = 128: 201 us for 24 rows this way, 566 for 100, 710 for 256).
 constexpr int kThinRows = 32;
 
 template <int D>
