@@ -38,14 +38,17 @@ ROOT = os.path.dirname(os.path.abspath(__file__))
 sys.path.insert(0, ROOT)
 
 PEAK_BF16_TFLOPS = 2516.6  # 256 CU x 4096 dense bf16 flop/clk x 2.4 GHz
-KERNEL_SOURCE = os.path.join(ROOT, "paper_2606_19271_amd", "csrc", "attn_kernels.hip")
+KERNEL_SOURCES = [os.path.join(ROOT, "paper_2606_19271_amd", "csrc", f) for f in ("attn_kernels.hip", "attn_tile.h")]
 TRAFFIC_FILE = os.path.join(ROOT, "profiles", "traffic.json")
 METRIC = "attention TFLOPS (4·L²·d·H) + % bf16 MFMA peak at L=32760,H=40,d=128"
 
 
 def kernel_sha():
-    with open(KERNEL_SOURCE, "rb") as f:
-        return hashlib.sha256(f.read()).hexdigest()[:16]
+    h = hashlib.sha256()
+    for source in KERNEL_SOURCES:
+        with open(source, "rb") as f:
+            h.update(f.read())
+    return h.hexdigest()[:16]
 
 
 def traffic_bytes(workload):
