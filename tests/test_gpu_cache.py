@@ -253,7 +253,8 @@ def test_attn_splits(n, rows, lens, d):
 @pytest.mark.parametrize("rows,lens,H,G", [
     ([280], [8000], 1, 1), ([512], [16_000], 1, 1), ([257, 40], [6001, 5999], 2, 1),  # items cut several times
     ([70, 300, 0, 33, 1], [5000, 900, 4000, 17_000, 0], 1, 2), ([35], [20_001], 2, 3),
-    ([40, 1] * 40, [300, 700] * 40, 1, 1), ([33], [63], 1, 1), ([600], [0], 1, 1)])
+    ([40, 1] * 40, [300, 700] * 40, 1, 1), ([70, 1] * 40, [300, 700] * 40, 1, 1), ([33], [63], 1, 1), ([65], [63], 1, 1),
+    ([600], [0], 1, 1)])
 def test_attn_equal_shares(rows, lens, H, G, d):
     """Many rows whose work is dealt out in equal shares, wherever those cut a row tile's keys: twice the same result,
     and the row tiles' own without a workspace."""
@@ -659,22 +660,23 @@ def same(a, b):
     return all(torch.equal(bits(x), bits(y)) for x, y in zip(a, b))
 
 
+@pytest.mark.parametrize("rows", [40, 70])
 @pytest.mark.parametrize("splits", [0, 4])
-def test_graph_replays(splits):
+def test_graph_replays(splits, rows):
     """A whole chunk step in one HIP graph, replayed with new inputs and eager work in between: every replay as
     the eager calls."""
     g = torch.Generator().manual_seed(11)
-    t = chunk_step(g)
-    run_step(clone(t), splits=splits)  # the device's first call is outside capture
+    t = chunk_step(g, rows=(rows, 3))
+    run_step(clone(t), rows, splits)  # the device's first call is outside capture
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        got = run_step(t, splits=splits)
+        got = run_step(t, rows, splits)
     for i in range(4):
         for n in ("q", "k", "v"):
             t[n].copy_(bf16(normal(g, *t[n].shape)))
         want_t = clone(t)
-        want = run_step(want_t, splits=splits)
+        want = run_step(want_t, rows, splits)
         torch.cuda.synchronize()
         graph.replay()
         torch.cuda.synchronize()
@@ -682,11 +684,12 @@ def test_graph_replays(splits):
         assert same(t["cache"], want_t["cache"]), i
 
 
-def test_two_streams_at_once():
+@pytest.mark.parametrize("rows,splits", [(40, 6), (70, 0)])
+def test_two_streams_at_once(rows, splits):
     """Interleaved steps on two streams share nothing, workspaces included."""
     g = torch.Generator().manual_seed(12)
-    ts_ = [chunk_step(g), chunk_step(g, rows=(40, 40), lens=(600, 300))]
-    want = [run_step(clone(t), splits=6) for t in ts_]
+    ts_ = [chunk_step(g, rows=(rows, 3)), chunk_step(g, rows=(rows, rows), lens=(600, 300))]
+    want = [run_step(clone(t), rows, splits) for t in ts_]
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream() for _ in ts_]
     got = [None, None]
@@ -696,7 +699,7 @@ def test_two_streams_at_once():
     for r in range(6):
         for i, st in enumerate(streams):
             with torch.cuda.stream(st):
-                got[i] = run_step(work[r][i], splits=6)
+                got[i] = run_step(work[r][i], rows, splits)
         rounds.append(list(got))
     torch.cuda.synchronize()
     for got in rounds:
@@ -736,7 +739,8 @@ def test_more_sessions_than_lanes_in_large_tiles():
     run_attn(g, rows, lens, 1, 1, 64)
 
 
-@pytest.mark.parametrize("d,rows,splits", [(64, 40, 1), (128, 40, 1), (128, 290, 2), (64, 3, 1), (128, 20, 2)])
+@pytest.mark.parametrize("d,rows,splits", [(64, 40, 1), (128, 40, 1), (64, 70, 1), (128, 70, 1), (128, 70, 0), (128, 290, 2),
+                                           (64, 3, 1), (128, 20, 2)])
 def test_attn_long_sessions(d, rows, splits):
     """More pages than an item keeps at hand at once; the longer session ends inside a page and inside a tile, and a
     page far behind is outside the pool."""
