@@ -74,7 +74,7 @@ __device__ __forceinline__ int first_ids(const int32_t* table, int width, int fi
 }
 
 // Rows [row0, row0 + 16 NB) of `rows` (see row_of) over a range of pages, `id` its first_ids; kW waves, RowGeo::kLds
-// bytes of LDS.  `to`: of kSlab the range's number; of kSlot the slot, row0 its first row, or -1 for a result.
+// bytes of LDS.  `to`: of kSlab the range's number; of kSlot the first row's place in the slots, or -1 for a result.
 template <int D, int NB, int kW, Out kOut>
 __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, const int32_t* table, int h, int row0,
                                           int rows, const PageRange& range, int id, int to, char* smem) {
@@ -264,7 +264,7 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
     const float lse = sum == 0.0f ? -INFINITY : (big + __builtin_amdgcn_logf(sum)) * kLn2;
     const int64_t at = row_of(se, r, h, H, G);
     if (kOut == kSlab || (kOut == kSlot && to >= 0)) {
-      const int64_t part = kOut == kSlot ? (int64_t)to * kTileRows + (r - row0) : (int64_t)to * a.ss.total * (H * G) + at;
+      const int64_t part = kOut == kSlot ? (int64_t)to + (r - row0) : (int64_t)to * a.ss.total * (H * G) + at;
       if (sum != 0.0f)
 #pragma unroll
         for (int x = 0; x < kCh / 4; ++x) *(f32x4*)(a.part_o + part * D + och + 4 * x) = acc[x] * inv;

@@ -507,9 +507,10 @@ __device__ __forceinline__ bool find_item(const RowArgs& a, TileItem* it) {
   return true;
 }
 
-// A last tile of at most this many rows is shared by the eight waves, each taking pages of its own (rows_item): in
+// A last tile of at most twice this many rows is shared by the eight waves, each taking pages of its own (rows_item): in
 // the schedule above one wave would work and seven keep its barriers, for three quarters of a full tile's time (32768
-// keys, d = 128: 201 us for 24 rows this way, 566 for 100, 710 for 256).
+// keys, d = 128: 201 us for 24 rows this way, 566 for 100, 710 for 256); six sessions of 16384 keys x 300 rows x 12 heads take
+// 258 us, and 318 with their 44 rows in the schedule above.
 constexpr int kThinRows = 32;
 
 template <int D>
@@ -583,7 +584,7 @@ struct Work {
       nq = (rows + kBM - 1) / kBM;
       cost = tiles + kStartCost;
       const int active = (rows - (nq - 1) * kBM + 31) / 32;  // waves
-      part = active == 1 ? 9 : 12 + active;
+      part = active <= 2 ? 8 * active : 12 + active;
       last = (int)((int64_t)tiles * part / 20) + kStartCost;
       head = (int64_t)(nq - 1) * cost + last;
     }
@@ -658,15 +659,18 @@ template <int D, Mode kMode>
 __device__ __forceinline__ void run_item(const TileItem& it, const RowArgs& a, char* smem) {
   constexpr Out kOut = kMode == kEven ? kSlot : kMode == kSplit ? kSlab : kResult;
   const int wave = __builtin_amdgcn_readfirstlane(thread_anew() >> 6);
-  if (it.ntiles <= 0 || it.rows - it.row0 <= kThinRows) {
+  if (it.ntiles <= 0 || it.rows - it.row0 <= 2 * kThinRows) {
     // (without keys as well: zeros, or nothing but the log-sum-exp of an empty range)
     const int begin = it.tile_begin * TileGeo<D>::kPages;
     const int end = min((it.se.len + kPage - 1) / kPage, begin + it.ntiles * TileGeo<D>::kPages);
     const int last = min(it.rows, it.row0 + kBM);
     const int id = first_ids<kWaves>(it.table, a.ss.width, begin, 1);
-    for (int row0 = it.row0; row0 < last; row0 += kThinRows)
+    for (int row0 = it.row0; row0 < last; row0 += kThinRows) {
+      const int slot = it.slot < 0 ? -1 : it.slot * kBM + row0 - it.row0;
+      if (row0 > it.row0) __syncthreads();  // every wave is done with the rows before
       rows_item<D, kThinRows / 16, kWaves, kOut>(a, it.se, it.table, it.h, row0, it.rows, {begin, 1, end}, id,
-                                                 kMode == kEven ? it.slot : it.split, smem);
+                                                 kMode == kEven ? slot : it.split, smem);
+    }
     return;
   }
   const bool active = it.row0 + 32 * wave < it.rows;

@@ -254,7 +254,7 @@ def test_attn_splits(n, rows, lens, d):
     ([280], [8000], 1, 1), ([512], [16_000], 1, 1), ([257, 40], [6001, 5999], 2, 1),  # items cut several times
     ([70, 300, 0, 33, 1], [5000, 900, 4000, 17_000, 0], 1, 2), ([35], [20_001], 2, 3),
     ([40, 1] * 40, [300, 700] * 40, 1, 1), ([70, 1] * 40, [300, 700] * 40, 1, 1), ([33], [63], 1, 1), ([65], [63], 1, 1),
-    ([600], [0], 1, 1)])
+    ([600], [0], 1, 1), ([310, 90], [9000, 2000], 1, 1), ([150, 289], [3000, 7000], 2, 2), ([301], [4000], 1, 1)])
 def test_attn_equal_shares(rows, lens, H, G, d):
     """Many rows whose work is dealt out in equal shares, wherever those cut a row tile's keys: twice the same result,
     and the row tiles' own without a workspace."""
