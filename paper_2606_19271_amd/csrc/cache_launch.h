@@ -92,8 +92,10 @@ Parts attn_parts(const Sessions& ss, int32_t H, int32_t G, int32_t d, int tile, 
 constexpr int kStartCost = 4, kShareMin = 12, kCutMin = 4;
 constexpr int kEvenItems = 2;
 // Workgroups of the other kernels.
-// weigh: a page to a workgroup where there are few, else four pages of a head, in 8 XCDs x nseq sessions x weigh_share
+// weigh: with up to 64 rows of a cached head, the parts that the pages of a session and head are dealt to (else 0: not this
+// kernel); a page to a workgroup where there are few, else four pages of a head, in 8 XCDs x nseq sessions x weigh_share
 // workgroups, at most weigh_items.
+int32_t weigh_rows(int32_t nseq, int32_t max_rows, int32_t max_len, int32_t H, int32_t G, int32_t cus);
 bool weigh_few(int32_t nseq, int32_t max_len, int32_t H, int32_t cus);
 int64_t weigh_share(int32_t max_len, int32_t H);
 int64_t weigh_items(int32_t nseq, int32_t max_len, int32_t H);

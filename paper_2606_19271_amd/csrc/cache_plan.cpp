@@ -72,6 +72,12 @@ Parts attn_parts(const Sessions& ss, int32_t H, int32_t G, int32_t d, int tile, 
   return ranges(n, ss.total, H * G, d);
 }
 
+int32_t weigh_rows(int32_t nseq, int32_t max_rows, int32_t max_len, int32_t H, int32_t G, int32_t cus) {
+  if ((int64_t)max_rows * G > 64) return 0;
+  const int64_t items = (int64_t)nseq * H;  // below the launch limit, as weigh_items is
+  return (int32_t)std::max<int64_t>(1, std::min(8 * (int64_t)cus / items, ceil_div(max_len, 4 * kPage)));
+}
+
 bool weigh_few(int32_t nseq, int32_t max_len, int32_t H, int32_t cus) {
   return (int64_t)nseq * H * ceil_div(max_len, 4 * kPage) <= 2 * (int64_t)cus;
 }

@@ -15,6 +15,7 @@
 #include "attn_tile.h"
 #include "cache_device.h"
 #include "cache_launch.h"
+#include "cache_rows.h"
 
 namespace tscache {
 
@@ -319,12 +320,141 @@ cache_weigh_few_kernel(Pool pool, Sessions ss, const __bf16* __restrict__ q, con
   out[to] = pool.weight[to] + ((sums[lane] + sums[kPage + lane]) + (sums[2 * kPage + lane] + sums[3 * kPage + lane]));
 }
 
+// ---- few rows (up to 16 NB of a cached head, a token or two of each session): bound by reading the keys.  A wave walks
+// over pages of one (session, head), first, first + step, ...; S^T = K Q^T on 16x16x32 MFMAs with the keys straight from memory (as
+// rows_item has them: lane: row lane & 15, keys 4 (lane >> 4) + 0..3 of each 16), the next page asked for a step ahead.
+// 32 single tokens over 16384 keys x 8 heads take 116 us at d = 128 (4.6 TB/s) and 50 at d = 64, and 251 and 147 by the
+// kernel for many keys; 32 times 64 rows 130 and 81 instead of 238 and 149.
+template <int D, int NB>
+__global__ void __launch_bounds__(256) cache_weigh_rows_kernel(Pool pool, Sessions ss, const __bf16* __restrict__ q,
+                                                               const float* __restrict__ lse, float* __restrict__ out, int G,
+                                                               int split, float c, unsigned flip) {
+  constexpr int kKK = D / 32, kKLoads = D / 64, kW = 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i16 = lane & 15, g = lane >> 4, H = pool.H;
+  const int b = blockIdx.x, sh = b / split, h = sh % H, s = sh / H;
+  const PageRange range{b % split, split, 0};
+  const int32_t* const table = ss.table + (int64_t)s * ss.width;
+  int id = first_ids<kW>(table, ss.width, range.first, split);
+  const Session se = session_of(ss, s);
+  if (!se.ok) return;
+  const int rows = se.rows * G, len = __builtin_amdgcn_readfirstlane(se.len);
+  const int left = (len + kPage - 1) / kPage - range.page(wave), apart = kW * split;
+  const int mine = left > 0 ? (left + apart - 1) / apart : 0;
+  if (mine == 0) return;
+
+  struct Page {
+    u32x4 k[4][kKLoads];
+    float weight;
+  };
+  int i0 = 0, now = min(mine, 64), kexp = 0;
+  unsigned long long good = 0;  // of the lanes' pages, those in the pool
+  auto exponents = [&] {
+    const bool ok = (unsigned)id < (unsigned)pool.pages;
+    good = __builtin_amdgcn_ballot_w64(ok && lane < now);
+    id = ok ? id : 0;
+    kexp = pool.k_exp[(int64_t)id * H + h];
+  };
+  auto load = [&](int i, Page& p) {  // page i0 + i of the wave; past the last of them, one of the pool's
+    const int64_t ph = (int64_t)__builtin_amdgcn_readlane(id, i & 63) * H + h;
+    const uint8_t* const from = pool.k + ph * (kPage * D) + i16 * D + D / 4 * g;
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+      for (int x = 0; x < kKLoads; ++x) p.k[kb][x] = *(const u32x4*)(from + 16 * kb * D + 16 * x);
+    p.weight = pool.weight[ph * kPage + lane];
+  };
+  exponents();
+  u32x4 qraw[NB][kKK];
+  float ls[NB];
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+    const int r = 16 * n + i16;
+    const int64_t at = row_of(se, r, h, H, G);
+#pragma unroll
+    for (int kk = 0; kk < kKK; ++kk) qraw[n][kk] = u32x4{};  // rows past the last one: zeros, with weights of zero
+    ls[n] = INFINITY;
+    if (r < rows) {
+#pragma unroll
+      for (int kk = 0; kk < kKK; ++kk) qraw[n][kk] = *(const u32x4*)(q + at * D + D / 4 * g + 8 * kk);
+      ls[n] = lse[at];
+    }
+  }
+  Page p0, p1;
+  load(0, p0);
+  bf16x8 qf[NB][kKK];
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+#pragma unroll
+    for (int kk = 0; kk < kKK; ++kk) qf[n][kk] = __builtin_bit_cast(bf16x8, qraw[n][kk] ^ u32x4{flip, flip, flip, flip});
+    ls[n] *= kLog2e;
+  }
+  auto page = [&](int i, Page& p, Page& next) {
+    load(i + 1, next);
+    __builtin_amdgcn_sched_barrier(0);  // the products stay behind those loads
+    const float ks = __uint_as_float((unsigned)__builtin_amdgcn_readlane(kexp, i) << 23);
+    f32x4 sc[NB][4] = {};
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+      for (int kk = 0; kk < kKK; ++kk) {
+        const bf16x8 kf = widen8(p.k[kb][kk / 2][2 * (kk & 1)], p.k[kb][kk / 2][2 * (kk & 1) + 1], ks);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) sc[n][kb] = mfma16(kf, qf[n][kk], sc[n][kb]);
+      }
+    float x[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      x[j] = 0.0f;
+#pragma unroll
+      for (int n = 0; n < NB; ++n) x[j] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][j >> 2][j & 3], c, -ls[n]));
+    }
+#pragma unroll
+    for (int m = 8; m > 0; m >>= 1)
+#pragma unroll
+      for (int j = 0; j < m; ++j) {
+        const bool up = (lane & m) != 0;
+        const float lo = x[j], hi = x[j + m];
+        x[j] = (up ? hi : lo) + __shfl_xor(up ? lo : hi, m);
+      }
+    // lane 16 g + i has the sum of key 16 (i / 4) + 4 g + i % 4; from there to the lane that has this key's weight
+    const float sum = __shfl(x[0], (lane >> 2 & 3) * 16 + (lane >> 4) * 4 + (lane & 3));
+    const int at = range.page(wave + kW * (i0 + i)) * kPage;
+    if ((good >> i & 1) && at + lane < len)  // (without rows, weights as they were, those of NaN keys too)
+      out[((int64_t)__builtin_amdgcn_readlane(id, i) * H + h) * kPage + lane] = rows > 0 ? p.weight + sum : p.weight;
+  };
+  for (; i0 < mine; i0 += 64) {
+    if (i0 > 0) {
+      now = min(mine - i0, 64);
+      id = lane < now ? table[range.page(wave + kW * (i0 + lane))] : -1;
+      exponents();
+      load(0, p0);
+    }
+    for (int i = 0; i < now; i += 2) {
+      page(i, p0, p1);
+      if (i + 1 < now) page(i + 1, p1, p0);
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------------------------
 // host-side launcher
 
 hipError_t launch_weigh(const WeighArgs& a, hipStream_t st) {
   const float c = fabsf(a.scale) * kLog2e;
   const unsigned flip = a.scale < 0.0f ? 0x80008000u : 0u;
+  if (const int split = weigh_rows(a.ss.nseq, a.ss.max_rows, a.ss.max_len, a.pool.H, a.G, a.cus)) {
+    const int64_t rows = (int64_t)a.ss.max_rows * a.G;
+    auto kern = a.d == 64 ? (rows <= 16   ? cache_weigh_rows_kernel<64, 1>
+                             : rows <= 32 ? cache_weigh_rows_kernel<64, 2>
+                                          : cache_weigh_rows_kernel<64, 4>)
+                          : (rows <= 16   ? cache_weigh_rows_kernel<128, 1>
+                             : rows <= 32 ? cache_weigh_rows_kernel<128, 2>
+                                          : cache_weigh_rows_kernel<128, 4>);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(a.ss.nseq * a.pool.H * split)), dim3(256), 0, st, a.pool, a.ss, (const __bf16*)a.q,
+                       a.lse, a.out, a.G, split, c, flip);
+    return hipGetLastError();
+  }
   if (weigh_few(a.ss.nseq, a.ss.max_len, a.pool.H, a.cus)) {
     const int slots = (a.ss.max_len + kPage - 1) / kPage;
     auto kern = a.d == 64 ? cache_weigh_few_kernel<64> : cache_weigh_few_kernel<128>;

@@ -380,7 +380,7 @@ def test_attn_bad_sessions_and_pages(d, rows, splits):
 
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("H,G", [(2, 1), (1, 5)])
-@pytest.mark.parametrize("rows,lens", [([1], [1]), ([1, 1, 3], [64, 200, 65]), ([40, 0, 7], [130, 77, 0]), ([257], [700]),
+@pytest.mark.parametrize("rows,lens", [([1], [1]), ([1, 1, 3], [64, 200, 65]), ([40, 0, 7], [130, 77, 0]), ([20, 31, 17], [300, 129, 64]), ([257], [700]),
                                        ([1000], [100])])
 @pytest.mark.parametrize("scale", [None, -0.3])
 def test_weigh(rows, lens, H, G, d, scale):
@@ -447,6 +447,56 @@ def test_weigh_many_keys(d, G, rows, lens):
     assert np.all(np.isinf(got[over]))
     live &= ~over
     assert (np.abs(got - want)[live] / want[live]).max() <= rel
+
+
+@pytest.mark.parametrize("rows", [1, 30, 64])
+def test_weigh_long_sessions_of_many_heads(rows):
+    """So many heads that a workgroup has all of a session's pages, and each wave more than 64 of them, in a pool beyond
+    2 GiB: against the kernel for many rows, whose choice goes by the stated most of them."""
+    H, d, n = 2048, 64, 16_500
+    pages = -(-n // PAGE) + 1
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    cache = ts.session_cache(pages, H, d)
+    cache.k.view(torch.uint8).random_(0, 100, generator=g)
+    cache.k_exp.fill_(122)
+    cache.weight.random_(0, 5, generator=g)
+    table = torch.randperm(pages, generator=g, device="cuda").int()[None].contiguous()
+    q = torch.randn(rows, H, d, generator=g, device="cuda").bfloat16()
+    lse = torch.full((rows, H), 6.0, device="cuda")
+    a, b = cache.weight.clone(), cache.weight.clone()
+    for out, most in ((a, rows), (b, 65)):
+        ts.ts_cache_weigh(q, lse, cache, ints([0, rows]), most, table, ints([n]), n, out=out)
+    assert not torch.equal(a, cache.weight)
+    # scores good to (d + 2) 2^-24 of their terms' sum (below 2^9 here), which shifts a weight by as much relatively
+    torch.testing.assert_close(a, b, rtol=2 * 66 * 2.0 ** -15, atol=0)
+
+
+@pytest.mark.parametrize("rows", [2, 20, 100])
+@pytest.mark.parametrize("d", [64, 128])
+def test_weigh_of_nothing_finite(d, rows):
+    """A session without rows keeps its weights, NaN keys or not; infinite queries and an infinite lse as the formula has
+    them, next to sessions that they do not touch."""
+    g = torch.Generator().manual_seed(d + rows)
+    H = 2
+    cache = make_pool(g, 12, H, d)
+    cache.k_exp[1] = 255
+    table, lens, cu = ints([[0, 1, 2], [3, 4, 5], [6, 7, 8], [9, 10, 11]]), [190, 150, 192, 65], [0, 0, rows, rows + 1, rows + 2]
+    q = bf16(normal(g, rows + 2, H, d))
+    q[rows, 0, 0] = math.inf
+    lse = torch.full((rows + 2, H), 3.0)
+    lse[rows + 1, 0], lse[rows + 1, 1] = math.inf, -math.inf
+    want, before = R.Pool.of(cache), cache.weight.clone()
+    ts.ts_cache_weigh(q.cuda(), lse.cuda(), cache, ints(cu), max(rows, 1), table, ints(lens), 192)
+    after = cache.weight
+    assert torch.equal(after[:3], before[:3])
+    k = [want.tokens("k", [6, 7, 8], 192, h) for h in range(H)]
+    sign = np.sign(k[0][:, 0])
+    got = after[6:9, 0].reshape(-1).cpu().numpy()
+    assert np.all(np.isposinf(got[sign > 0])) and np.all(np.isnan(got[sign == 0]))
+    assert np.array_equal(got[sign < 0], before[6:9, 0].reshape(-1).cpu().numpy()[sign < 0])
+    assert torch.equal(after[9, 0], before[9, 0]) and torch.all(torch.isposinf(after[9, 1]))
+    assert torch.equal(after[10:], before[10:]) is False and torch.equal(after[10, :, 1:], before[10, :, 1:])
+    assert torch.all(torch.isfinite(after[3:5])) and torch.all(torch.isfinite(after[6:9, 1]))
 
 
 def test_weigh_bad_sessions_and_pages():
