@@ -88,9 +88,10 @@ struct Parts {
 Parts attn_parts(const Sessions& ss, int32_t H, int32_t G, int32_t d, int tile, int32_t num_splits, int64_t workspace,
                  int32_t cus);
 // Equal shares (Work in cache_tiles.hip), costs in key tiles: what an item costs beside its tiles, the least share, the
-// least part of an item.  With kEvenItems row tiles a CU and more, whole ones end evenly enough.
+// least part of an item.  With kEvenItems row tiles a CU and more, whole ones end evenly enough;
+// less than kEvenCost tiles a CU are not worth the shares.
 constexpr int kStartCost = 4, kShareMin = 12, kCutMin = 4;
-constexpr int kEvenItems = 2;
+constexpr int kEvenItems = 2, kEvenCost = 40;
 // Workgroups of the other kernels.
 // weigh: with up to 64 rows of a cached head, the parts that the pages of a session and head are dealt to (else 0: not this
 // kernel); a page to a workgroup where there are few, else four pages of a head, in 8 XCDs x nseq sessions x weigh_share

@@ -58,15 +58,19 @@ Parts attn_parts(const Sessions& ss, int32_t H, int32_t G, int32_t d, int tile, 
       while (n > 1 && ranges(n, ss.total, H * G, d).bytes > workspace) --n;
     } else if (items < kEvenItems * (int64_t)cus) {
       const int64_t tiles = ceil_div(ss.max_len, d == 64 ? 2 * kPage : kPage), cost = items * (tiles + kStartCost);  // at most
-      // One session has the stated length, so ranges that fill the device can be told from here; costs in key tiles.
+      // Ranges that fill the device when all sessions have the stated length, as one has; costs in key tiles.  They are
+      // also what small calls take, where the shares' longer start counts for more: two sessions of 512 and 1536 keys x 256
+      // rows x 4 heads 23 us, in shares 38.
+      const bool known = ss.nseq == 1 || ceil_div(cost, cus) < kEvenCost;
       int64_t best = INT64_MAX;
-      for (int32_t i = 1; ss.nseq == 1 && i <= 16 && (i == 1 || tiles / i >= kCutMin); ++i) {
+      for (int32_t i = 1; known && i <= 16 && (i == 1 || tiles / i >= kCutMin); ++i) {
         const int64_t c = ceil_div(items * i, cus) * (ceil_div(tiles, i) + kStartCost) + (i > 1 ? 6 : 0);
         if (c < best && ranges(i, ss.total, H * G, d).bytes <= workspace) best = c, n = i;
       }
       const int64_t shares = std::min<int64_t>(cus, ceil_div(cost, kShareMin));
       const Parts p = parts(1, (int32_t)shares, 2 * shares * kTileRows, d);
-      if (shares > 1 && p.bytes <= workspace && ceil_div(cost, shares) * 7 / 6 + 14 < best) return p;
+      const bool even = ss.nseq == 1 ? ceil_div(cost, shares) * 7 / 6 + 14 < best : !known;
+      if (even && shares > 1 && p.bytes <= workspace) return p;
     }
   }
   return ranges(n, ss.total, H * G, d);

@@ -530,7 +530,8 @@ constexpr int kStateBytes = 32;  // where a share stands (kEven)
 // when all sessions have the stated length: 257 .. 640 odd rows x 777 .. 20011 keys x 12 heads x 2, d = 64, 152 -> 119 us; six
 // sessions of 2730 to 32760 keys 961 -> 923.  But the workgroups of an XCD no longer read the same keys at one time: one session
 // of 32760 keys x 1560 rows x 12 heads, whose row tiles in three ranges just fill the device, took 302 us instead of 294,
-// so a call of one session takes shares only where ranges leave a sixth idle (attn_parts).
+// so a call of one session takes shares only where ranges leave a sixth idle; and finding a share takes 10 us, so
+// small calls take none (attn_parts).
 struct Spot {
   int s, h, tile, t;  // session, head, row tile, key tile of it (0 unless the spot is inside an item)
   int64_t from;       // where its item begins
@@ -659,13 +660,21 @@ template <int D, Mode kMode>
 __device__ __forceinline__ void run_item(const TileItem& it, const RowArgs& a, char* smem) {
   constexpr Out kOut = kMode == kEven ? kSlot : kMode == kSplit ? kSlab : kResult;
   const int wave = __builtin_amdgcn_readfirstlane(thread_anew() >> 6);
-  if (it.ntiles <= 0 || it.rows - it.row0 <= 2 * kThinRows) {
-    // (without keys as well: zeros, or nothing but the log-sum-exp of an empty range)
+  if (it.ntiles <= 0) {  // no keys: zeros, or nothing but the log-sum-exp of an empty range
+    const int n = min(it.rows - it.row0, kBM), H = a.pool.H;
+    float* const lse = kOut == kSlab ? a.part_lse + (int64_t)it.split * a.ss.total * (H * a.G) : a.lse;
+    for (int i = thread_anew(); i < n * (D / 8); i += kThreads) {
+      const int64_t at = row_of(it.se, it.row0 + i / (D / 8), it.h, H, a.G);
+      if (kOut != kSlab) *(u32x4*)(a.o + at * D + i % (D / 8) * 8) = u32x4{};
+      if (lse != nullptr && i % (D / 8) == 0) lse[at] = -INFINITY;
+    }
+    return;
+  }
+  if (it.rows - it.row0 <= 2 * kThinRows) {
     const int begin = it.tile_begin * TileGeo<D>::kPages;
     const int end = min((it.se.len + kPage - 1) / kPage, begin + it.ntiles * TileGeo<D>::kPages);
-    const int last = min(it.rows, it.row0 + kBM);
     const int id = first_ids<kWaves>(it.table, a.ss.width, begin, 1);
-    for (int row0 = it.row0; row0 < last; row0 += kThinRows) {
+    for (int row0 = it.row0; row0 < it.rows; row0 += kThinRows) {
       const int slot = it.slot < 0 ? -1 : it.slot * kBM + row0 - it.row0;
       if (row0 > it.row0) __syncthreads();  // every wave is done with the rows before
       rows_item<D, kThinRows / 16, kWaves, kOut>(a, it.se, it.table, it.h, row0, it.rows, {begin, 1, end}, id,
