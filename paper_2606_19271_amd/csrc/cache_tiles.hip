@@ -504,6 +504,7 @@ __device__ __forceinline__ bool find_item(const RowArgs& a, TileItem* it) {
   const int per = a.n_split == 1 ? tiles : __builtin_amdgcn_readfirstlane((tiles + a.n_split - 1) / a.n_split);
   it->tile_begin = it->split * per;
   it->ntiles = max(0, min(per, tiles - it->tile_begin));
+  it->slot = -1;
   return true;
 }
 
