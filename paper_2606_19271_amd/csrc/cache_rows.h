@@ -29,7 +29,9 @@ __device__ __forceinline__ void wait_vmem_in_order() {
 // are taken in the order in which two score blocks hold them.  K goes from memory to MFMA operands in registers: a
 // lane loads D / 4 consecutive channels of a key, and the sum over channels takes them in that order on both sides.
 // V's bytes go by LDS DMA to the wave's own two buffers, in an order (v_chunk) in which the 8-bit transpose reads
-// spread over the banks; both arrive a page ahead of their use.
+// spread over the banks; both arrive a page ahead of their use.  Bound by HBM: 32 single tokens x 8 heads x 5 over 32760 to
+// 6193 keys, d = 128, 215 us, 1.28 GB at 5.9 TB/s (one page's keys in registers at a time: 219); short calls by the round trips
+// from the lengths to the pages' numbers, to their bytes, to the result: 9.4 us for a page a wave.
 template <int D, int NB, int kW>
 struct RowGeo {
   static constexpr int kKK = D / 32;                     // MFMA steps over the channels
