@@ -436,10 +436,21 @@ struct Share {  // of a session's `count` items, `before` items of earlier sessi
   }
 };
 
+//
+// There are as many workgroups as disjoint sessions can have items (attn_items).  Where offsets run backwards, sessions can
+// name rows that others have too, and their items be more: then (crossed, in some lane) every workgroup goes on to the item
+// that comes a grid later.  A session's items are less than 2^23, so that those of 64 fit 32 bits.
+__device__ __forceinline__ bool crossed(const Sessions& ss) {
+  bool back = false;
+  for (int s = threadIdx.x & 63; s < ss.nseq; s += 64) back |= ss.cu[s + 1] < ss.cu[s];
+  return back;
+}
+
+// The at-th item of this workgroup's XCD.
 template <int D>
-__device__ __forceinline__ bool find_item(const RowArgs& a, TileItem* it) {
-  const int lane = threadIdx.x & 63, per_tile = a.pool.H * a.n_split;
-  const int xcd = blockIdx.x & 7, at = blockIdx.x >> 3;  // the at-th workgroup of that XCD
+__device__ __forceinline__ bool find_item(const RowArgs& a, int64_t at, TileItem* it) {
+  const int lane = thread_anew() & 63, per_tile = a.pool.H * a.n_split;
+  const int xcd = blockIdx.x & 7;
   auto items_of = [&](const Session& se) {
     return se.ok ? per_tile * (int)(((int64_t)se.rows * a.G + kBM - 1) / kBM) : 0;
   };
@@ -458,7 +469,7 @@ __device__ __forceinline__ bool find_item(const RowArgs& a, TileItem* it) {
     const unsigned long long hit = __builtin_amdgcn_ballot_w64(start <= at && at - start < share.n);
     if (hit != 0) {
       s = __builtin_ctzll(hit);
-      local = at - __builtin_amdgcn_readlane(start, s) + __builtin_amdgcn_readlane(share.first, s);
+      local = (int)at - __builtin_amdgcn_readlane(start, s) + __builtin_amdgcn_readlane(share.first, s);
     }
   } else {
     auto scan = [&](int x) {  // inclusive, over the lanes
@@ -469,19 +480,21 @@ __device__ __forceinline__ bool find_item(const RowArgs& a, TileItem* it) {
       }
       return x;
     };
-    int items = 0, base = 0;  // of the sessions so far: in all, and this XCD's
+    unsigned items = 0;  // of the sessions so far, modulo 8
+    int64_t base = 0;    // of them, this XCD's
     for (int s0 = 0; s0 < a.ss.nseq && s < 0; s0 += 64) {
       const int count = s0 + lane < a.ss.nseq ? items_of(session_of(a.ss, s0 + lane)) : 0;
       const int counts = scan(count);
-      const Share share(count, items + counts - count, xcd);
-      const int shares = scan(share.n), start = base + shares - share.n;
+      const Share share(count, (int)(items & 7) + counts - count, xcd);
+      const int shares = scan(share.n);
+      const int64_t start = base + (shares - share.n);
       const unsigned long long hit = __builtin_amdgcn_ballot_w64(start <= at && at - start < share.n);
       if (hit != 0) {
         const int i = __builtin_ctzll(hit);
         s = s0 + i;
-        local = at - __builtin_amdgcn_readlane(start, i) + __builtin_amdgcn_readlane(share.first, i);
+        local = (int)(at - base) - __builtin_amdgcn_readlane(shares - share.n, i) + __builtin_amdgcn_readlane(share.first, i);
       }
-      items += __builtin_amdgcn_readlane(counts, 63);
+      items += (unsigned)__builtin_amdgcn_readlane(counts, 63);
       base += __builtin_amdgcn_readlane(shares, 63);
     }
   }
@@ -658,31 +671,40 @@ struct Work {
 };
 
 template <int D, Mode kMode>
+constexpr Out out_of() { return kMode == kEven ? kSlot : kMode == kSplit ? kSlab : kResult; }
+
+// An item without keys: zeros, or nothing but the log-sum-exp of an empty range.
+template <int D, Mode kMode>
+__device__ __forceinline__ void run_empty(const TileItem& it, const RowArgs& a) {
+  constexpr Out kOut = out_of<D, kMode>();
+  const int n = min(it.rows - it.row0, kBM), H = a.pool.H;
+  float* const lse = kOut == kSlab ? a.part_lse + (int64_t)it.split * a.ss.total * (H * a.G) : a.lse;
+  for (int i = thread_anew(); i < n * (D / 8); i += kThreads) {
+    const int64_t at = row_of(it.se, it.row0 + i / (D / 8), it.h, H, a.G);
+    if (kOut != kSlab) *(u32x4*)(a.o + at * D + i % (D / 8) * 8) = u32x4{};
+    if (lse != nullptr && i % (D / 8) == 0) lse[at] = -INFINITY;
+  }
+}
+
+// An item's rows, kThinRows at a time, by waves that take pages of their own.
+template <int D, Mode kMode>
+__device__ __forceinline__ void run_thin(const TileItem& it, const RowArgs& a, char* smem) {
+  const int begin = it.tile_begin * TileGeo<D>::kPages, row_end = min(it.rows, it.row0 + kBM);
+  const int end = min((it.se.len + kPage - 1) / kPage, begin + it.ntiles * TileGeo<D>::kPages);
+  const int id = first_ids<kWaves>(it.table, a.ss.width, begin, 1);
+  for (int row0 = it.row0; row0 < row_end; row0 += kThinRows) {
+    const int slot = it.slot < 0 ? -1 : it.slot * kBM + row0 - it.row0;
+    if (row0 > it.row0) __syncthreads();  // every wave is done with the rows before
+    rows_item<D, kThinRows / 16, kWaves, out_of<D, kMode>()>(a, it.se, it.table, it.h, row0, it.rows, {begin, 1, end}, id,
+                                                             kMode == kEven ? slot : it.split, smem);
+  }
+}
+
+template <int D, Mode kMode>
 __device__ __forceinline__ void run_item(const TileItem& it, const RowArgs& a, char* smem) {
-  constexpr Out kOut = kMode == kEven ? kSlot : kMode == kSplit ? kSlab : kResult;
   const int wave = __builtin_amdgcn_readfirstlane(thread_anew() >> 6);
-  if (it.ntiles <= 0) {  // no keys: zeros, or nothing but the log-sum-exp of an empty range
-    const int n = min(it.rows - it.row0, kBM), H = a.pool.H;
-    float* const lse = kOut == kSlab ? a.part_lse + (int64_t)it.split * a.ss.total * (H * a.G) : a.lse;
-    for (int i = thread_anew(); i < n * (D / 8); i += kThreads) {
-      const int64_t at = row_of(it.se, it.row0 + i / (D / 8), it.h, H, a.G);
-      if (kOut != kSlab) *(u32x4*)(a.o + at * D + i % (D / 8) * 8) = u32x4{};
-      if (lse != nullptr && i % (D / 8) == 0) lse[at] = -INFINITY;
-    }
-    return;
-  }
-  if (it.rows - it.row0 <= 2 * kThinRows) {
-    const int begin = it.tile_begin * TileGeo<D>::kPages;
-    const int end = min((it.se.len + kPage - 1) / kPage, begin + it.ntiles * TileGeo<D>::kPages);
-    const int id = first_ids<kWaves>(it.table, a.ss.width, begin, 1);
-    for (int row0 = it.row0; row0 < it.rows; row0 += kThinRows) {
-      const int slot = it.slot < 0 ? -1 : it.slot * kBM + row0 - it.row0;
-      if (row0 > it.row0) __syncthreads();  // every wave is done with the rows before
-      rows_item<D, kThinRows / 16, kWaves, kOut>(a, it.se, it.table, it.h, row0, it.rows, {begin, 1, end}, id,
-                                                 kMode == kEven ? slot : it.split, smem);
-    }
-    return;
-  }
+  if (it.ntiles <= 0) return run_empty<D, kMode>(it, a);
+  if (it.rows - it.row0 <= 2 * kThinRows) return run_thin<D, kMode>(it, a, smem);
   const bool active = it.row0 + 32 * wave < it.rows;
   if (wave >= kWaves / 2) {
     if (active) run_tile_group<D, true, kMode, true>(it, a, smem);
@@ -699,8 +721,21 @@ cache_tiles_kernel(RowArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   if constexpr (kMode != kEven) {
     TileItem it;
-    if (find_item<D>(a, &it)) run_item<D, kMode>(it, a, smem);
-    return;
+    const bool back = crossed(a.ss);  // (asked for with the sessions, looked at behind them)
+    if (!find_item<D>(a, blockIdx.x >> 3, &it)) return;
+    const bool more = __builtin_amdgcn_ballot_w64(back) != 0;
+    run_item<D, kMode>(it, a, smem);
+    if (!more) return;
+    // The items that are left where sessions share rows, by the thin path whatever their rows: run_item in a loop would have
+    // the registers of every call's items hold what the next one needs (4680 rows x 32760 keys x 40 heads, d = 128: 3030
+    // instead of 2706 us).
+    for (int64_t at = (blockIdx.x >> 3) + (gridDim.x >> 3);; at += gridDim.x >> 3) {
+      __syncthreads();  // every wave is done with the last item's LDS
+      const RowArgs b = args_anew();
+      if (!find_item<D>(b, at, &it)) return;
+      if (it.ntiles <= 0) run_empty<D, kMode>(it, b);
+      else run_thin<D, kMode>(it, b, smem);
+    }
   }
   // Between items the share's place is in LDS and the arguments are read again: held in scalar registers through the
   // items, they leave the scheduler without room (the matrix step's reads then wait for each other).
