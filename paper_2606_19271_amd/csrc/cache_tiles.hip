@@ -107,7 +107,11 @@ struct NoHook {
   __device__ void operator()(int) const {}
 };
 
-constexpr float kTileBias = 39.0f;  // as kBias of attn_kernels.hip: the largest weight so far is 2^-39
+// As kBias of attn_kernels.hip, the running maximum is raised by this, so that the largest weight so far is 2^-15 and a later one can
+// be 2^16 times as large before the maximum moves.  Less than kBias: exponents of the largest weights are good to half a step
+// at 15, 2^-21 (of numbers around 39 it is 2^-19), which the log-sum-exp shows, and products with the smallest values that
+// a page holds, 2^-109, stay normal numbers.
+constexpr float kTileBias = 15.0f;
 enum TilePlace { kFirst = 0, kInner = 1, kLast = 2 };
 
 // The online softmax of one tile, as softmax_tile of attn_kernels.hip: the running maximum stays while the weights of
@@ -201,7 +205,9 @@ __device__ __forceinline__ void write_rows(const TileItem& it, const RowArgs& a,
   }
   float* const lse = kPartial ? a.part_lse : a.lse;
   if (lse != nullptr && hb == 0 && q0 + col < it.rows)
-    lse[place(q0 + col)] = l == 0.0f ? -INFINITY : (m_c + __builtin_amdgcn_logf(l)) * kLn2;
+    // the bias is taken out of both terms first: numbers of its size that cancel would leave their rounding
+    lse[place(q0 + col)] =
+        l == 0.0f ? -INFINITY : ((m_c - kTileBias) + __builtin_amdgcn_logf(l * (float)(1 << (int)kTileBias))) * kLn2;
 }
 
 // kActive = false: a wave whose rows all lie past the session's: it fetches its share and keeps the barriers.

@@ -81,3 +81,65 @@ def test_attn_sessions_that_overlap_leave_the_others_alone(cu, most, splits, d):
     assert (out[rows].float() - alone[0].float()).abs().max() <= 4 * 2.0 ** -8 * 6
     assert (lse[rows] - alone[1]).abs().max() <= 1e-4
     assert torch.all(out[:cu[-2]] != 7.0)
+
+
+# ---- the log-sum-exp's last bits
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows", [20, 70])
+def test_lse_of_equal_scores(rows, d):
+    """Queries of zeros: every weight is the same power of two and every sum exact, so that the log-sum-exp is ln of the
+    length but for one logarithm (an ulp, 2^-23), the constant ln 2 (2^-25) and their product's rounding (2^-24): less than
+    2^-22 of its value."""
+    lens = [1, 2, 3, 5, 17, 63, 64, 65, 100, 127, 128, 129, 200, 333, 500, 700, 1000, 1023, 1300, 1999]
+    g = gen(rows + d)
+    cache, table = filled(g, lens, 1, d)
+    q = torch.zeros(rows * len(lens), 1, d, dtype=torch.bfloat16, device="cuda")
+    cu = [rows * i for i in range(len(lens) + 1)]
+    _, lse = ts.ts_cache_attn(q, cache, ints(cu), rows, ints(table), ints(lens), max(lens), return_lse=True, num_splits=1)
+    got = lse.double().cpu().numpy().reshape(len(lens), rows)
+    want = np.log(lens)[:, None]
+    assert np.all(np.abs(got - want) <= 2.0 ** -22 * want)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows", [20, 70])
+def test_lse_of_one_token(rows, d):
+    """One key: the log-sum-exp is its score.  q and k have one channel that is not zero and few bits, so the product is
+    exact; scaled to log2 units (2^-23: the constant and a rounding), taken from the running maximum and put back (a weight's
+    exponent is good to 2^-21, half a step at the size of the bias), and times ln 2 (2^-23)."""
+    n = 50
+    score = torch.arange(1, n + 1).float() * 0.375 - 9.0
+    k = torch.zeros(n, 1, d)
+    k[:, 0, 0] = score
+    k = k.bfloat16().cuda()
+    cache, table = filled(gen(1), [1] * n, 1, d, k=k, v=k)
+    q = torch.zeros(n * rows, 1, d, dtype=torch.bfloat16, device="cuda")
+    q[:, 0, 0] = 1.0
+    pool = R.Pool.of(cache)
+    want = np.array([pool.tokens("k", table[s], 1, 0)[0, 0] for s in range(n)])[:, None]
+    _, lse = ts.ts_cache_attn(q, cache, ints([rows * i for i in range(n + 1)]), rows, ints(table), ints([1] * n), 64, scale=1.0,
+                              return_lse=True, num_splits=1)
+    got = lse.double().cpu().numpy().reshape(n, rows)
+    assert np.all(np.abs(got - want) <= 2.0 ** -21 * math.log(2) + 2.0 ** -22 * np.abs(want))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows,splits", [(3, 1), (70, 1), (70, 3)])
+@pytest.mark.parametrize("size", [-96, -104])
+def test_attn_of_the_smallest_values(size, rows, splits, d):
+    """Values near the least exponent of a page: products with weights of 2^-15 of the largest one's size stay normal numbers.
+    The weights' rounding (2^-8 of the values' average size), the result's (2^-8), a score good to (d + 2) 2^-24 of its terms' sum, and
+    what a product under 2^-126 could lose: n weights of less than 2^-111 / |v|, relative to a total of at least 1."""
+    g = gen(rows + d + splits)
+    H, n = 2, 400
+    cache, table = filled(g, [n], H, d, v=2.0 ** size)
+    q = normal(g, rows, H, d).bfloat16()
+    o = ts.ts_cache_attn(q, cache, ints([0, rows]), rows, ints(table), ints([n]), n, num_splits=splits)
+    pool, q64 = R.Pool.of(cache), q.double().cpu().numpy()
+    scale = float(np.float32(1 / math.sqrt(d)))
+    ro, _, av = R.attend(pool, q64, [0, rows], table, [n], scale)
+    terms = max(np.abs(pool.tokens("k", table[0], n, h)).max() for h in range(H)) * np.abs(q64).sum(2).max() * scale
+    bound = (2.0 ** -8 + 2 * (d + 2) * 2.0 ** -24 * terms) * av + 2.0 ** -8 * np.abs(ro) + n * 2.0 ** -133
+    off = np.abs(o.double().cpu().numpy() - ro)
+    assert np.all(off <= bound), (off / bound).max()
