@@ -143,3 +143,52 @@ def test_attn_of_the_smallest_values(size, rows, splits, d):
     bound = (2.0 ** -8 + 2 * (d + 2) * 2.0 ** -24 * terms) * av + 2.0 ** -8 * np.abs(ro) + n * 2.0 ** -133
     off = np.abs(o.double().cpu().numpy() - ro)
     assert np.all(off <= bound), (off / bound).max()
+
+
+# ---- rows that one key dominates
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H,G,rows,n,splits", [(1, 1, 300, 1300, 1), (2, 2, 70, 1999, 1), (1, 1, 300, 3000, 4), (1, 1, 513, 777, 0)])
+@pytest.mark.parametrize("gain", [0.5, 2.0, 5.0])
+def test_attn_of_equal_values(gain, H, G, rows, n, splits, d):
+    """Values that are the same for every token, so that whatever the weights O is that value, but for their rounding to 16 bits:
+    2^-8 of it at most, and a rounding of the result.  A key that holds more than two thirds of a row is more than twice of what
+    comes before it, and its weight is exact: there only the others' third is off, by less than the 0.53 * 2^-8 that half a
+    step is of these values (mantissas up to 1.875), and O is the value itself."""
+    g = gen(rows + n + d)
+    v = torch.tensor([1.875, -1.75, 3.5, 0.9375])[torch.arange(d) % 4].expand(n, H, d).bfloat16().contiguous().cuda()
+    cache, table = filled(g, [n], H, d, k=gain, v=v)
+    q = normal(g, rows, H * G, d).bfloat16()
+    args = (q, cache, ints([0, rows]), rows, ints(table), ints([n]), n)
+    o, _ = ts.ts_cache_attn(*args, return_lse=True, num_splits=splits)
+    assert torch.equal(ts.ts_cache_attn(*args, num_splits=splits), o)
+    pool, held = R.Pool.of(cache), torch.zeros(rows, H * G, dtype=torch.bool, device="cuda")
+    for hq in range(H * G):
+        k = torch.from_numpy(pool.tokens("k", table[0], n, hq // G)).cuda()
+        w = torch.softmax(q[:, hq].double() @ k.T / math.sqrt(d), 1)
+        held[:, hq] = w.max(1).values > 0.67
+    assert held.any() or gain < 5
+    want = v[:1, :1].expand_as(o)
+    assert torch.equal(o[held], want[held])
+    assert ((o.double() / want.double()) - 1).abs().max() <= 2 * 2.0 ** -8
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("height", [3.3, 5.1, 7.9])
+def test_attn_of_a_dominating_key(height, d):
+    """One key of more than twice the weight of all that come before it, in a tile between the first and the last, and of values where
+    the others have zeros: O is the key's value times its share, within a rounding of the result (2^-8) and the shift of two
+    scores (each good to (d + 2) 2^-24 of its one term, 10 at most here, and 2^-20).  Had its weight been rounded too, it would be
+    off by up to another 2^-8."""
+    n, rows, at = 400, 80, 200
+    k, v = torch.zeros(n, 1, d), torch.zeros(n, 1, d)
+    k[:, 0, 0] = -4.0
+    k[at, 0, 0] = 4.0
+    v[at, 0] = torch.tensor([1.875, -1.25, 3.5, 1.0])[torch.arange(d) % 4]
+    cache, table = filled(gen(2), [n], 1, d, k=k.bfloat16().cuda(), v=v.bfloat16().cuda())
+    q = torch.zeros(rows, 1, d)
+    q[:, 0, 0] = height * (1 + torch.arange(rows) / rows / 8)
+    q = q.bfloat16().cuda()
+    o = ts.ts_cache_attn(q, cache, ints([0, rows]), rows, ints(table), ints([n]), n, scale=0.25, num_splits=1).double().cpu().numpy()
+    ro, _, _ = R.attend(R.Pool.of(cache), q.double().cpu().numpy(), [0, rows], table, [n], 0.25)
+    assert np.all(np.abs(o - ro) <= (2.0 ** -8 + 2 * (d + 2) * 2.0 ** -24 * 20 + 2.0 ** -19) * np.abs(ro))
