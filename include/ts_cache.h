@@ -12,7 +12,7 @@
  *   k_exp, v_exp  uint8 [pages][H]: a stored element stands for e4m3 * 2^(exp - 127); 255 makes the
  *                 page's elements NaN.  ts_cache_append and ts_cache_evict write exponents in 27..247,
  *                 and every element of such a page is exact in bfloat16; tokens of a page with any other
- *                 exponent have unspecified values.
+ *                 exponent, and elements of 2^128 and more, have unspecified values.
  *   weight        float32 [pages][H][64] (16-byte aligned): the attention weight each token has
  *                 collected.  May be NULL where a call does not use it (ts_cache_attn; append, which
  *                 then clears nothing).
@@ -71,8 +71,9 @@ typedef struct ts_cache {
  * is also skipped when its new length passes 64 * width.
  * Per page and head, n is the least integer >= -100 with |x| <= 448 * 2^n for every finite new element x
  * (-100 where there is none); a page that already holds tokens of the session keeps at least its exponent.
- * exp = n + 127, elements are stored as x * 2^-n rounded to nearest even (infinities and NaN as NaN), and
- * older tokens of a page whose exponent rises are rounded again.  The new tokens' weights become 0; other
+ * exp = n + 127, elements are stored as x * 2^-n rounded to nearest even (infinities and NaN as NaN; where
+ * exp is 247, as 240 at most, since 256 * 2^120 is no bfloat16), and older tokens of a page whose exponent
+ * rises are rounded again.  The new tokens' weights become 0; other
  * slots stay as they are.  The sessions' written pages must be distinct.
  */
 int ts_cache_append(const ts_cache* cache, const void* k, const void* v, const int32_t* cu,

@@ -60,6 +60,14 @@ __device__ __forceinline__ unsigned narrow4(float a, float b, float c, float d) 
   return (unsigned)r;
 }
 
+// Four bytes of a page with this exponent.  At the largest one, 247, a magnitude of 1.9375 * 2^127 or more is rounded to
+// 256 * 2^120, which is no bfloat16: it becomes the element before, 240 * 2^120.
+__device__ __forceinline__ unsigned in_bf16(unsigned bytes, int exp) {
+  if (exp != 247) return bytes;
+  const unsigned off = (bytes & 0x7f7f7f7fu) ^ 0x78787878u;  // 0 where the byte is +-256
+  return bytes - (~(off + 0x7f7f7f7fu) >> 7 & 0x01010101u);
+}
+
 // The largest finite magnitude of packed bfloat16 bits, as bits (a positive bfloat16 orders as its bits).
 __device__ __forceinline__ unsigned amax_bits(unsigned amax, unsigned packed) {
   const unsigned lo = packed & 0x7fffu, hi = packed >> 16 & 0x7fffu;

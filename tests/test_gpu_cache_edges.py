@@ -192,3 +192,39 @@ def test_attn_of_a_dominating_key(height, d):
     o = ts.ts_cache_attn(q, cache, ints([0, rows]), rows, ints(table), ints([n]), n, scale=0.25, num_splits=1).double().cpu().numpy()
     ro, _, _ = R.attend(R.Pool.of(cache), q.double().cpu().numpy(), [0, rows], table, [n], 0.25)
     assert np.all(np.abs(o - ro) <= (2.0 ** -8 + 2 * (d + 2) * 2.0 ** -24 * 20 + 2.0 ** -19) * np.abs(ro))
+
+
+# ---- the ends of the format
+
+def test_append_and_evict_of_the_largest_magnitudes():
+    """The largest bfloat16 magnitudes would round to 2^128, which no bfloat16 holds: they become the largest element that does,
+    240 * 2^120, so that every element is a finite bfloat16 and survives an eviction."""
+    d, H = 64, 2
+    top = torch.tensor([0x7f00, 0x7f60, 0x7f61, 0x7f70, 0x7f71, 0x7f77, 0x7f78, 0x7f7f], dtype=torch.int16)  # 2^127 .. the largest
+    x = torch.zeros(70, H, d, dtype=torch.bfloat16)
+    x.view(torch.int16)[:, 0] = top[torch.arange(70 * d) % 8].reshape(70, d)
+    x[:, 1] = -x[:, 0]
+    x[3, 0, 0], x[4, 0, 0] = math.inf, math.nan
+    cache = ts.session_cache(4, H, d)
+    x = x.cuda()
+    ts.ts_cache_append(cache, x, x, ints([0, 70]), 70, ints([[2, 0]]), ints([0]))
+    pool = R.Pool.of(cache)
+    assert np.all(pool.k_exp[[2, 0]] == 247) and np.all(pool.v_exp[[2, 0]] == 247)
+    xs = x.double().cpu().numpy()
+    want = np.minimum(np.abs(np.where(np.isfinite(xs), xs, 0)), 240 * 2.0 ** 120)
+    want = R.VALUES[R.round_e4m3(want * 2.0 ** -120)] * 2.0 ** 120 * np.where(np.isfinite(xs), np.sign(np.nan_to_num(xs)), np.nan)
+    for name in ("k", "v"):
+        for h in range(H):
+            got = pool.tokens(name, [2, 0], 70, h)
+            np.testing.assert_array_equal(got, want[:, h])
+            fine = np.isfinite(got)
+            assert np.all(torch.from_numpy(got[fine]).bfloat16().double().numpy() == got[fine])
+    # older tokens of a page whose exponent rises, and an eviction
+    cache.weight.copy_(torch.rand(cache.weight.shape, generator=gen(1), device="cuda"))
+    ts.ts_cache_append(cache, x[:1] * 0.25, x[:1], ints([0, 1]), 1, ints([[2, 0]]), ints([70]))
+    want_pool = R.Pool.of(cache)
+    ts.ts_cache_evict(cache, ints([[2, 0]]), ints([71]), 71, ints([[1]]), 40, 5, 5)
+    R.evict(want_pool, [[2, 0]], [71], [[1]], 40, 5, 5)
+    for name in ("k", "v"):
+        assert R.same_values(getattr(cache, name).view(torch.uint8).cpu().numpy(), getattr(want_pool, name))
+        np.testing.assert_array_equal(getattr(cache, name + "_exp").cpu().numpy(), getattr(want_pool, name + "_exp"))
