@@ -39,6 +39,11 @@ __device__ __forceinline__ float scale_of(unsigned exp, bool bad) {
   return __uint_as_float((bad ? 255u : exp) << 23);
 }
 
+// A page's exponent `down` lower.  Values are widened to 2^-down of their size, and a row's sums scaled back with the division:
+// products of the largest values with weights of 1 and less, added up over a row's keys, would pass the largest float.
+// The smallest element of a page, 2^-109, stays a normal bfloat16 up to 17.
+__device__ __forceinline__ unsigned value_exp(unsigned exp, unsigned down) { return exp < 255 ? max(exp, down) - down : exp; }
+
 // Four e4m3 bytes as four bfloat16, times the scale's power of two (exact for the exponents that this
 // library writes: e4m3 has 4 significant bits, and 2^-9 2^-100 is a normal bfloat16).
 __device__ __forceinline__ bf16x4 widen4(unsigned x, float scale) {
@@ -128,6 +133,8 @@ struct RowArgs {
 // or the part of it that a share of the work has (part_o[slots][256], kTileRows rows each).
 enum Out { kResult, kSlab, kSlot };
 
+constexpr float kPartDown = 1.0f / 1024;  // of up to that many parts: their sum stays below the largest float
+
 // The 8 channels from `ch` on of a row whose n parts lie at rows part(0) .. part(n - 1) of part_o and part_lse:
 // O = sum_i exp(lse_i - lse) O_i with lse = ln sum_i exp(lse_i), kBatch parts loaded at once.
 template <int D, int kBatch, typename Part>
@@ -155,11 +162,12 @@ __device__ __forceinline__ void join_parts(const RowArgs& a, int n, Part&& part,
       const bool none = e[k] == -INFINITY;  // a part without keys has no O
       const float w = none ? 0.0f : e[k] == big ? 1.0f : __builtin_amdgcn_exp2f((e[k] - big) * kLog2e);
       sum += w;
+      const float f = w * kPartDown;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) x[c] += none ? 0.0f : w * px[k][c], y[c] += none ? 0.0f : w * py[k][c];
+      for (int c = 0; c < 4; ++c) x[c] += none ? 0.0f : f * px[k][c], y[c] += none ? 0.0f : f * py[k][c];
     }
   }
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / (sum * kPartDown);
   bf16x8 r;
 #pragma unroll
   for (int c = 0; c < 4; ++c) r[c] = (__bf16)(x[c] * inv), r[4 + c] = (__bf16)(y[c] * inv);

@@ -48,6 +48,8 @@ struct RowGeo {
   static constexpr int kCh = D / (4 * kW) < 4 ? 4 : D / (4 * kW);
 };
 
+constexpr int kRowsDown = 17;  // value_exp: sums of weights of up to 1, of 2^17 keys
+
 // f over the lanes that differ in bits 4 and 5.
 template <typename F>
 __device__ __forceinline__ float across(float x, F&& f) {
@@ -99,6 +101,7 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
     kexp = a.pool.k_exp[(int64_t)id * H + h];
     vexp = a.pool.v_exp[(int64_t)id * H + h];
     if (bad) kexp = vexp = 255;  // reads as NaN
+    vexp = value_exp(vexp, kRowsDown);
   };
   typedef u32x4 Keys[4][kKLoads];
   const int koff = i16 * D + D / 4 * g;
@@ -262,7 +265,7 @@ __device__ __forceinline__ void rows_item(const RowArgs& a, const Session& se, c
 #pragma unroll
       for (int x = 0; x < kCh / 4; ++x) acc[x] += f * *(const lds_f32x4*)(obuf + (w * 16 + orow) * D + och + 4 * x);
     }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float inv = sum == 0.0f ? 0.0f : (float)(1 << kRowsDown) / sum;
     const float lse = sum == 0.0f ? -INFINITY : (big + __builtin_amdgcn_logf(sum)) * kLn2;
     const int64_t at = row_of(se, r, h, H, G);
     if (kOut == kSlab || (kOut == kSlot && to >= 0)) {

@@ -112,6 +112,7 @@ struct NoHook {
 // at 15, 2^-21 (of numbers around 39 it is 2^-19), which the log-sum-exp shows, and products with the smallest values that
 // a page holds, 2^-109, stay normal numbers.
 constexpr float kTileBias = 15.0f;
+constexpr int kTileDown = 4;  // value_exp: beside the bias, for rows of 2^19 keys
 enum TilePlace { kFirst = 0, kInner = 1, kLast = 2 };
 
 // The online softmax of one tile, as softmax_tile of attn_kernels.hip: the running maximum stays while the weights of
@@ -169,7 +170,7 @@ __device__ __forceinline__ void write_rows(const TileItem& it, const RowArgs& a,
                                            float l, float m_c, int q0, lds_char* stage, int lane) {
   using G = Geo<D>;
   const int col = lane & 31, hb = lane >> 5, H = a.pool.H;
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const float inv = l == 0.0f ? 0.0f : (float)(1 << kTileDown) / l;
   const int orow = lane >> 3, ochunk = lane & 7;
   lds_char* const put = stage + col * G::kORow;
   const lds_char* const get = stage + orow * G::kORow + ochunk * 16;
@@ -250,7 +251,7 @@ __device__ __forceinline__ void run_tile_group(const TileItem& it, const RowArgs
   auto put_entry = [&](int i, int id) {
     const bool bad = (unsigned)id >= (unsigned)a.pool.pages;
     const unsigned e = exps[(int64_t)(bad ? 0 : id) * H + it.h];
-    const unsigned scale = (bad ? 255u : first + i < pages ? e : 127u) << 23;
+    const unsigned exp = bad ? 255u : first + i < pages ? e : 127u, scale = (kGroupB ? value_exp(exp, kTileDown) : exp) << 23;
     *(lds_entry*)(list + (i & (T::kEntries - 1)) * 8) = u32x2{bad ? 0u : (unsigned)id, scale};
   };
   {

@@ -228,3 +228,18 @@ def test_append_and_evict_of_the_largest_magnitudes():
     for name in ("k", "v"):
         assert R.same_values(getattr(cache, name).view(torch.uint8).cpu().numpy(), getattr(want_pool, name))
         np.testing.assert_array_equal(getattr(cache, name + "_exp").cpu().numpy(), getattr(want_pool, name + "_exp"))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows,n,splits", [(1, 5000, 1), (3, 5000, 0), (40, 900, 3), (300, 5000, 1), (300, 3000, 5)])
+def test_attn_of_the_largest_values(rows, n, splits, d):
+    """Values of the largest size that a page holds, the same for every token: O is that value, whatever the number of tokens
+    whose products are added up on the way to it."""
+    v = torch.full((n, 1, d), 240 * 2.0 ** 120)
+    v[:, :, 1::2] *= -1
+    cache, table = filled(gen(n), [n], 1, d, k=0.1, v=v.bfloat16().cuda())
+    q = normal(gen(rows), rows, 1, d).bfloat16()
+    o = ts.ts_cache_attn(q, cache, ints([0, rows]), rows, ints(table), ints([n]), n, num_splits=splits)
+    want = v[:1].bfloat16().cuda().expand_as(o)
+    # sums of up to n weights, each rounded to 2^-8 of itself, over their fp32 sum
+    assert torch.isfinite(o).all() and ((o.double() / want.double()) - 1).abs().max() <= 2 * 2.0 ** -8
