@@ -1,6 +1,8 @@
 // cache_device.h -- device code shared by the session cache's kernels: sessions, pages and the 8-bit format.
 #pragma once
+#include <float.h>
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 #include "attn_tile.h"
@@ -113,6 +115,9 @@ __device__ __forceinline__ int64_t row_of(const Session& se, int r, int h, int H
   return ((int64_t)se.q0 + t) * (H * G) + h * G + (r - t * G);
 }
 
+// |scale| log2(e); of the largest scales the largest float, since infinity times a score of 0 would be NaN.
+inline float log2_scale(float scale) { return fminf(fabsf(scale) * kLog2e, FLT_MAX); }
+
 // What the attention kernels take.
 struct RowArgs {
   Pool pool;
@@ -125,7 +130,7 @@ struct RowArgs {
   int G, n_split;
   int shares;     // equal shares of the work (cache_tiles_kernel), or 0
   int tiles;      // row tiles of a session at most (cache_rows_kernel)
-  float c;        // |scale| log2(e)
+  float c;        // log2_scale
   unsigned flip;  // sign bits of Q to invert (negative scales)
 };
 

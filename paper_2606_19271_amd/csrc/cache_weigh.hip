@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(256) cache_weigh_rows_kernel(Pool pool, Sessio
 // host-side launcher
 
 hipError_t launch_weigh(const WeighArgs& a, hipStream_t st) {
-  const float c = fabsf(a.scale) * kLog2e;
+  const float c = log2_scale(a.scale);
   const unsigned flip = a.scale < 0.0f ? 0x80008000u : 0u;
   if (const int split = weigh_rows(a.ss.nseq, a.ss.max_rows, a.ss.max_len, a.pool.H, a.G, a.cus)) {
     const int64_t rows = (int64_t)a.ss.max_rows * a.G;

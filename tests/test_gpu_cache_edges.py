@@ -243,3 +243,22 @@ def test_attn_of_the_largest_values(rows, n, splits, d):
     want = v[:1].bfloat16().cuda().expand_as(o)
     # sums of up to n weights, each rounded to 2^-8 of itself, over their fp32 sum
     assert torch.isfinite(o).all() and ((o.double() / want.double()) - 1).abs().max() <= 2 * 2.0 ** -8
+
+
+@pytest.mark.parametrize("rows", [5, 90])
+@pytest.mark.parametrize("scale", [3.4e38, -3.4e38, 1e-45])
+def test_scales_at_the_ends_of_float32(scale, rows):
+    """Any finite scale: queries of zeros have equal weights for every token, by the formula."""
+    d, n = 64, 300
+    cache, table = filled(gen(rows), [n], 1, d)
+    q = torch.zeros(rows, 1, d, dtype=torch.bfloat16, device="cuda")
+    args = (ints([0, rows]), rows, ints(table), ints([n]), n)
+    o, lse = ts.ts_cache_attn(q, cache, *args, scale=scale, return_lse=True)
+    pool = R.Pool.of(cache)
+    v = pool.tokens("v", table[0], n, 0)
+    # (weights of equal powers of two: exact; fp32 sums, and a rounding of the result)
+    assert np.all(np.abs(o.double().cpu().numpy()[:, 0] - v.mean(0)) <= 2.0 ** -8 * np.abs(v.mean(0)) + 2.0 ** -20 * np.abs(v).mean(0))
+    assert (lse.double() - math.log(n)).abs().max() <= 2.0 ** -22 * math.log(n)
+    w = ts.ts_cache_weigh(q, lse, cache, *args, scale=scale, out=torch.zeros_like(cache.weight))
+    got = torch.cat([w[p, 0] for p in table[0]])[:n]
+    assert (got - rows / n).abs().max() <= 1e-5 * rows / n
