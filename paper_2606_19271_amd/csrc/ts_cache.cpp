@@ -27,7 +27,7 @@ struct DeviceState {
   std::once_flag once;
   std::atomic<bool> set_up{false};  // init_device has run (whatever its outcome)
   int status = TS_ERR_UNSUPPORTED;
-  int cus = 256;
+  std::atomic<int32_t> cus{0};  // compute units, or 0: not asked for yet
 };
 
 DeviceState g_dev[kMaxDevices];
@@ -49,6 +49,25 @@ bool capturing(hipStream_t s) {
     return false;
   }
   return cs != hipStreamCaptureStatusNone;
+}
+
+// Compute units of the calling thread's current device, or 0.  Sets nothing up, so that it can be asked while a stream is
+// being captured, the device's first call or not.
+int32_t current_cus() {
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) {
+    (void)hipGetLastError();
+    return 0;
+  }
+  int n = g_dev[dev].cus.load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) {
+      (void)hipGetLastError();
+      return 0;
+    }
+    g_dev[dev].cus.store(n, std::memory_order_relaxed);
+  }
+  return n;
 }
 
 // The calling thread's current device, initialised once, never under stream capture.
@@ -268,13 +287,8 @@ int64_t ts_cache_attn_workspace(int32_t nseq, int32_t max_rows, int32_t max_len,
       (d != 64 && d != 128) || num_splits < 0 || num_splits > TS_CACHE_MAX_SPLITS)
     return 0;
   if ((int64_t)max_rows + 256 > (kByteLimit - 1) / ((int64_t)Hq * d * 2)) return 0;
-  int rc = TS_OK;
-  int32_t cus = 256;
-  if (num_splits == 0) {
-    DeviceState* st = current_device(&rc, nullptr);
-    if (!st) return 0;
-    cus = st->cus;
-  }
+  const int32_t cus = num_splits == 0 ? current_cus() : 1;  // (forced ranges are the same on any device)
+  if (cus == 0) return 0;
   const tscache::Sessions ss{nullptr, nullptr, nullptr, nseq, 0, max_rows, max_len, total};
   const int tile = tscache::row_tile((int64_t)max_rows * (Hq / H), 1.0f);
   return tscache::attn_parts(ss, H, Hq / H, d, tile, num_splits, INT64_MAX, cus).bytes;

@@ -2,6 +2,9 @@
 other, rows that one key dominates, the log-sum-exp's last bits, the ends of the number formats, what is not finite, and
 work that is dealt out in equal shares."""
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -14,6 +17,7 @@ pytestmark = pytest.mark.gpu
 ts = pytest.importorskip("paper_2606_19271_amd")
 
 PAGE = 64
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -262,3 +266,41 @@ def test_scales_at_the_ends_of_float32(scale, rows):
     w = ts.ts_cache_weigh(q, lse, cache, *args, scale=scale, out=torch.zeros_like(cache.weight))
     got = torch.cat([w[p, 0] for p in table[0]])[:n]
     assert (got - rows / n).abs().max() <= 1e-5 * rows / n
+
+
+# ---- a process's first call
+
+FIRST = r"""
+import sys; sys.path.insert(0, %r)
+import torch
+import paper_2606_19271_amd as ts
+from paper_2606_19271_amd import _lib
+cache = ts.session_cache(40, 2, 64)
+cache.k.view(torch.uint8).random_(0, 100); cache.v.view(torch.uint8).random_(0, 100)
+cache.k_exp.fill_(120); cache.v_exp.fill_(120)
+ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+args = (torch.randn(300, 2, 64, device="cuda").bfloat16(), cache, ints([0, 300]), 300, ints([list(range(40))]), ints([2500]), 2560)
+x = torch.zeros(4, device="cuda") + 1
+torch.cuda.synchronize()
+graph, status = torch.cuda.CUDAGraph(), None
+with torch.cuda.graph(graph):
+    x.add_(1)
+    try:
+        ts.ts_cache_attn(*args)
+    except ts.TsAttnError as e:
+        status = e.status
+print("status", status == _lib.TS_ERR_CAPTURE, flush=True)
+want = ts.ts_cache_attn(*args)
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    got = ts.ts_cache_attn(*args)
+graph.replay()
+torch.cuda.synchronize()
+print("same", torch.equal(got.view(torch.int16), want.view(torch.int16)), flush=True)
+"""
+
+
+def test_a_process_s_first_call_under_capture_is_refused():
+    """And leaves the capture usable; after a call outside capture, one under it is recorded."""
+    r = subprocess.run([sys.executable, "-c", FIRST % ROOT], capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0 and "status True" in r.stdout and "same True" in r.stdout, r.stdout + r.stderr
