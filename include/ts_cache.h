@@ -93,8 +93,9 @@ int ts_cache_append(const ts_cache* cache, const void* k, const void* v, const i
  *  workspace   (DEVICE, 256-byte aligned, of this call alone until it is done): ts_cache_attn_workspace
  *              bytes.  With num_splits = 0 a smaller one, or NULL, divides less or not at all; a forced n
  *              that does not fit returns TS_ERR_SCRATCH.
- * The bits of a session's result depend on how its keys are divided: with num_splits = 0 on the call's
- * sizes and the other sessions' too, with n >= 1 on its own length alone.
+ * The bits of a session's result depend on how its keys are divided, with num_splits = 0 on the call's
+ * sizes and the other sessions' too; with n >= 1 on the session's own rows and length, on max_rows * G
+ * (up to 16, up to 64, or more: another kernel each), and on whether scale is 0.
  * o, lse and workspace must not overlap each other or any input (TS_ERR_ALIAS).
  */
 #define TS_CACHE_MAX_SPLITS 64

@@ -304,3 +304,23 @@ def test_a_process_s_first_call_under_capture_is_refused():
     """And leaves the capture usable; after a call outside capture, one under it is recorded."""
     r = subprocess.run([sys.executable, "-c", FIRST % ROOT], capture_output=True, text=True, timeout=100)
     assert r.returncode == 0 and "status True" in r.stdout and "same True" in r.stdout, r.stdout + r.stderr
+
+
+# ---- what a session's bits depend on
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows", [[3, 16, 1], [20, 17, 64], [300, 70, 129]])
+@pytest.mark.parametrize("splits", [1, 3])
+def test_a_session_s_bits_with_forced_ranges(rows, splits, d):
+    """Alone, with its own rows as the most, and in a batch whose most is of the same kind (up to 16, up to 64, more): the same."""
+    g = gen(sum(rows) + splits)
+    H, lens = 2, [900, 333, 2000]
+    cache, table = filled(g, lens, H, d)
+    cu = [0] + np.cumsum(rows).tolist()
+    q = normal(g, cu[-1], H, d).bfloat16()
+    o, lse = ts.ts_cache_attn(q, cache, ints(cu), max(rows), ints(table), ints(lens), 2000, return_lse=True, num_splits=splits)
+    for s, n in enumerate(rows):
+        r = slice(cu[s], cu[s + 1])
+        alone = ts.ts_cache_attn(q[r].contiguous(), cache, ints([0, n]), n, ints(table[s:s + 1]), ints(lens[s:s + 1]), lens[s],
+                                 return_lse=True, num_splits=splits)
+        assert same(alone, [o[r], lse[r]]), s
