@@ -324,3 +324,114 @@ def test_a_session_s_bits_with_forced_ranges(rows, splits, d):
         alone = ts.ts_cache_attn(q[r].contiguous(), cache, ints([0, n]), n, ints(table[s:s + 1]), ints(lens[s:s + 1]), lens[s],
                                  return_lse=True, num_splits=splits)
         assert same(alone, [o[r], lse[r]]), s
+
+
+# ---- what is not finite
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows,splits", [(3, 0), (40, 2), (70, 1), (300, 1), (300, 3)])
+def test_attn_of_queries_that_are_not_finite(rows, splits, d):
+    """A query of NaN or infinities makes its own row NaN and no other: the rows beside it stay within a rounding of the weights
+    and one of the result (2^-8 of the values each) of what they are without it."""
+    g = gen(rows + d)
+    H, n = 2, 900
+    cache, table = filled(g, [n], H, d)
+    q = normal(g, rows, H, d).bfloat16()
+    args = (cache, ints([0, rows]), rows, ints(table), ints([n]), n)
+    o, lse = ts.ts_cache_attn(q, *args, return_lse=True, num_splits=splits)
+    bad = q.clone()
+    bad[0, 0, 3], bad[rows // 2, 1, 0], bad[rows - 1, 0, d - 1] = math.nan, math.inf, -math.inf
+    o2, lse2 = ts.ts_cache_attn(bad, *args, return_lse=True, num_splits=splits)
+    hit = torch.zeros(rows, H, dtype=torch.bool, device="cuda")
+    hit[0, 0] = hit[rows // 2, 1] = hit[rows - 1, 0] = True
+    assert torch.isnan(o2[hit]).all() and torch.isnan(lse2[hit]).all()
+    assert (o2[~hit].float() - o[~hit].float()).abs().max() <= 4 * 2.0 ** -8 * 6
+    assert (lse2[~hit] - lse[~hit]).abs().max() <= 1e-4
+
+
+# ---- equal shares of the work
+
+def shares_of(rows, lens, H, G, d):
+    """The number of equal shares that the library deals this call out in (by its workspace: two slots of 256 rows to a share),
+    or 0."""
+    total = sum(rows)
+    need = ts.load_cache().ts_cache_attn_workspace(len(rows), max(rows), max(lens), total, H, H * G, d, 0)
+    for n in range(2, 1025):
+        slots = 2 * n * 256 * 4
+        if need == slots + 2 * n * 256 * d * 4:
+            return n
+    return 0
+
+
+SHARED = dict(H=32, rows=[280, 90, 300, 257], lens=[9000, 2000, 5000, 6001])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_shares_with_bad_sessions_and_pages(d):
+    """Sessions that break the rules leave their rows, also between two that are cut; a page outside the pool inside a cut item
+    makes its session NaN; the others are what they are alone."""
+    g = gen(d)
+    H, rows, lens = SHARED["H"], SHARED["rows"] + [70, 0], SHARED["lens"] + [300, 77]
+    assert shares_of(rows, lens, H, 1, d) > 1
+    cu = [0] + np.cumsum(rows).tolist()
+    cache, table = filled(g, lens, H, d, spare=1)
+    stated = list(lens)
+    stated[1] = 9001  # longer than the most that is stated
+    stated[4] = -1
+    table[2][40] = 1 << 29
+    q = normal(g, cu[-1], H, d).bfloat16()
+    out, lse = torch.full_like(q, 7.0), torch.full((cu[-1], H), 7.0, device="cuda")
+    ts.ts_cache_attn(q, cache, ints(cu), max(rows), ints(table), ints(stated), 9000, out=out, lse=lse)
+    for s, n in enumerate(rows):
+        r = slice(cu[s], cu[s + 1])
+        if s in (1, 4):
+            assert torch.all(out[r] == 7.0) and torch.all(lse[r] == 7.0)
+        elif s == 2:
+            assert torch.isnan(out[r]).all() and torch.isnan(lse[r]).all()
+        elif n:
+            o, l = ts.ts_cache_attn(q[r].contiguous(), cache, ints([0, n]), n, ints(table[s:s + 1]), ints(lens[s:s + 1]), lens[s], return_lse=True,
+                                    num_splits=1)
+            # two results, each off by a rounding of the weights and one of the result: 2^-8 of an average of the values' sizes each
+            assert (out[r].float() - o.float()).abs().max() <= 4 * 2.0 ** -8 * 6
+            assert (lse[r] - l).abs().max() <= 1e-4
+
+
+def shared_step(g, d):
+    H, rows, lens = SHARED["H"], SHARED["rows"], SHARED["lens"]
+    assert shares_of(rows, lens, H, 1, d) > 1
+    cache, table = filled(g, lens, H, d)
+    cu = [0] + np.cumsum(rows).tolist()
+    return normal(g, cu[-1], H, d).bfloat16(), (cache, ints(cu), max(rows), ints(table), ints(lens), max(lens))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_shares_in_a_graph(d):
+    g = gen(20 + d)
+    q, args = shared_step(g, d)
+    ts.ts_cache_attn(q, *args)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = ts.ts_cache_attn(q, *args, return_lse=True)
+    for i in range(4):
+        q.copy_(normal(g, *q.shape).bfloat16())
+        want = ts.ts_cache_attn(q, *args, return_lse=True)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(got, want), i
+
+
+def test_shares_on_two_streams():
+    g = gen(30)
+    steps = [shared_step(g, 128), shared_step(g, 64)]
+    want = [ts.ts_cache_attn(q, *args, return_lse=True) for q, args in steps]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in steps], []
+    for _ in range(4):
+        for i, (q, args) in enumerate(steps):
+            with torch.cuda.stream(streams[i]):
+                got.append((i, ts.ts_cache_attn(q, *args, return_lse=True)))
+    torch.cuda.synchronize()
+    for i, r in got:
+        assert same(r, want[i])
