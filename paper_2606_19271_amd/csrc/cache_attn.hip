@@ -68,9 +68,9 @@ static void launch_rows(const RowArgs& r, int tile, unsigned grid, hipStream_t s
 template <int D>
 static hipError_t launch_attn_d(const AttnArgs& a, hipStream_t st) {
   const int64_t rows = (int64_t)a.ss.max_rows * a.G;
-  const int tile = row_tile(rows, a.scale);
+  const int tile = a.tile;
   RowArgs r{a.pool, a.ss, (const __bf16*)a.q, (__bf16*)a.o, a.lse, a.part_o, a.part_lse, a.G, a.n_split, a.shares,
-            (int)((rows + tile - 1) / tile), log2_scale(a.scale), a.scale < 0.0f ? 0x80008000u : 0u};
+            (int)((rows + tile - 1) / tile), tile == kTileRows && rows <= 64, log2_scale(a.scale), a.scale < 0.0f ? 0x80008000u : 0u};
   const int64_t items = attn_items(a.ss.nseq, a.ss.max_rows, a.ss.total, a.pool.H, a.G, tile) * a.n_split;
   if (tile == kTileRows) launch_tiles(r, D, items, st);
   else if (a.n_split > 1) launch_rows<D, kSlab>(r, tile, (unsigned)items, st);

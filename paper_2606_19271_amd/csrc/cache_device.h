@@ -130,6 +130,7 @@ struct RowArgs {
   int G, n_split;
   int shares;     // equal shares of the work (cache_tiles_kernel), or 0
   int tiles;      // row tiles of a session at most (cache_rows_kernel)
+  bool few;       // up to 64 rows in 256-row tiles (call_tile)
   float c;        // log2_scale
   unsigned flip;  // sign bits of Q to invert (negative scales)
 };

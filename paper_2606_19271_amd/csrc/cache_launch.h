@@ -37,7 +37,7 @@ struct AttnArgs {
   float* lse;       // or null
   float* part_o;    // [n_split][total][Hq][d] (n_split > 1), [2 shares][256][d] (shares > 0)
   float* part_lse;  // the same without d
-  int32_t d, G, n_split, shares;
+  int32_t d, G, tile, n_split, shares;
   float scale;
 };
 
@@ -75,6 +75,7 @@ struct EvictArgs {
 // (cache_rows_kernel).
 constexpr int kTileRows = 256;
 int row_tile(int64_t rows, float scale);
+int call_tile(int32_t nseq, int64_t rows, int32_t max_len, int32_t H, int32_t d, float scale, int32_t num_splits);
 // Workgroups of an unsplit attention call, and of its merge kernel.
 int64_t attn_items(int32_t nseq, int32_t max_rows, int32_t total, int32_t H, int32_t G, int tile);
 int64_t merge_blocks(int32_t nseq, int32_t max_rows, int32_t Hq, int32_t d);

@@ -13,11 +13,26 @@ int64_t ceil_div(int64_t a, int64_t b) { return a / b + (a % b != 0); }
 }  // namespace
 
 // Up to 64 rows two tiles of 32, which read the pages twice, cost less than one of 256 with a quarter of its waves at work:
-// 32 sessions of 16384 keys x 8 heads x 64 rows, d = 128, 307 against 449 us, 8 of 8192 keys x 40 heads 208 against 302, at d = 64 122
-// against 178; one session of 32760 keys x 12 heads 59 against 52.  With 96 rows and three tiles the large one is ahead.
+// 32 sessions of 16384 keys x 8 heads x 64 rows, d = 128, 307 against 419 us, 8 of 8192 keys x 40 heads 208 against 282, at d = 64 122
+// against 143 (but see call_tile).  With 96 rows and three tiles the large one is ahead.
 // Scale 0 is left to the row kernel: with a factor of 0 the tile kernel's masked scores would not vanish.
 int row_tile(int64_t rows, float scale) {
   return rows <= 16 ? 16 : rows <= 64 || scale == 0.0f ? 32 : kTileRows;
+}
+
+// 33 to 64 rows that the library divides as it likes: where a few heads' keys are enough for a key range to each CU and no more,
+// the ranges of 256-row tiles are fewer and longer than the row kernel's, and the pages are read once.  Both sides, us, row kernel
+// against large tiles, 64 rows, d = 128 (d = 64): 12 heads x 4096 keys 23 / 20 (19 / 19), 12 x 16384 44 / 32 (31 / 25), 12 x 32768 56 / 50 (39 / 36),
+// 40 x 4096 39 / 26 (26 / 21), 80 x 2048 39 / 27 (25 / 21), 96 x 4096 53 / 50 (34 / 36).  Less work than that ends together (12 x 2048 19 / 19,
+// 40 x 512 14 / 16); more is bound by reading, where row tiles of every session go better together (48 x 16384 76 / 83,
+// 24 x 32768 76 / 84, 128 x 2048 44 / 46); and few heads of long sessions have too few ranges (8 x 32768 47 / 59).
+int call_tile(int32_t nseq, int64_t rows, int32_t max_len, int32_t H, int32_t d, float scale, int32_t num_splits) {
+  const int tile = row_tile(rows, scale);
+  const int64_t heads = (int64_t)nseq * H;
+  if (num_splits != 0 || tile == kTileRows || scale == 0.0f || rows <= 32) return tile;
+  if (heads < 8 || heads > (d == 64 ? 48 : 96) || max_len <= 768 || max_len > 2800 * heads) return tile;
+  const int64_t keys = heads * max_len;
+  return keys >= (d == 64 ? 90000 : 45000) && keys <= 400000 ? kTileRows : tile;
 }
 
 int64_t attn_items(int32_t nseq, int32_t max_rows, int32_t total, int32_t H, int32_t G, int tile) {

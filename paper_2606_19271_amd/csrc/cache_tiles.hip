@@ -534,10 +534,12 @@ __device__ __forceinline__ bool find_item(const RowArgs& a, int64_t at, TileItem
   return true;
 }
 
-// A last tile of at most twice this many rows is shared by the eight waves, each taking pages of its own (rows_item): in
+// A last tile of at most twice kThinRows rows is shared by the eight waves, each taking pages of its own (rows_item): in
 // the schedule above one wave would work and seven keep its barriers, for three quarters of a full tile's time (32768
 // keys, d = 128: 201 us for 24 rows this way, 566 for 100, 710 for 256); six sessions of 16384 keys x 300 rows x 12 heads take
-// 258 us, and 318 with their 44 rows in the schedule above.
+// 258 us, and 318 with their 44 rows in the schedule above.  Calls of up to 64 rows that come here at all (call_tile) do so for that
+// schedule, in a kernel of their own whose thin tiles (kThin) end at kThinRows: as an argument the limit costs the other
+// calls up to 4 %.
 constexpr int kThinRows = 32;
 
 template <int D>
@@ -713,11 +715,11 @@ __device__ __forceinline__ void run_thin(const TileItem& it, const RowArgs& a, c
   }
 }
 
-template <int D, Mode kMode>
+template <int D, Mode kMode, int kThin>
 __device__ __forceinline__ void run_item(const TileItem& it, const RowArgs& a, char* smem) {
   const int wave = __builtin_amdgcn_readfirstlane(thread_anew() >> 6);
   if (it.ntiles <= 0) return run_empty<D, kMode>(it, a);
-  if (it.rows - it.row0 <= 2 * kThinRows) return run_thin<D, kMode>(it, a, smem);
+  if (it.rows - it.row0 <= kThin) return run_thin<D, kMode>(it, a, smem);
   const bool active = it.row0 + 32 * wave < it.rows;
   if (wave >= kWaves / 2) {
     if (active) run_tile_group<D, true, kMode, true>(it, a, smem);
@@ -728,7 +730,7 @@ __device__ __forceinline__ void run_item(const TileItem& it, const RowArgs& a, c
   }
 }
 
-template <int D, Mode kMode>
+template <int D, Mode kMode, int kThin = 2 * kThinRows>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 cache_tiles_kernel(RowArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -737,7 +739,7 @@ cache_tiles_kernel(RowArgs a) {
     const bool back = crossed(a.ss);  // (asked for with the sessions, looked at behind them)
     if (!find_item<D>(a, blockIdx.x >> 3, &it)) return;
     const bool more = __builtin_amdgcn_ballot_w64(back) != 0;
-    run_item<D, kMode>(it, a, smem);
+    run_item<D, kMode, kThin>(it, a, smem);
     if (!more) return;
     // The items that are left where sessions share rows, by the thin path whatever their rows: run_item in a loop would have
     // the registers of every call's items hold what the next one needs (4680 rows x 32760 keys x 40 heads, d = 128: 3030
@@ -792,7 +794,7 @@ cache_tiles_kernel(RowArgs a) {
     else next_item(p, nq, b.pool.H);
     __syncthreads();  // every wave has read the state
     if (threadIdx.x == 0) state[0] = p.s, state[1] = p.h, state[2] = p.tile, state[3] = p.t;
-    if (!none) run_item<D, kEven>(it, b, smem);
+    if (!none) run_item<D, kEven, kThin>(it, b, smem);
   }
 }
 
@@ -832,7 +834,7 @@ __global__ void __launch_bounds__(kMergeThreads) cache_join_kernel(RowArgs a) {
 template <int D>
 static hipError_t configure_d() {
   const void* const all[] = {(const void*)cache_tiles_kernel<D, kWhole>, (const void*)cache_tiles_kernel<D, kSplit>,
-                             (const void*)cache_tiles_kernel<D, kEven>};
+                             (const void*)cache_tiles_kernel<D, kEven>, (const void*)cache_tiles_kernel<D, kSplit, kThinRows>};
   for (const void* kern : all) {
     const hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, tiles_lds<D>() + kStateBytes);
     if (e != hipSuccess) return e;
@@ -853,7 +855,7 @@ static void launch_tiles_d(const RowArgs& r, int64_t items, hipStream_t st) {
     return;
   }
   const unsigned grid = (unsigned)((items + 7) / 8 * 8);  // every XCD has up to ceil(items / 8)
-  auto kern = r.n_split > 1 ? cache_tiles_kernel<D, kSplit> : cache_tiles_kernel<D, kWhole>;
+  auto kern = r.n_split == 1 ? cache_tiles_kernel<D, kWhole> : r.few ? cache_tiles_kernel<D, kSplit, kThinRows> : cache_tiles_kernel<D, kSplit>;
   hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), tiles_lds<D>(), st, r);
 }
 

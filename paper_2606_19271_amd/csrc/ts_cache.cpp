@@ -243,7 +243,7 @@ int ts_cache_attn(const ts_cache* cache, const void* q, void* o, float* lse, con
   rc = check_sessions(cache, nseq, width, max_rows, max_len, total, Hq);
   if (rc != TS_OK) return rc;
   const int32_t G = Hq / cache->H;
-  const int tile = tscache::row_tile((int64_t)max_rows * G, scale);
+  const int tile = tscache::call_tile(nseq, (int64_t)max_rows * G, max_len, cache->H, cache->d, scale, num_splits);
   if (tscache::attn_items(nseq, max_rows, total, cache->H, G, tile) * std::max(1, num_splits) >= tscache::kGridLimit ||
       tscache::merge_blocks(nseq, max_rows, Hq, cache->d) >= tscache::kGridLimit)
     return TS_ERR_SHAPE;
@@ -274,7 +274,7 @@ int ts_cache_attn(const ts_cache* cache, const void* q, void* o, float* lse, con
   if (!st) return rc;
   const tscache::Parts parts = parts_on(st->cus);
   const tscache::AttnArgs a{pool_of(cache), ss, q, o, lse, (float*)((char*)workspace + parts.o_offset), (float*)workspace,
-                            cache->d, G, parts.n_split, parts.shares, scale};
+                            cache->d, G, tile, parts.n_split, parts.shares, scale};
   if (validate_mode() && !capturing(s) &&
       (rc = validate(a.ss, cache->pages, false, nullptr, 0, 0, s)) != TS_OK)
     return rc;
@@ -290,7 +290,7 @@ int64_t ts_cache_attn_workspace(int32_t nseq, int32_t max_rows, int32_t max_len,
   const int32_t cus = num_splits == 0 ? current_cus() : 1;  // (forced ranges are the same on any device)
   if (cus == 0) return 0;
   const tscache::Sessions ss{nullptr, nullptr, nullptr, nseq, 0, max_rows, max_len, total};
-  const int tile = tscache::row_tile((int64_t)max_rows * (Hq / H), 1.0f);
+  const int tile = tscache::call_tile(nseq, (int64_t)max_rows * (Hq / H), max_len, H, d, 1.0f, num_splits);
   return tscache::attn_parts(ss, H, Hq / H, d, tile, num_splits, INT64_MAX, cus).bytes;
 }
 

@@ -249,25 +249,6 @@ def test_attn_of_the_largest_values(rows, n, splits, d):
     assert torch.isfinite(o).all() and ((o.double() / want.double()) - 1).abs().max() <= 2 * 2.0 ** -8
 
 
-@pytest.mark.parametrize("rows", [5, 90])
-@pytest.mark.parametrize("scale", [3.4e38, -3.4e38, 1e-45])
-def test_scales_at_the_ends_of_float32(scale, rows):
-    """Any finite scale: queries of zeros have equal weights for every token, by the formula."""
-    d, n = 64, 300
-    cache, table = filled(gen(rows), [n], 1, d)
-    q = torch.zeros(rows, 1, d, dtype=torch.bfloat16, device="cuda")
-    args = (ints([0, rows]), rows, ints(table), ints([n]), n)
-    o, lse = ts.ts_cache_attn(q, cache, *args, scale=scale, return_lse=True)
-    pool = R.Pool.of(cache)
-    v = pool.tokens("v", table[0], n, 0)
-    # (weights of equal powers of two: exact; fp32 sums, and a rounding of the result)
-    assert np.all(np.abs(o.double().cpu().numpy()[:, 0] - v.mean(0)) <= 2.0 ** -8 * np.abs(v.mean(0)) + 2.0 ** -20 * np.abs(v).mean(0))
-    assert (lse.double() - math.log(n)).abs().max() <= 2.0 ** -22 * math.log(n)
-    w = ts.ts_cache_weigh(q, lse, cache, *args, scale=scale, out=torch.zeros_like(cache.weight))
-    got = torch.cat([w[p, 0] for p in table[0]])[:n]
-    assert (got - rows / n).abs().max() <= 1e-5 * rows / n
-
-
 # ---- a process's first call
 
 FIRST = r"""
@@ -324,6 +305,25 @@ def test_a_session_s_bits_with_forced_ranges(rows, splits, d):
         alone = ts.ts_cache_attn(q[r].contiguous(), cache, ints([0, n]), n, ints(table[s:s + 1]), ints(lens[s:s + 1]), lens[s],
                                  return_lse=True, num_splits=splits)
         assert same(alone, [o[r], lse[r]]), s
+
+
+@pytest.mark.parametrize("rows", [5, 90])
+@pytest.mark.parametrize("scale", [3.4e38, -3.4e38, 1e-45])
+def test_scales_at_the_ends_of_float32(scale, rows):
+    """Any finite scale: queries of zeros have equal weights for every token, by the formula."""
+    d, n = 64, 300
+    cache, table = filled(gen(rows), [n], 1, d)
+    q = torch.zeros(rows, 1, d, dtype=torch.bfloat16, device="cuda")
+    args = (ints([0, rows]), rows, ints(table), ints([n]), n)
+    o, lse = ts.ts_cache_attn(q, cache, *args, scale=scale, return_lse=True)
+    pool = R.Pool.of(cache)
+    v = pool.tokens("v", table[0], n, 0)
+    # (weights of equal powers of two: exact; fp32 sums, and a rounding of the result)
+    assert np.all(np.abs(o.double().cpu().numpy()[:, 0] - v.mean(0)) <= 2.0 ** -8 * np.abs(v.mean(0)) + 2.0 ** -20 * np.abs(v).mean(0))
+    assert (lse.double() - math.log(n)).abs().max() <= 2.0 ** -22 * math.log(n)
+    w = ts.ts_cache_weigh(q, lse, cache, *args, scale=scale, out=torch.zeros_like(cache.weight))
+    got = torch.cat([w[p, 0] for p in table[0]])[:n]
+    assert (got - rows / n).abs().max() <= 1e-5 * rows / n
 
 
 # ---- what is not finite
@@ -435,3 +435,25 @@ def test_shares_on_two_streams():
     torch.cuda.synchronize()
     for i, r in got:
         assert same(r, want[i])
+
+
+# ---- 33 to 64 rows of a cached head, where large row tiles take fewer and longer ranges of keys
+
+@pytest.mark.parametrize("d,H,G,rows,lens", [(128, 12, 1, [64], [8192]), (128, 6, 2, [20, 32], [8001, 7000]), (64, 12, 1, [64, 1], [8192, 100]),
+                                             (64, 24, 1, [40], [8000]), (128, 40, 1, [33], [4095])])
+def test_attn_of_up_to_64_rows_in_large_tiles(d, H, G, rows, lens):
+    """Against ranges of the row kernel, which forced ones are: two results, each off by a rounding of the weights and one of the
+    result, 2^-8 of an average of the values' sizes each."""
+    g = gen(d + H + rows[0])
+    cache, table = filled(g, lens, H, d)
+    cu = [0] + np.cumsum(rows).tolist()
+    q = normal(g, cu[-1], H * G, d).bfloat16()
+    # (the row kernel would take more than 16 ranges, large tiles take 16 at most)
+    ranges = ts.load_cache().ts_cache_attn_workspace(len(rows), max(rows), max(lens), cu[-1], H, H * G, d, 0) // (cu[-1] * H * G * 4 * (d + 1))
+    assert 1 < ranges <= 16
+    args = (q, cache, ints(cu), max(rows), ints(table), ints(lens), max(lens))
+    o, lse = ts.ts_cache_attn(*args, return_lse=True)
+    o2, lse2 = ts.ts_cache_attn(*args, return_lse=True, num_splits=5)
+    assert (o.float() - o2.float()).abs().max() <= 4 * 2.0 ** -8 * 6
+    assert (lse - lse2).abs().max() <= 1e-4
+    assert same(ts.ts_cache_attn(*args, return_lse=True), [o, lse])
