@@ -13,17 +13,16 @@
 #include <mutex>
 
 #include "attn_launch.h"
+#include "device_setup.h"
 
 namespace {
 
-constexpr int kMaxDevices = 64;
+using namespace tshost;
+
 constexpr int64_t kByteLimit = (int64_t)1 << 31;
 constexpr int64_t kGridLimit = (int64_t)1 << 23;  // workgroups per launch (x 512 threads < 2^32)
 
-struct DeviceState {
-  std::once_flag once;
-  std::atomic<bool> set_up{false};  // init_device has run (whatever its outcome)
-  int status = TS_ERR_UNSUPPORTED;  // TS_OK once the device is known to be usable
+struct DeviceState : DeviceSetup {
   int dev = -1;
   int xcd_chunk = 32;
   int cus = 256;
@@ -85,37 +84,7 @@ hipMemPool_t device_pool(DeviceState* st) {
   return st->pool;
 }
 
-// Whether stream s is recording a HIP graph.  A failed query (which leaves an error behind that
-// a later launch check would report) is cleared and read as "not capturing".
-bool capturing(hipStream_t s) {
-  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(s, &cs) != hipSuccess) {
-    (void)hipGetLastError();
-    return false;
-  }
-  return cs != hipStreamCaptureStatusNone;
-}
-
-// The calling thread's current device, initialised once -- never under stream capture, where
-// the set-up's pool creation and kernel attributes have no place (TS_ERR_CAPTURE).
-DeviceState* current_device(int* status, hipStream_t s) {
-  int dev = -1;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) {
-    *status = TS_ERR_UNSUPPORTED;
-    return nullptr;
-  }
-  DeviceState* st = &g_dev[dev];
-  if (!st->set_up.load(std::memory_order_acquire) && capturing(s)) {
-    *status = TS_ERR_CAPTURE;
-    return nullptr;
-  }
-  std::call_once(st->once, [dev, st] {
-    init_device(dev, st);
-    st->set_up.store(true, std::memory_order_release);
-  });
-  *status = st->status;
-  return st->status == TS_OK ? st : nullptr;
-}
+DeviceState* current_device(int* status, hipStream_t s) { return tshost::current_device(g_dev, init_device, status, s); }
 
 bool misaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
 

@@ -15,18 +15,17 @@
 #include <new>
 
 #include "cache_launch.h"
+#include "device_setup.h"
 
 namespace {
 
-constexpr int kMaxDevices = 64;
+using namespace tshost;
+
 constexpr int64_t kByteLimit = (int64_t)1 << 31;
 
 static_assert(tscache::kPage == TS_CACHE_PAGE, "page size");
 
-struct DeviceState {
-  std::once_flag once;
-  std::atomic<bool> set_up{false};  // init_device has run (whatever its outcome)
-  int status = TS_ERR_UNSUPPORTED;
+struct DeviceState : DeviceSetup {
   std::atomic<int32_t> cus{0};  // compute units, or 0: not asked for yet
 };
 
@@ -41,24 +40,11 @@ void init_device(int dev, DeviceState* st) {
   st->status = TS_OK;
 }
 
-// Whether stream s is recording a HIP graph (a failed query is cleared and read as "not capturing").
-bool capturing(hipStream_t s) {
-  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(s, &cs) != hipSuccess) {
-    (void)hipGetLastError();
-    return false;
-  }
-  return cs != hipStreamCaptureStatusNone;
-}
-
 // Compute units of the calling thread's current device, or 0.  Sets nothing up, so that it can be asked while a stream is
 // being captured, the device's first call or not.
 int32_t current_cus() {
-  int dev = -1;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) {
-    (void)hipGetLastError();
-    return 0;
-  }
+  const int dev = current_index();
+  if (dev < 0) return 0;
   int n = g_dev[dev].cus.load(std::memory_order_relaxed);
   if (n == 0) {
     if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) {
@@ -70,26 +56,7 @@ int32_t current_cus() {
   return n;
 }
 
-// The calling thread's current device, initialised once, never under stream capture.
-DeviceState* current_device(int* status, hipStream_t s) {
-  int dev = -1;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) {
-    (void)hipGetLastError();
-    *status = TS_ERR_UNSUPPORTED;
-    return nullptr;
-  }
-  DeviceState* st = &g_dev[dev];
-  if (!st->set_up.load(std::memory_order_acquire) && capturing(s)) {
-    *status = TS_ERR_CAPTURE;
-    return nullptr;
-  }
-  std::call_once(st->once, [dev, st] {
-    init_device(dev, st);
-    st->set_up.store(true, std::memory_order_release);
-  });
-  *status = st->status;
-  return st->status == TS_OK ? st : nullptr;
-}
+DeviceState* current_device(int* status, hipStream_t s) { return tshost::current_device(g_dev, init_device, status, s); }
 
 bool misaligned(const void* p, unsigned to) { return ((uintptr_t)p & (to - 1)) != 0; }
 
