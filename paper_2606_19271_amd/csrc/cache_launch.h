@@ -1,5 +1,5 @@
 // cache_launch.h -- internal interface between the C ABI of the session cache (ts_cache.cpp) and its
-// kernels (cache_attn.hip, cache_pages.hip).  Not installed; the public interface is include/ts_cache.h.
+// kernels (cache_attn.hip, cache_tiles.hip, cache_weigh.hip, cache_pages.hip).  Not installed; the public interface is include/ts_cache.h.
 #pragma once
 #include <hip/hip_runtime_api.h>
 #include <stdint.h>
@@ -72,16 +72,16 @@ struct EvictArgs {
 
 // Host-side sizes (cache_plan.cpp).
 // Query rows (tokens x G) of an attention workgroup's tile: 256 (cache_tiles_kernel), or 32 or 16
-// (cache_rows_kernel).
+// (cache_rows_kernel); by the rows of a cached head at most, and by the call (call_tile).
 constexpr int kTileRows = 256;
 int row_tile(int64_t rows, float scale);
 int call_tile(int32_t nseq, int64_t rows, int32_t max_len, int32_t H, int32_t d, float scale, int32_t num_splits);
 // Workgroups of an unsplit attention call, and of its merge kernel.
 int64_t attn_items(int32_t nseq, int32_t max_rows, int32_t total, int32_t H, int32_t G, int tile);
 int64_t merge_blocks(int32_t nseq, int32_t max_rows, int32_t Hq, int32_t d);
-// How the keys of an attention call are dealt out, and its workspace of partial results.  Calls of few rows are split
-// into n_split ranges of pages, as many as fill the device; 256-row tiles into `shares` equal shares of the work.
-// A workspace that is too small makes them fewer or none.
+// How the keys of an attention call are dealt out, and its workspace of partial results: every row tile's in n_split ranges of
+// pages, as calls of few rows are, and 256-row tiles of one session or of little work; or those of several sessions in
+// `shares` equal shares of the work.  A workspace that is too small makes them fewer or none.
 struct Parts {
   int32_t n_split, shares;
   int64_t o_offset, bytes;  // the partial log-sum-exps lie first, then O
@@ -93,6 +93,9 @@ Parts attn_parts(const Sessions& ss, int32_t H, int32_t G, int32_t d, int tile, 
 // less than kEvenCost tiles a CU are not worth the shares.
 constexpr int kStartCost = 4, kShareMin = 12, kCutMin = 4;
 constexpr int kEvenItems = 2, kEvenCost = 40;
+// In key tiles too, of 1.7 us at 1560 rows x 32760 keys x 12 heads, d = 128: what ranges cost beside their tiles (writing the parts, and the
+// merge kernel's 8 us and its launch), and shares (finding them, 10 us, and the join kernel, 10 to 20).
+constexpr int kMergeCost = 6, kJoinCost = 14;
 // Workgroups of the other kernels.
 // weigh: with up to 64 rows of a cached head, the parts that the pages of a session and head are dealt to (else 0: not this
 // kernel); a page to a workgroup where there are few, else four pages of a head, in 8 XCDs x nseq sessions x weigh_share

@@ -79,12 +79,14 @@ Parts attn_parts(const Sessions& ss, int32_t H, int32_t G, int32_t d, int tile, 
       const bool known = ss.nseq == 1 || ceil_div(cost, cus) < kEvenCost;
       int64_t best = INT64_MAX;
       for (int32_t i = 1; known && i <= 16 && (i == 1 || tiles / i >= kCutMin); ++i) {
-        const int64_t c = ceil_div(items * i, cus) * (ceil_div(tiles, i) + kStartCost) + (i > 1 ? 6 : 0);
+        const int64_t c = ceil_div(items * i, cus) * (ceil_div(tiles, i) + kStartCost) + (i > 1 ? kMergeCost : 0);
         if (c < best && ranges(i, ss.total, H * G, d).bytes <= workspace) best = c, n = i;
       }
       const int64_t shares = std::min<int64_t>(cus, ceil_div(cost, kShareMin));
       const Parts p = parts(1, (int32_t)shares, 2 * shares * kTileRows, d);
-      const bool even = ss.nseq == 1 ? ceil_div(cost, shares) * 7 / 6 + 14 < best : !known;
+      // (of one session, whose row tiles in ranges read the same keys at one time and in shares do not, only where ranges
+      // leave a sixth of the device idle: see Work in cache_tiles.hip)
+      const bool even = ss.nseq == 1 ? ceil_div(cost, shares) * 7 / 6 + kJoinCost < best : !known;
       if (even && shares > 1 && p.bytes <= workspace) return p;
     }
   }

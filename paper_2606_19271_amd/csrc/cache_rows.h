@@ -1,5 +1,5 @@
 // cache_rows.h -- attention of up to 32 query rows of one cached head over a range of its session's pages, by a
-// workgroup whose waves take the pages in turn.  Used for calls of few rows (cache_attn.hip) and for the last, thin
+// workgroup whose waves take the pages in turn.  Used for calls of few rows (cache_attn.hip) and, once or twice, for the last, thin
 // tile of a session's rows (cache_tiles.hip).
 #pragma once
 #include <hip/hip_runtime.h>

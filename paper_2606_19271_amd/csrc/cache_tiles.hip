@@ -217,11 +217,11 @@ __device__ __forceinline__ void write_rows(const TileItem& it, const RowArgs& a,
         l == 0.0f ? -INFINITY : ((m_c - kTileBias) + __builtin_amdgcn_logf(l * (float)(1 << (int)kTileBias))) * kLn2;
 }
 
-// kActive = false: a wave whose rows all lie past the session's: it fetches its share and keeps the barriers.
 // How the work is dealt to workgroups: an item each (find_item), whole or in n_split ranges of keys; or equal shares of it
 // (Work below).
 enum Mode { kWhole, kSplit, kEven };
 
+// kActive = false: a wave whose rows all lie past the session's: it fetches its share and keeps the barriers.
 template <int D, bool kGroupB, Mode kMode, bool kActive>
 __device__ __forceinline__ void run_tile_group(const TileItem& it, const RowArgs& a, char* smem) {
   using G = Geo<D>;
