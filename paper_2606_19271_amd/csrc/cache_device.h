@@ -67,10 +67,10 @@ __device__ __forceinline__ unsigned narrow4(float a, float b, float c, float d) 
   return (unsigned)r;
 }
 
-// Four bytes of a page with this exponent.  At the largest one, 247, a magnitude of 1.9375 * 2^127 or more is rounded to
-// 256 * 2^120, which is no bfloat16: it becomes the element before, 240 * 2^120.
-__device__ __forceinline__ unsigned in_bf16(unsigned bytes, int exp) {
-  if (exp != 247) return bytes;
+// Four bytes of a page with the largest exponent.  There a magnitude of 1.9375 * 2^127 or more is rounded to 256 * 2^120, which
+// is no bfloat16: it becomes the element before, 240 * 2^120.
+constexpr int kTopExp = 247;
+__device__ __forceinline__ unsigned in_bf16(unsigned bytes) {
   const unsigned off = (bytes & 0x7f7f7f7fu) ^ 0x78787878u;  // 0 where the byte is +-256
   return bytes - (~(off + 0x7f7f7f7fu) >> 7 & 0x01010101u);
 }
