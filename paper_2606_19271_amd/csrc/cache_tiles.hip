@@ -115,12 +115,24 @@ constexpr float kTileBias = 15.0f;
 constexpr int kTileDown = 4;  // value_exp: beside the bias, for rows of 2^19 keys
 enum TilePlace { kFirst = 0, kInner = 1, kLast = 2 };
 
+// x of the wave's two 32-lane halves (lane l and lane l ^ 32) added up.
+__device__ __forceinline__ float half_sum(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // The online softmax of one tile, as softmax_tile of attn_kernels.hip: the running maximum stays while the weights of
-// no lane add up to 2, nor to more than twice those of the tiles before.  So a key that holds most of a row moves the maximum
-// to itself, and its weight is a power of two, which the product's 16 bits hold: O is its value as it is, though l sums the
-// weights before they are rounded.  (Dividing by sums of the rounded ones instead, from the matrix core as in attn_kernels.hip
-// beside these, takes 2.5 to 5 % more time; this 307 -> 311 us at 1560 rows x 32760 keys x 12 heads, d = 128, and 23.4 -> 24.3 where tiles
-// are few.)  l: the row sum over the lane's half of the keys.
+// no lane add up to 2, nor to more than kDominant times what the row has.  So a key that dominates a row moves the maximum to
+// itself, and its weight is a power of two, which the product's 16 bits hold: O is its value as it is, though l sums the
+// weights before they are rounded.  The test takes 1 % (1560 rows x 32760 keys x 12 heads, d = 128, 295 -> 298 us), and each move
+// another tile's time, so the cost goes by how far scores spread.  1536 rows x 16384 keys x 12 heads, scores of standard deviation 1,
+// 2, 3 and 5, in us without it, with 16 times, with 2 times:
+//   d = 128   159 161 162 165    161 162 166 179    160 165 178 196
+//   d = 64    105 105 105 108    105 105 109 130    106 109 127 140
+// Dividing by sums of the rounded weights instead, from the matrix core as in attn_kernels.hip beside these, takes 2.5 to 5 %
+// more time for any scores.  l: the row sum over the lane's half of the keys.
+constexpr float kDominant = 16.0f;
+
 template <int D, int kPlace, int kHooks, int kEvery, typename Issue>
 __device__ __forceinline__ void tile_softmax(f32x16 (&s)[Geo<D>::kBN / 32], bf16x8 (&p)[Geo<D>::kBN / 16],
                                              float& m_c, float& l, f32x16 (&o)[D / 32], float c, int keys,
@@ -131,7 +143,8 @@ __device__ __forceinline__ void tile_softmax(f32x16 (&s)[Geo<D>::kBN / 32], bf16
     const float sum = exp_pack<kBN / 16, kHooks, kEvery>(s, p, m_c, c, issue);
     float before = l;
     __asm__ volatile("" : "+v"(before));  // (l itself, when it is tested here, has the compiler spill 40 to 120 registers)
-    if (__builtin_amdgcn_ballot_w64(!(sum < fminf(2.0f, 2.0f * before))) == 0) {  // (NaN and infinities among them)
+    before = half_sum(before);            // the row's: a lane's own is next to nothing where the other one's keys hold the row
+    if (__builtin_amdgcn_ballot_w64(!(sum < fminf(2.0f, kDominant * before))) == 0) {  // (NaN and infinities among them)
       l += sum;
       return;
     }
@@ -422,8 +435,7 @@ __device__ __forceinline__ void run_tile_group(const TileItem& it, const RowArgs
   if (!kGroupB) block_sync();  // matches group B's extra barrier at the start
 
   if constexpr (kActive) {
-    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
-    l = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    l = half_sum(l);
     const int q0 = it.row0 + 32 * wave;
     lds_char* const stage = lds + T::kOBase + wave * G::kOWave;
     if constexpr (kMode != kEven) write_rows<D, kMode == kSplit ? kSlab : kResult>(it, a, oacc, l, m_c, q0, stage, lane);
