@@ -124,9 +124,9 @@ __device__ __forceinline__ float half_sum(float x) {
 // The online softmax of one tile, as softmax_tile of attn_kernels.hip: the running maximum stays while the weights of
 // no lane add up to 2, nor to more than kDominant times what the row has.  So a key that dominates a row moves the maximum to
 // itself, and its weight is a power of two, which the product's 16 bits hold: O is its value as it is, though l sums the
-// weights before they are rounded.  The test takes 1 % (1560 rows x 32760 keys x 12 heads, d = 128, 295 -> 298 us), and each move
-// another tile's time, so the cost goes by how far scores spread.  1536 rows x 16384 keys x 12 heads, scores of standard deviation 1,
-// 2, 3 and 5, in us without it, with 16 times, with 2 times:
+// weights before they are rounded.  The test takes 0.7 % (1560 rows x 32760 keys x 12 heads, d = 128, 290 -> 292 us; 293 with its
+// limit formed behind the weights), each move another tile's time: the cost goes by how far scores spread.  1536 rows x 16384
+// keys x 12 heads, scores of standard deviation 1, 2, 3 and 5, in us without it, with 16 times, with 2 times:
 //   d = 128   159 161 162 165    161 162 166 179    160 165 178 196
 //   d = 64    105 105 105 108    105 105 109 130    106 109 127 140
 // Dividing by sums of the rounded weights instead, from the matrix core as in attn_kernels.hip beside these, takes 2.5 to 5 %
@@ -140,11 +140,13 @@ __device__ __forceinline__ void tile_softmax(f32x16 (&s)[Geo<D>::kBN / 32], bf16
   constexpr int kBN = Geo<D>::kBN;
   const int hb = lane >> 5;
   if (kPlace == kInner) {
-    const float sum = exp_pack<kBN / 16, kHooks, kEvery>(s, p, m_c, c, issue);
     float before = l;
     __asm__ volatile("" : "+v"(before));  // (l itself, when it is tested here, has the compiler spill 40 to 120 registers)
-    before = half_sum(before);            // the row's: a lane's own is next to nothing where the other one's keys hold the row
-    if (__builtin_amdgcn_ballot_w64(!(sum < fminf(2.0f, kDominant * before))) == 0) {  // (NaN and infinities among them)
+    // of the row: a lane's own is next to nothing where the other one's keys hold the row
+    float limit = fminf(2.0f, kDominant * half_sum(before));
+    __asm__ volatile("" : "+v"(limit));
+    const float sum = exp_pack<kBN / 16, kHooks, kEvery>(s, p, m_c, c, issue);
+    if (__builtin_amdgcn_ballot_w64(!(sum < limit)) == 0) {  // (NaN and infinities among them)
       l += sum;
       return;
     }

@@ -123,7 +123,7 @@ __device__ __forceinline__ int key_of_lane(int lane) {
 // ---- many keys.  A workgroup of four waves, one page each, walks over the rows, 64 at a time; two workgroups share a CU.
 // A wave forms the weights of 32 rows while its MFMAs form the products of the next 32: between every two MFMAs two
 // scores are weighed, and an operand is read again, for the rows after the next, when its second MFMA has it.  1560 rows x
-// 32760 keys x 12 heads, d = 128: 146 us (1.08 PFLOP/s; 154 on a slower device), against 177 us for two waves that take turns at a SIMD, one with
+// 32760 keys x 12 heads, d = 128: 153 us (1.03 PFLOP/s), against 177 us for two waves that take turns at a SIMD, one with
 // its MFMAs and the other with its weights (the attention kernels' schedule): without the sums of a second product to
 // form, a lone wave's exponentials take longer than the MFMAs they are to hide, and two waves fill each other's gaps.
 //
