@@ -1,6 +1,6 @@
-"""Builds, in-tree: libts_attn.so (the attention kernels and their C ABI) and libts_cache.so (the 8-bit
-session cache) for gfx950 with hipcc, and libts_sched.so (the closed-loop session scheduler, host code
-only) with g++."""
+"""Builds, in-tree: libts_attn.so (the attention kernels and their C ABI), libts_cache.so (the 8-bit
+session cache) and libts_block.so (norm and rotation of queries and keys, and the gradients) for gfx950 with
+hipcc, and libts_sched.so (the closed-loop session scheduler, host code only) with g++."""
 import os
 import subprocess
 
@@ -16,6 +16,10 @@ CACHE_LIB = os.path.join(HERE, "libts_cache.so")
 CACHE_SOURCES = [os.path.join(CSRC, "cache_attn.hip"), os.path.join(CSRC, "cache_tiles.hip"),
                  os.path.join(CSRC, "cache_weigh.hip"), os.path.join(CSRC, "cache_pages.hip"),
                  os.path.join(CSRC, "cache_plan.cpp"), os.path.join(CSRC, "ts_cache.cpp")]
+
+BLOCK_LIB = os.path.join(HERE, "libts_block.so")
+BLOCK_SOURCES = [os.path.join(CSRC, "qk_rope.hip"), os.path.join(CSRC, "attn_bwd.hip"), os.path.join(CSRC, "block_plan.cpp"),
+                 os.path.join(CSRC, "ts_block.cpp")]
 
 SCHED_LIB = os.path.join(HERE, "libts_sched.so")
 SCHED_SOURCES = [os.path.join(CSRC, "sched.cpp")]
@@ -52,6 +56,11 @@ def build_cache(out=CACHE_LIB, extra_flags=()):
     return build(out, extra_flags, CACHE_SOURCES)
 
 
+def build_block(out=BLOCK_LIB, extra_flags=()):
+    """Compile the library of the transformer block's calls `out` (always recompiles); returns out."""
+    return build(out, extra_flags, BLOCK_SOURCES)
+
+
 def build_sched(out=SCHED_LIB):
     """Compile the scheduler library `out` with g++ (always recompiles); returns out."""
     tmp = out + ".tmp%d" % os.getpid()
@@ -66,4 +75,5 @@ def build_sched(out=SCHED_LIB):
 if __name__ == "__main__":
     print(build())
     print(build_cache())
+    print(build_block())
     print(build_sched())

@@ -1,0 +1,89 @@
+// block_launch.h -- internal interface between the C ABI of the transformer block's calls (ts_block.cpp) and its
+// kernels (qk_rope.hip, attn_bwd.hip).  Not installed; the public interface is include/ts_block.h.
+#pragma once
+#include <hip/hip_runtime_api.h>
+#include <stdint.h>
+
+namespace tsblock {
+
+// Rows of heads (ts_rows), or p = null.
+struct Rows {
+  void* p;
+  int64_t stride;
+  int32_t heads;
+};
+
+// Rotation (ts_rope); freq null: none.
+struct Rope {
+  const int32_t* pos;
+  const double* freq;
+  int32_t n0, n01;  // pairs of the first axis, of the first two
+  int32_t interleaved;
+};
+
+struct RopeArgs {
+  Rows q, k, q_out, k_out;
+  const float* q_weight;
+  const float* k_weight;
+  Rope rope;
+  int32_t T, d;
+  float eps;
+};
+
+struct RopeBwdArgs {
+  Rows dq_out, dk_out, q, k, dq, dk;
+  const float* q_weight;
+  const float* k_weight;
+  float* dq_weight;
+  float* dk_weight;
+  float* part;  // [rope_bwd_blocks][2][d]: sums of each workgroup
+  Rope rope;
+  int32_t T, d;
+  float eps;
+};
+
+constexpr int kRopeThreads = 256;
+// The workgroups of a gradient call with weights, whatever the device: its sums' order goes by them.
+int32_t rope_bwd_blocks(int32_t T, int32_t q_heads, int32_t k_heads, int32_t d);
+
+struct BwdArgs {
+  const void* d_o;
+  const void* q;
+  const void* k;
+  const void* v;
+  const void* o;
+  const float* lse;
+  void* dq;
+  void* dk;
+  void* dv;
+  const int32_t* cu_q;
+  const int32_t* cu_k;
+  float* stat;     // [2][H][total_q]: -lse / scale, -D
+  float* part_q;   // [n_q][total_q][H][d], where n_q > 1
+  float* part_k;   // [n_k][total_k][H][d] of dk, then of dv, where n_k > 1
+  int32_t nseq, max_q, max_k, total_q, total_k, H, d;
+  int32_t n_q, n_k;
+  float scale;
+};
+
+constexpr int kBwdTile = 256;  // queries (dq) or keys (dk, dv) of a workgroup
+constexpr int64_t kBwdGrid = (int64_t)1 << 22;  // workgroups of a launch, which take more items than one where there are more
+// Rows of the other side that a workgroup holds in LDS at a time.
+constexpr int bwd_step(int d) { return d == 64 ? 128 : 64; }
+
+// How a call is divided: the keys of a query tile in n_q ranges, the queries of a key tile in n_k; the workspace's layout.
+struct BwdParts {
+  int32_t n_q, n_k;
+  int64_t q_offset, k_offset, bytes;
+};
+BwdParts bwd_parts(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d,
+                   int32_t num_splits, int64_t workspace, int32_t cus);
+// Upper bounds of the tiles of one side over all segments and heads.
+int64_t bwd_tiles(int32_t nseq, int32_t most, int32_t total, int32_t H);
+
+hipError_t configure_kernels();
+hipError_t launch_rope(const RopeArgs& a, hipStream_t st);
+hipError_t launch_rope_bwd(const RopeBwdArgs& a, hipStream_t st);
+hipError_t launch_attn_bwd(const BwdArgs& a, hipStream_t st);
+
+}  // namespace tsblock

@@ -1,0 +1,328 @@
+// qk_rope.hip -- norm and rotation of queries and keys in one pass (ts_qk_rope), and its gradients.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "block_launch.h"
+
+namespace tsblock {
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kWaves = kRopeThreads / 64;
+
+// A head's d channels lie over d / 16 lanes: lane j has channels 8j..8j+7 and d/2 + 8j..8j+7, two 16-byte loads, so that
+// the pairs of both orders lie within a lane: neighbours (2i, 2i + 1), or (i, i + d / 2).  A wave's step is
+// 64 / (d / 16) heads of one token.
+template <int D>
+struct Geo {
+  static constexpr int kLanes = D / 16;
+  static constexpr int kHeads = 64 / kLanes;
+};
+
+struct Head {
+  bf16x8 lo, hi;
+};
+
+template <int D>
+__device__ __forceinline__ Head load_head(const __bf16* p, bool live) {
+  if (!live) return Head{};
+  return Head{*(const bf16x8*)p, *(const bf16x8*)(p + D / 2)};
+}
+
+template <int D>
+__device__ __forceinline__ void store_head(__bf16* p, const float (&x)[16], bool live) {
+  if (!live) return;
+  bf16x8 lo, hi;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) lo[i] = (__bf16)x[i], hi[i] = (__bf16)x[8 + i];
+  *(bf16x8*)p = lo;
+  *(bf16x8*)(p + D / 2) = hi;
+}
+
+__device__ __forceinline__ void widen(const Head& h, float (&x)[16]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = (float)h.lo[i], x[8 + i] = (float)h.hi[i];
+}
+
+// The lane's slots of its eight pairs, in x[16]: pair i's members.
+template <bool kPairs>
+__device__ __forceinline__ constexpr int member(int i, int which) {
+  return kPairs ? 2 * i + which : i + 8 * which;
+}
+
+// cos and sin of the lane's eight angles.  A turn's fraction is exact to 2^-53 of the angle in 64 bits, and what is left
+// of it, half a turn at most, fits 32.
+template <int D, bool kPairs>
+__device__ __forceinline__ void angles(const Rope& rope, int t, int j, float (&c)[8], float (&s)[8]) {
+  const int32_t p0 = rope.pos[3 * (int64_t)t], p1 = rope.pos[3 * (int64_t)t + 1], p2 = rope.pos[3 * (int64_t)t + 2];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int pair = !kPairs ? 8 * j + i : i < 4 ? 4 * j + i : D / 4 + 4 * j + i - 4;
+    const int32_t p = pair < rope.n0 ? p0 : pair < rope.n01 ? p1 : p2;
+    double turns = (double)p * (rope.freq[pair] * 0.15915494309189535);
+    turns -= __builtin_rint(turns);
+    sincospif(2.0f * (float)turns, &s[i], &c[i]);
+  }
+}
+
+// x of the lane l ^ kXor (1, 2 or 4) of its eight.
+template <int kXor>
+__device__ __forceinline__ int from_lane(int x) {
+  constexpr int kCtrl = kXor == 1 ? 0xB1 : kXor == 2 ? 0x4E : 0x141;  // quad_perm, quad_perm, row_half_mirror
+  return __builtin_amdgcn_update_dpp(0, x, kCtrl, 0xF, 0xF, true);
+}
+template <int kXor>
+__device__ __forceinline__ float from_lane(float x) { return __int_as_float(from_lane<kXor>(__float_as_int(x))); }
+template <int kXor>
+__device__ __forceinline__ double from_lane(double x) {
+  return __hiloint2double(from_lane<kXor>(__double2hiint(x)), from_lane<kXor>(__double2loint(x)));
+}
+
+// The sum over a head's lanes, in each of them (the half mirror takes a quad's sum from the other quad).
+template <int D, typename T>
+__device__ __forceinline__ T head_sum(T x) {
+  x += from_lane<1>(x);
+  x += from_lane<2>(x);
+  if (D == 128) x += from_lane<4>(x);
+  return x;
+}
+
+// 1 / sqrt(mean of squares + eps).  In 64 bits, where no bfloat16 square overflows or vanishes.
+template <int D>
+__device__ __forceinline__ float inverse_rms(const float (&x)[16], float eps) {
+  double sum = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) sum = __builtin_fma((double)x[i], (double)x[i], sum);
+  const double m = __builtin_fma(head_sum<D>(sum), 1.0 / D, (double)eps);
+  const double y = __builtin_amdgcn_rsq(m);
+  const double z = y * __builtin_fma(-0.5 * m * y, y, 1.5);  // (NaN at infinity, where y is 0)
+  return (float)(y == 0 ? y : z);
+}
+
+template <int D>
+__device__ __forceinline__ void load_weights(const float* w, int j, float (&x)[16]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = w ? w[8 * j + i] : 1.0f, x[8 + i] = w ? w[D / 2 + 8 * j + i] : 1.0f;
+}
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// A wave's steps: `count` from `first` on, step s being heads kHeads (s % groups) .. of token s / groups, those of q before
+// those of k.
+struct Steps {
+  int t, g, left;
+  __device__ Steps(int wave, int per, int all, int groups) {
+    const int first = (int)min((int64_t)wave * per, (int64_t)all);
+    t = first / groups;
+    g = first - t * groups;
+    left = min(per, all - first);
+  }
+  __device__ bool next(int groups) {  // whether the token is another one
+    --left;
+    if (++g < groups) return false;
+    g = 0;
+    ++t;
+    return true;
+  }
+};
+
+template <int D, bool kPairs>
+__global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int groups_q, int groups, int steps, int per) {
+  using G = Geo<D>;
+  const int lane = threadIdx.x & 63, wave = uniform(blockIdx.x * kWaves + (threadIdx.x >> 6));
+  const int j = lane % G::kLanes, r = lane / G::kLanes;
+  Steps at(wave, per, steps, groups);
+  if (at.left <= 0) return;
+  float wq[16], wk[16], c[8], s[8];
+  load_weights<D>(a.q_weight, j, wq);
+  load_weights<D>(a.k_weight, j, wk);
+  auto rows = [&](const Rows& q, const Rows& k, const Steps& at, bool& live) {
+    const bool is_k = at.g >= groups_q;
+    const Rows& x = is_k ? k : q;
+    const int h = (at.g - (is_k ? groups_q : 0)) * G::kHeads + r;
+    live = h < x.heads;
+    return (__bf16*)x.p + at.t * x.stride + h * D + 8 * j;
+  };
+  bool live;
+  const __bf16* from = rows(a.q, a.k, at, live);
+  Head in = load_head<D>(from, live);
+  bool fresh = true;
+  while (true) {
+    if (fresh && a.rope.freq) angles<D, kPairs>(a.rope, at.t, j, c, s);
+    const Steps here = at;
+    Head after = in;
+    fresh = at.next(groups);
+    if (at.left > 0) {
+      bool next_live;
+      from = rows(a.q, a.k, at, next_live);
+      after = load_head<D>(from, next_live);
+    }
+    float x[16];
+    widen(in, x);
+    const bool is_k = here.g >= groups_q;
+    if (is_k ? a.k_weight : a.q_weight) {
+      const float f = inverse_rms<D>(x, a.eps);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = x[i] * f * (is_k ? wk[i] : wq[i]);
+    }
+    if (a.rope.freq) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float u = x[member<kPairs>(i, 0)], v = x[member<kPairs>(i, 1)];
+        x[member<kPairs>(i, 0)] = u * c[i] - v * s[i];
+        x[member<kPairs>(i, 1)] = u * s[i] + v * c[i];
+      }
+    }
+    __bf16* const to = rows(a.q_out, a.k_out, here, live);
+    store_head<D>(to, x, live);
+    if (at.left <= 0) return;
+    in = after;
+  }
+}
+
+// Gradients.  With g the result's gradient turned back, n = x r the normalised row:
+//   dw = sum g n,   dx = r (g w - n mean(g w n))
+// Each wave sums dw over its steps, the workgroup its waves' sums, and rope_bwd_join_kernel those of the workgroups.
+template <int D, bool kPairs>
+__global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(RopeBwdArgs a, int groups_q, int groups, int steps, int per) {
+  using G = Geo<D>;
+  const int lane = threadIdx.x & 63, wave = uniform(blockIdx.x * kWaves + (threadIdx.x >> 6));
+  const int j = lane % G::kLanes, r = lane / G::kLanes;
+  Steps at(wave, per, steps, groups);
+  float wq[16], wk[16], c[8], s[8], sum_q[16] = {}, sum_k[16] = {};
+  load_weights<D>(a.q_weight, j, wq);
+  load_weights<D>(a.k_weight, j, wk);
+  auto rows = [&](const Rows& q, const Rows& k, const Steps& at, bool& live) {
+    const bool is_k = at.g >= groups_q;
+    const Rows& x = is_k ? k : q;
+    const int h = (at.g - (is_k ? groups_q : 0)) * G::kHeads + r;
+    live = h < x.heads && x.p;
+    return (__bf16*)x.p + at.t * x.stride + h * D + 8 * j;
+  };
+  bool fresh = true;
+  auto load = [&](Head& dy, Head& x) {
+    bool live;
+    const __bf16* p = rows(a.dq_out, a.dk_out, at, live);
+    dy = load_head<D>(p, live);
+    p = rows(a.q, a.k, at, live);
+    x = load_head<D>(p, live && (at.g >= groups_q ? a.k_weight : a.q_weight));
+  };
+  Head dy_in{}, x_in{};
+  if (at.left > 0) load(dy_in, x_in);
+  while (at.left > 0) {
+    if (fresh && a.rope.freq) angles<D, kPairs>(a.rope, at.t, j, c, s);
+    const Steps here = at;
+    Head dy_next = dy_in, x_next = x_in;
+    fresh = at.next(groups);
+    if (at.left > 0) load(dy_next, x_next);
+    float g[16];
+    widen(dy_in, g);
+    if (a.rope.freq) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float u = g[member<kPairs>(i, 0)], v = g[member<kPairs>(i, 1)];
+        g[member<kPairs>(i, 0)] = u * c[i] + v * s[i];
+        g[member<kPairs>(i, 1)] = v * c[i] - u * s[i];
+      }
+    }
+    const bool is_k = here.g >= groups_q;
+    if (is_k ? a.k_weight : a.q_weight) {
+      float n[16], dot = 0;
+      widen(x_in, n);
+      const float f = inverse_rms<D>(n, a.eps);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        n[i] *= f;
+        const float dw = g[i] * n[i];
+        if (is_k) sum_k[i] += dw;
+        else sum_q[i] += dw;
+        g[i] *= is_k ? wk[i] : wq[i];
+        dot = __builtin_fmaf(g[i], n[i], dot);
+      }
+      dot = head_sum<D>(dot) * (1.0f / D);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) g[i] = (g[i] - n[i] * dot) * f;
+    }
+    bool live;
+    __bf16* const to = rows(a.dq, a.dk, here, live);
+    store_head<D>(to, g, live);
+    dy_in = dy_next;
+    x_in = x_next;
+  }
+  if (!a.part) return;
+  __shared__ float sums[kWaves][2 * D];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+#pragma unroll
+    for (int o = G::kLanes; o < 64; o <<= 1) {
+      sum_q[i] += __shfl_xor(sum_q[i], o);
+      sum_k[i] += __shfl_xor(sum_k[i], o);
+    }
+    if (r == 0) {
+      const int ch = (i < 8 ? 8 * j + i : D / 2 + 8 * j + i - 8);
+      sums[threadIdx.x >> 6][ch] = sum_q[i];
+      sums[threadIdx.x >> 6][D + ch] = sum_k[i];
+    }
+  }
+  __syncthreads();
+  for (int ch = threadIdx.x; ch < 2 * D; ch += kRopeThreads) {
+    float x = sums[0][ch];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) x += sums[w][ch];
+    a.part[(int64_t)blockIdx.x * 2 * D + ch] = x;
+  }
+}
+
+// The weights' gradients: 16 channels to a workgroup, the workgroups' sums dealt to 16 threads each, in 64 bits.
+template <int D>
+__global__ __launch_bounds__(256) void rope_bwd_join_kernel(const float* part, int blocks, float* dq_weight, float* dk_weight) {
+  __shared__ double sums[16][17];
+  const int ch = blockIdx.x * 16 + (threadIdx.x & 15), u = threadIdx.x >> 4;
+  double x = 0;
+  for (int b = u; b < blocks; b += 16) x += part[(int64_t)b * 2 * D + ch];
+  sums[u][threadIdx.x & 15] = x;
+  __syncthreads();
+  if (u != 0) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) x += sums[i][threadIdx.x];
+  float* const to = ch < D ? dq_weight : dk_weight;
+  if (to) to[ch < D ? ch : ch - D] = (float)x;
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return a / b + (a % b != 0); }
+
+template <int D>
+hipError_t rope(const RopeArgs& a, hipStream_t st) {
+  const int gq = (int)ceil_div(a.q.heads, Geo<D>::kHeads), groups = gq + (int)ceil_div(a.k.heads, Geo<D>::kHeads);
+  const int steps = a.T * groups;
+  const int per = (int)std::max({(int64_t)1, std::min<int64_t>(groups, steps / 8192), ceil_div(steps, (int64_t)1 << 24)});
+  const unsigned blocks = (unsigned)ceil_div(ceil_div(steps, per), kWaves);
+  if (a.rope.interleaved) rope_kernel<D, true><<<blocks, kRopeThreads, 0, st>>>(a, gq, groups, steps, per);
+  else rope_kernel<D, false><<<blocks, kRopeThreads, 0, st>>>(a, gq, groups, steps, per);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t rope_bwd(const RopeBwdArgs& a, hipStream_t st) {
+  const int gq = (int)ceil_div(a.dq.heads, Geo<D>::kHeads), groups = gq + (int)ceil_div(a.dk.heads, Geo<D>::kHeads);
+  const int steps = a.T * groups;
+  const int blocks = rope_bwd_blocks(a.T, a.dq.heads, a.dk.heads, D);
+  const int per = blocks ? (int)ceil_div(steps, (int64_t)blocks * kWaves) : 1;
+  if (blocks > 0) {
+    if (a.rope.interleaved) rope_bwd_kernel<D, true><<<blocks, kRopeThreads, 0, st>>>(a, gq, groups, steps, per);
+    else rope_bwd_kernel<D, false><<<blocks, kRopeThreads, 0, st>>>(a, gq, groups, steps, per);
+  }
+  if (a.dq_weight || a.dk_weight) rope_bwd_join_kernel<D><<<2 * D / 16, 256, 0, st>>>(a.part, blocks, a.dq_weight, a.dk_weight);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rope(const RopeArgs& a, hipStream_t st) { return a.d == 64 ? rope<64>(a, st) : rope<128>(a, st); }
+hipError_t launch_rope_bwd(const RopeBwdArgs& a, hipStream_t st) { return a.d == 64 ? rope_bwd<64>(a, st) : rope_bwd<128>(a, st); }
+
+}  // namespace tsblock
