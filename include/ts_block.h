@@ -97,12 +97,12 @@ int64_t ts_qk_rope_bwd_workspace(int32_t T, int32_t q_heads, int32_t k_heads, in
  *   dk[j]  = scale * sum_t S[t,j] * q[t]
  * per head.  P and S are formed in 32 bits and rounded to bfloat16 for the products they enter; sums are 32 bits.
  *  q, o, d_o, dq   bfloat16 [total_q][H][d];  k, v, dk, dv  bfloat16 [total_k][H][d];  lse  float32 [total_q][H]
- *  cu_seqlens_q/k  int32, nseq + 1 entries each, read on the device only.  A segment whose rows are not
- *                  inside [0, total] or outnumber max_seqlen, on either side, is skipped: its gradients are not
- *                  written.  Nor are rows of no segment.  Segments that share rows leave their gradients
- *                  unspecified.  A segment's queries without keys get dq = 0, keys without queries
- *                  dk = dv = 0.  With TS_ATTN_VALIDATE=1 the call synchronizes and returns TS_ERR_SEGMENTS
- *                  for offsets that ts_attn_fwd_kvcache would refuse (not on a capturing stream).
+ *  cu_seqlens_q/k  int32, nseq + 1 entries each, read on the device only, under the rules of ts_attn_fwd_kvcache: they
+ *                  start at 0, do not descend, end at total_q / total_k, and no segment is longer than its
+ *                  max_seqlen.  Offsets that break them make the call a device-side no-op (the gradients are left
+ *                  unwritten); with TS_ATTN_VALIDATE=1 the call instead synchronizes and returns
+ *                  TS_ERR_SEGMENTS (not on a capturing stream).  Segments may be empty on either side: queries without
+ *                  keys get dq = 0, keys without queries dk = dv = 0.
  *  scale           0, or a float of magnitude 2^-100 to 2^100 (TS_ERR_SCALE)
  *  num_splits      0: the library divides the work.  n in 1..16: the keys of each query tile and the queries of each key tile
  *                  are taken in n ranges, whose 32-bit sums another kernel adds up in order.
@@ -111,7 +111,7 @@ int64_t ts_qk_rope_bwd_workspace(int32_t T, int32_t q_heads, int32_t k_heads, in
  * The bits of a segment's gradients depend on its own rows and on the division; with n >= 1 on nothing else.
  * No output may overlap another one, an input or the workspace (TS_ERR_ALIAS).  Sizes, TS_ERR_SHAPE:
  * (max_seqlen + 256) * H * d * 2 below 2^31 for each side, and for the work items nseq * H * (max_seqlen_q / 256 +
- * max_seqlen_k / 256 + 2) below 2^26 and H * (total / 256 + nseq) below 2^21 for each side.
+ * max_seqlen_k / 256 + 2) below 2^26 and H * (total / 256 + nseq) below 2^19 for each side.
  */
 #define TS_ATTN_BWD_MAX_SPLITS 16
 int ts_attn_bwd(const void* d_o, const void* q, const void* k, const void* v, const void* o, const float* lse, void* dq,

@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_tile.h"
 #include "block_launch.h"
@@ -42,74 +43,6 @@ struct Bwd {
   }
 };
 
-// Item `item` of a call: which segment, head, tile and range.
-struct Found {
-  int seg, h, tile, split;
-  bool keys;  // dk, dv (held rows are keys), else dq
-  int q0, nq, k0, nk;  // the segment's rows
-};
-
-struct Offsets {
-  const int32_t* cu_q;
-  const int32_t* cu_k;
-  int nseq, max_q, max_k, total_q, total_k;
-};
-
-// A segment's rows; none where its offsets break the rules.
-__device__ __forceinline__ void segment(const Offsets& f, int s, int& q0, int& nq, int& k0, int& nk) {
-  q0 = f.cu_q[s];
-  k0 = f.cu_k[s];
-  const int q1 = f.cu_q[s + 1], k1 = f.cu_k[s + 1];
-  const bool ok = q0 >= 0 && q1 >= q0 && q1 <= f.total_q && q1 - q0 <= f.max_q && k0 >= 0 && k1 >= k0 &&
-                  k1 <= f.total_k && k1 - k0 <= f.max_k;
-  nq = ok ? q1 - q0 : 0;
-  nk = ok ? k1 - k0 : 0;
-}
-
-__device__ __forceinline__ int wave_sum_to(int x, int lane) {  // inclusive prefix sum over the lanes
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
-  return x;
-}
-
-// Tiles of both sides over all segments.
-__device__ __forceinline__ void count_tiles(const Offsets& f, int lane, int& tiles_q, int& tiles_k) {
-  tiles_q = tiles_k = 0;
-  for (int s0 = 0; s0 < f.nseq; s0 += 64) {
-    int q0, nq = 0, k0, nk = 0;
-    if (s0 + lane < f.nseq) segment(f, s0 + lane, q0, nq, k0, nk);
-    const int a = wave_sum_to((nq + kBwdTile - 1) / kBwdTile, lane), b = wave_sum_to((nk + kBwdTile - 1) / kBwdTile, lane);
-    tiles_q += __shfl(a, 63);
-    tiles_k += __shfl(b, 63);
-  }
-}
-
-// The segment that holds item `at` of one side, whose segments have H * n items a tile; `at` becomes the item's place in it.
-__device__ __forceinline__ void find_segment(const Offsets& f, bool keys, int per_tile, int lane, int& at, Found& w) {
-  int before = 0;
-  for (int s0 = 0; s0 < f.nseq; s0 += 64) {
-    int q0 = 0, nq = 0, k0 = 0, nk = 0;
-    if (s0 + lane < f.nseq) segment(f, s0 + lane, q0, nq, k0, nk);
-    const int items = ((keys ? nk : nq) + kBwdTile - 1) / kBwdTile * per_tile;
-    const int upto = before + wave_sum_to(items, lane);
-    const uint64_t beyond = __builtin_amdgcn_ballot_w64(upto > at);
-    if (beyond != 0) {
-      const int l = __builtin_ctzll(beyond);
-      w.seg = s0 + l;
-      w.q0 = __shfl(q0, l);
-      w.nq = __shfl(nq, l);
-      w.k0 = __shfl(k0, l);
-      w.nk = __shfl(nk, l);
-      at -= __shfl(upto - items, l);
-      return;
-    }
-    before = __shfl(upto, 63);
-  }
-}
-
 struct BwdCall {
   const __bf16* d_o;
   const __bf16* q;
@@ -121,47 +54,84 @@ struct BwdCall {
   __bf16* dv;
   float* part_q;
   float* part_k;
-  Offsets f;
-  int H, n_q, n_k;
-  bool q_first;
+  const BwdPlan* plan;
+  int total_q, total_k, H, n_q, n_k, most_q;
   float scale, c;  // c: log2(e) times the scale, or log2(e) for a scale of 0
 };
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// Item `item`, or false past the last one.  The side with the longer items comes first; a side's items go by segment, head,
-// range and tile, so that neighbours stream the same rows.
-__device__ __forceinline__ bool find_item(const BwdCall& a, int item, int tiles_q, int tiles_k, int lane, Found& w) {
-  const int items_q = tiles_q * a.H * a.n_q, items_k = tiles_k * a.H * a.n_k;
-  if (item >= items_q + items_k) return false;
-  int at = item;
-  w.keys = a.q_first ? at >= items_q : at < items_k;
-  if (w.keys && a.q_first) at -= items_q;
-  if (!w.keys && !a.q_first) at -= items_k;
-  const int n = w.keys ? a.n_k : a.n_q;
-  find_segment(a.f, w.keys, a.H * n, lane, at, w);
-  const int tiles = ((w.keys ? w.nk : w.nq) + kBwdTile - 1) / kBwdTile;
-  const int j = at / tiles;
-  w.tile = uniform(at - j * tiles);
-  w.h = uniform(j / n);
-  w.split = uniform(j % n);
-  w.q0 = uniform(w.q0);
-  w.nq = uniform(w.nq);
-  w.k0 = uniform(w.k0);
-  w.nk = uniform(w.nk);
-  return true;
+// An item of a call: which head, tile and range, of which segment's rows.
+struct Item {
+  int h, tile, split;
+  int held0, held_len, str0, str_len;
+};
+
+// Item `at` of one side, whose tiles each have `heads` * n items.  They go by segment, head, range and tile, so that
+// neighbours stream the same rows.
+__device__ __forceinline__ Item find_item(const BwdTile* tiles, int at, int heads, int n) {
+  const BwdTile* const t = tiles + at / (heads * n);  // (any tile of the item's segment)
+  at -= t->first * heads * n;
+  Item w;
+  const int j = at / t->tiles;
+  w.tile = at - j * t->tiles;
+  w.h = j / n;
+  w.split = j - w.h * n;
+  w.held0 = t->held0;
+  w.held_len = t->held_len;
+  w.str0 = t->str0;
+  w.str_len = t->str_len;
+  return w;
 }
 
-// Workgroup `item` of the dq (kKeys = false) or the dk, dv side.
+typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+
+// The LDS reads of a step take their address as a restrict pointer: the compiler then knows that they do not wait for the
+// DMA of the steps ahead.
+
+// to += x y^T for a block of 32 rows of X1 or X2.
+template <int D>
+__device__ __forceinline__ void rows_product(const lds_char* __restrict__ x, const bf16x8 (&y)[D / 16], f32x16& to) {
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk) to = mfma32(*(const lds_bf16x8*)(x + 32 * kk), y[kk], to);
+}
+
+// acc^T += x^T w for a block's 32 rows of X1 or X2.
+template <int D>
+__device__ __forceinline__ void columns_product(const lds_char* __restrict__ x, const bf16x8 (&w)[2], f32x16 (&acc)[D / 32]) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      const lds_char* const at = x + 4 * u * Bwd<D>::kGroup + 64 * db;
+      const bf16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)at);
+      const bf16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + 2 * Bwd<D>::kGroup));
+      acc[db] = mfma32(bf16x8{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]}, w[u], acc[db]);
+    }
+}
+
+// The statistics of a block's 32 queries, as the rows of an accumulator.
+__device__ __forceinline__ f32x16 row_statistics(const lds_char* __restrict__ x, int hb) {
+  f32x16 to;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const f32x4 y = *(const lds_f32x4*)(x + 32 * g + 16 * hb);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) to[4 * g + r] = y[r];
+  }
+  return to;
+}
+
+// One item of the dq (kKeys = false) or the dk, dv side.
 template <int D, bool kKeys>
-__device__ __forceinline__ void run_item(const BwdCall& a, const Found& w, lds_char* lds) {
+__device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_char* lds) {
   using G = Bwd<D>;
   constexpr int kBN = G::kBN;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int col = lane & 31, hb = lane >> 5;
   const int row_bytes = a.H * D * 2;
-  const int held_len = kKeys ? w.nk : w.nq, len = kKeys ? w.nq : w.nk;  // held and streamed rows of the segment
-  const int64_t held0 = ((int64_t)(kKeys ? w.k0 : w.q0) * a.H + w.h) * D, str0 = ((int64_t)(kKeys ? w.q0 : w.k0) * a.H + w.h) * D;
+  const int held_len = w.held_len, len = w.str_len;  // rows of the segment
+  const int64_t held0 = ((int64_t)w.held0 * a.H + w.h) * D, str0 = ((int64_t)w.str0 * a.H + w.h) * D;
   const int row0 = w.tile * kBwdTile + 32 * wave;  // this wave's first held row
 
   // the range of steps
@@ -183,10 +153,10 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Found& w, lds_c
     const __amdgpu_buffer_rsrc_t rx1 = make_rsrc((kKeys ? a.q : a.k) + str0, str_bytes);
     const __amdgpu_buffer_rsrc_t rx2 = make_rsrc((kKeys ? a.d_o : a.v) + str0, str_bytes);
     // the head's statistics of the segment's queries
-    const float* const stat = a.stat + (int64_t)w.h * a.f.total_q + w.q0;
-    const int64_t stat_d = (int64_t)a.H * a.f.total_q;
-    const __amdgpu_buffer_rsrc_t ra = make_rsrc(stat, (uint32_t)w.nq * 4);
-    const __amdgpu_buffer_rsrc_t rd = make_rsrc(stat + stat_d, (uint32_t)w.nq * 4);
+    const float* const stat = a.stat + (int64_t)w.h * a.total_q + (kKeys ? w.str0 : w.held0);
+    const uint32_t stat_bytes = (uint32_t)(kKeys ? len : held_len) * 4;
+    const __amdgpu_buffer_rsrc_t ra = make_rsrc(stat, stat_bytes);
+    const __amdgpu_buffer_rsrc_t rd = make_rsrc(stat + (int64_t)a.H * a.total_q, stat_bytes);
 
     // DMA: instruction i = wave + 8 u of a tile fills LDS bytes [1024 i, 1024 i + 1024), lane l 16 of them; lanes of the
     // pads fetch a row's first chunk again
@@ -249,82 +219,88 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Found& w, lds_c
     const float c = a.c;
     const bool active = row0 < held_len;
 
+    // s becomes P.  kRagged: rows from `left` on are past the segment's end, their P is 0 (and so is R below).
+    auto weights = [&](f32x16& s, auto ragged, int left) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] = __builtin_amdgcn_exp2f(kKeys ? s[r] * c : __builtin_fmaf(s[r], c, la));
+        if (decltype(ragged)::value && 8 * (r >> 2) + 4 * hb + (r & 3) >= left) s[r] = 0.0f;
+      }
+    };
+    auto pack = [&](const f32x16& x, bf16x8 (&to)[2]) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) to[r >> 3][r & 7] = (__bf16)x[r];
+    };
+    auto residuals = [&](const f32x16& p, const f32x16& t, bf16x8 (&to)[2], auto ragged, int left) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float x = p[r] * t[r];
+        if (decltype(ragged)::value && 8 * (r >> 2) + 4 * hb + (r & 3) >= left) x = 0.0f;
+        to[r >> 3][r & 7] = (__bf16)x;
+      }
+    };
+    // One step.  The order is such that the vector work of a block runs under matrix work that does not wait for it.
+    auto step_of = [&](const lds_char* stage, auto ragged, int left) {
+      const lds_char* xr = stage + row_lane;
+      const lds_char* xt = stage + tr_lane;
+      if constexpr (kKeys) {
+        const lds_char* st = stage + G::kStat;
+#pragma unroll 1
+        for (int b = 0; b < kBN / 32; ++b) {
+          f32x16 s = row_statistics(st, hb), t = row_statistics(st + kBN * 4, hb);
+          bf16x8 p[2], ds[2];
+          rows_product<D>(xr, y1, s);
+          rows_product<D>(xr + G::kTile, y2, t);
+          weights(s, ragged, left);
+          pack(s, p);
+          columns_product<D>(xt + G::kTile, p, acc2);
+          residuals(s, t, ds, ragged, left);
+          columns_product<D>(xt, ds, acc1);
+          xr += 8 * G::kGroup;
+          xt += 8 * G::kGroup;
+          st += 128;
+          left -= 32;
+        }
+      } else {
+#pragma unroll 1
+        for (int b = 0; b < kBN / 64; ++b) {
+          f32x16 s0 = {}, s1 = {}, t0, t1;
+          bf16x8 ds0[2], ds1[2];
+#pragma unroll
+          for (int r = 0; r < 16; ++r) t0[r] = ld, t1[r] = ld;
+          rows_product<D>(xr, y1, s0);
+          rows_product<D>(xr + G::kTile, y2, t0);
+          weights(s0, ragged, left);
+          rows_product<D>(xr + 8 * G::kGroup, y1, s1);
+          residuals(s0, t0, ds0, ragged, left);
+          rows_product<D>(xr + G::kTile + 8 * G::kGroup, y2, t1);
+          weights(s1, ragged, left - 32);
+          columns_product<D>(xt, ds0, acc1);
+          residuals(s1, t1, ds1, ragged, left - 32);
+          columns_product<D>(xt + 8 * G::kGroup, ds1, acc1);
+          xr += 16 * G::kGroup;
+          xt += 16 * G::kGroup;
+          left -= 64;
+        }
+      }
+    };
+
     int slot = 0;
-    for (int j = 0; j < steps; ++j) {
+    auto open_step = [&](int j) {  // step j's stage, complete; the fetch of step j + 2
       wait_lds();
       wait_vmem<2 * G::kDmaMin>();  // step j is here, step j + 1 may be on its way
       block_sync();
-      {
-        int to = slot + 2;
-        to -= to >= 3 ? 3 : 0;
-        fetch(j + 2, lds + to * G::kStage);
-      }
       const lds_char* const stage = lds + slot * G::kStage;
-      const lds_char* const xr = stage + row_lane;
-      const lds_char* const xt = stage + tr_lane;
-      const int left = len - (begin + j) * kBN;  // streamed rows from the step's first one on
-      if (active) {
-#pragma unroll 1
-        for (int b = 0; b < kBN / 32; ++b) {
-          f32x16 s = {}, t = {};
-          if (kKeys) {
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
-              const f32x4 x = *(const lds_f32x4*)(stage + G::kStat + (32 * b + 8 * g + 4 * hb) * 4);
-              const f32x4 y = *(const lds_f32x4*)(stage + G::kStat + kBN * 4 + (32 * b + 8 * g + 4 * hb) * 4);
-#pragma unroll
-              for (int r = 0; r < 4; ++r) s[4 * g + r] = x[r], t[4 * g + r] = y[r];
-            }
-          }
-#pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {
-            s = mfma32(*(const lds_bf16x8*)(xr + 8 * b * G::kGroup + 32 * kk), y1[kk], s);
-            t = mfma32(*(const lds_bf16x8*)(xr + G::kTile + 8 * b * G::kGroup + 32 * kk), y2[kk], t);
-          }
-          // the reads of two products ahead of them
-          __builtin_amdgcn_sched_group_barrier(0x100, kKeys ? 12 : 4, 0);
-#pragma unroll
-          for (int i = 0; i < D / 8; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            if (i < D / 8 - 4) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-          }
-          __builtin_amdgcn_sched_barrier(0);
-          bf16x8 p[2], ds[2];
-          const bool whole = left >= 32 * b + 32;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            float e = __builtin_amdgcn_exp2f(kKeys ? s[r] * c : __builtin_fmaf(s[r], c, la));
-            float x = e * (kKeys ? t[r] : t[r] + ld);
-            if (!whole && 32 * b + 8 * (r >> 2) + 4 * hb + (r & 3) >= left) e = x = 0.0f;
-            p[r >> 3][r & 7] = (__bf16)e;
-            ds[r >> 3][r & 7] = (__bf16)x;
-          }
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int db = 0; db < D / 32; ++db) {
-              const lds_char* at = xt + (8 * b + 4 * u) * G::kGroup + 64 * db;
-              bf16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)at);
-              bf16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + 2 * G::kGroup));
-              acc1[db] = mfma32(bf16x8{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]}, ds[u], acc1[db]);
-              if (kKeys) {
-                a0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + G::kTile));
-                a1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + G::kTile + 2 * G::kGroup));
-                acc2[db] = mfma32(bf16x8{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]}, p[u], acc2[db]);
-              }
-            }
-          __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-#pragma unroll
-          for (int i = 0; i < D / 16 * (kKeys ? 2 : 1); ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            if (i < D / 16 * (kKeys ? 2 : 1) - 4) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-          }
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
+      fetch(j + 2, lds + (slot == 0 ? 2 : slot - 1) * G::kStage);
       slot = slot == 2 ? 0 : slot + 1;
+      return stage;
+    };
+    const int whole = min(steps, len / kBN - begin);  // steps without rows past the segment's end: all but the last one
+    if (active) {
+      for (int j = 0; j < whole; ++j) step_of(open_step(j), std::false_type{}, kBN);
+      if (whole < steps) step_of(open_step(whole), std::true_type{}, len - (begin + whole) * kBN);
+    } else {
+      for (int j = 0; j < steps; ++j) open_step(j);
     }
     wait_lds();
     wait_vmem<0>();
@@ -336,7 +312,7 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Found& w, lds_c
   if (row >= held_len) return;
   const float scale = a.scale;
   if (n > 1) {
-    const int64_t rows = (int64_t)(kKeys ? a.f.total_k : a.f.total_q) * a.H * D;
+    const int64_t rows = (int64_t)(kKeys ? a.total_k : a.total_q) * a.H * D;
     float* const to = (kKeys ? a.part_k : a.part_q) + w.split * rows + held0 + (int64_t)row * a.H * D + 4 * hb;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
@@ -366,28 +342,89 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Found& w, lds_c
     }
 }
 
-template <int D>
+template <int D, bool kKeys>
 __global__ __launch_bounds__(kThreads, 2) void attn_bwd_kernel(BwdCall a) {
   extern __shared__ char smem[];
-  const int lane = threadIdx.x & 63;
-  int tiles_q, tiles_k;
-  count_tiles(a.f, lane, tiles_q, tiles_k);
-  const int total = tiles_q * a.H * a.n_q + tiles_k * a.H * a.n_k;
-  for (int b = blockIdx.x; b < total; b += gridDim.x) {
-    Found w;
-    if (!find_item(a, remap_block(b, total, 32), tiles_q, tiles_k, lane, w)) break;
-    if (w.keys) run_item<D, true>(a, w, (lds_char*)smem);
-    else run_item<D, false>(a, w, (lds_char*)smem);
-  }
+  const int n = kKeys ? a.n_k : a.n_q;
+  const int total = (kKeys ? a.plan->tiles_k : a.plan->tiles_q) * a.H * n;
+  if ((int)blockIdx.x >= total) return;
+  const BwdTile* const tiles = (const BwdTile*)(a.plan + 1) + (kKeys ? a.most_q : 0);
+  run_item<D, kKeys>(a, find_item(tiles, remap_block(blockIdx.x, total, 32), a.H, n), (lds_char*)smem);
 }
 
-// -lse / scale and -D of every query and head, [2][H][total_q]: 64 tokens of one head to a workgroup, a row of d bf16 to
-// d / 8 lanes.
+// The tiles of both sides (see BwdPlan), by one workgroup.  A side's segments are taken longest streamed side first, up to
+// kSorted of them; more keep their order.  Offsets that break the rules leave a plan without tiles.
+constexpr int kPlanThreads = 256, kSorted = 1024;
+
+__device__ __forceinline__ int wave_sum_to(int x, int lane) {  // inclusive prefix sum over the lanes
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
+__device__ __forceinline__ void plan_side(const int32_t* cu_held, const int32_t* cu_str, int nseq, BwdTile* to, int32_t* count,
+                                          int* len, int* order, int* part) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const bool sorted = nseq > 1 && nseq <= kSorted;
+  if (sorted) {
+    for (int s = tid; s < nseq; s += kPlanThreads) len[s] = cu_str[s + 1] - cu_str[s];
+    __syncthreads();
+    for (int s = tid; s < nseq; s += kPlanThreads) {
+      const int mine = len[s];
+      int rank = 0;
+      for (int i = 0; i < nseq; ++i) rank += len[i] > mine || (len[i] == mine && i < s);
+      order[rank] = s;
+    }
+    __syncthreads();
+  }
+  int before = 0;  // tiles of the segments before this round's
+  for (int i0 = 0; i0 < nseq; i0 += kPlanThreads) {
+    const int i = i0 + tid, s = i < nseq ? sorted ? order[i] : i : 0;
+    const int held0 = cu_held[s], n = i < nseq ? cu_held[s + 1] - held0 : 0, tiles = (n + kBwdTile - 1) / kBwdTile;
+    const int upto = wave_sum_to(tiles, lane);
+    __syncthreads();  // (the round before has read its sums)
+    if (lane == 63) part[wave] = upto;
+    __syncthreads();
+    int first = before + upto - tiles;
+    for (int w = 0; w < wave; ++w) first += part[w];
+    for (int w = 0; w < kPlanThreads / 64; ++w) before += part[w];
+    const int str0 = cu_str[s];
+    for (int t = 0; t < tiles; ++t) to[first + t] = BwdTile{held0, n, str0, cu_str[s + 1] - str0, first, tiles, {}};
+  }
+  if (tid == 0) *count = before;
+}
+
+__device__ void make_plan(BwdPlan* plan, BwdOffsets f, int most_q) {
+  __shared__ int len[kSorted], order[kSorted], part[kPlanThreads / 64];
+  bool bad = false;
+  for (int s = threadIdx.x; s < f.nseq; s += kPlanThreads) {
+    const int q0 = f.cu_q[s], q1 = f.cu_q[s + 1], k0 = f.cu_k[s], k1 = f.cu_k[s + 1];
+    // (differences of ascending offsets from 0 to the totals do not overflow; others are bad by themselves)
+    bad |= q0 < 0 || q1 < q0 || q1 > f.total_q || q1 - q0 > f.max_q || k0 < 0 || k1 < k0 || k1 > f.total_k || k1 - k0 > f.max_k;
+    bad |= s == 0 && (q0 != 0 || k0 != 0);
+    bad |= s == f.nseq - 1 && (q1 != f.total_q || k1 != f.total_k);
+  }
+  if (__syncthreads_or(bad)) {
+    if (threadIdx.x == 0) plan->tiles_q = plan->tiles_k = 0;
+    return;
+  }
+  BwdTile* const tiles = (BwdTile*)(plan + 1);
+  plan_side(f.cu_q, f.cu_k, f.nseq, tiles, &plan->tiles_q, len, order, part);
+  __syncthreads();
+  plan_side(f.cu_k, f.cu_q, f.nseq, tiles + most_q, &plan->tiles_k, len, order, part);
+}
+
+// Before the gradients: the plan, by workgroup 0, and by the others -lse / scale and -D of every query and head,
+// [2][H][total_q], 64 tokens of one head to a workgroup and a row of d bf16 to d / 8 lanes.
 template <int D>
-__global__ __launch_bounds__(256) void bwd_stat_kernel(const __bf16* d_o, const __bf16* o, const float* lse, float* stat, int T,
-                                                       int H, float inv) {
-  constexpr int kLanes = D / 8, kRows = 256 / kLanes;
-  const int h = blockIdx.x % H, t0 = blockIdx.x / H * 64;
+__global__ __launch_bounds__(kPlanThreads) void bwd_prepare_kernel(const __bf16* d_o, const __bf16* o, const float* lse, float* stat,
+                                                                   int T, int H, float inv, BwdPlan* plan, BwdOffsets f, int most_q) {
+  if (blockIdx.x == 0) return make_plan(plan, f, most_q);
+  constexpr int kLanes = D / 8, kRows = kPlanThreads / kLanes;
+  const int h = (blockIdx.x - 1) % H, t0 = (blockIdx.x - 1) / H * 64;
   const int r = threadIdx.x / kLanes, i = threadIdx.x % kLanes;
 #pragma unroll
   for (int u = 0; u < 64 / kRows; ++u) {
@@ -407,34 +444,29 @@ __global__ __launch_bounds__(256) void bwd_stat_kernel(const __bf16* d_o, const 
   }
 }
 
-// Sums of the ranges' partial gradients, in order.  Workgroups take the tiles of the segments, as attn_bwd_kernel does.
+// Sums of the ranges' partial gradients, in order: 16 rows of a head to a workgroup.  (Rows are those of the plan's segments,
+// which are all rows, or none.)
+constexpr int kJoinRows = 16;
+
 template <int D>
-__global__ __launch_bounds__(256) void bwd_join_kernel(BwdCall a) {
-  const int lane = threadIdx.x & 63;
-  int tiles_q, tiles_k;
-  count_tiles(a.f, lane, tiles_q, tiles_k);
-  BwdCall whole = a;
-  whole.n_q = whole.n_k = 1;
-  const int total = (tiles_q + tiles_k) * a.H;
-  for (int b = blockIdx.x; b < total; b += gridDim.x) {
-    Found w;
-    if (!find_item(whole, b, tiles_q, tiles_k, lane, w)) break;
-    const int n = w.keys ? a.n_k : a.n_q;
-    if (n == 1) continue;
-    const int64_t rows = (int64_t)(w.keys ? a.f.total_k : a.f.total_q) * a.H * D;
-    const int64_t start = ((int64_t)(w.keys ? w.k0 : w.q0) * a.H + w.h) * D;
-    const int end = min(w.keys ? w.nk : w.nq, (w.tile + 1) * kBwdTile);
-    constexpr int kLanes = D / 4;
-    for (int r = w.tile * kBwdTile + threadIdx.x / kLanes; r < end; r += 256 / kLanes) {
-      const int64_t at = start + (int64_t)r * a.H * D + 4 * (threadIdx.x % kLanes);
-      for (int which = 0; which < (w.keys ? 2 : 1); ++which) {
-        const float* p = (w.keys ? a.part_k + which * n * rows : a.part_q) + at;
-        f32x4 sum = *(const f32x4*)p;
-        for (int i = 1; i < n; ++i) sum += *(const f32x4*)(p + i * rows);
-        const float f = which == 1 ? 1.0f : a.scale;
-        __bf16* const to = !w.keys ? a.dq : which == 1 ? a.dv : a.dk;
-        *(bf16x4*)(to + at) = bf16x4{(__bf16)(sum[0] * f), (__bf16)(sum[1] * f), (__bf16)(sum[2] * f), (__bf16)(sum[3] * f)};
-      }
+__global__ __launch_bounds__(256) void bwd_join_kernel(BwdCall a, int blocks_k) {
+  if (a.plan->tiles_q + a.plan->tiles_k == 0) return;
+  const bool keys = (int)blockIdx.x < blocks_k;
+  const int b = keys ? blockIdx.x : blockIdx.x - blocks_k, n = keys ? a.n_k : a.n_q;
+  const int64_t all = (int64_t)(keys ? a.total_k : a.total_q) * a.H, row0 = (int64_t)b * kJoinRows;
+  constexpr int kLanes = D / 4;
+#pragma unroll
+  for (int u = 0; u < kJoinRows * kLanes / 256; ++u) {
+    const int64_t row = row0 + 256 / kLanes * u + threadIdx.x / kLanes;
+    if (row >= all) return;
+    const int64_t at = row * D + 4 * (threadIdx.x % kLanes);
+    for (int which = 0; which < (keys ? 2 : 1); ++which) {
+      const float* p = (keys ? a.part_k + which * n * all * D : a.part_q) + at;
+      f32x4 sum = *(const f32x4*)p;
+      for (int i = 1; i < n; ++i) sum += *(const f32x4*)(p + i * all * D);
+      const float f = which == 1 ? 1.0f : a.scale;
+      __bf16* const to = !keys ? a.dq : which == 1 ? a.dv : a.dk;
+      *(bf16x4*)(to + at) = bf16x4{(__bf16)(sum[0] * f), (__bf16)(sum[1] * f), (__bf16)(sum[2] * f), (__bf16)(sum[3] * f)};
     }
   }
 }
@@ -442,17 +474,19 @@ __global__ __launch_bounds__(256) void bwd_join_kernel(BwdCall a) {
 template <int D>
 hipError_t launch(const BwdArgs& x, hipStream_t st) {
   const float s = x.scale == 0.0f ? 1.0f : x.scale;
+  const int most_q = (int)bwd_tiles(x.nseq, x.max_q, x.total_q), most_k = (int)bwd_tiles(x.nseq, x.max_k, x.total_k);
   const BwdCall a{(const __bf16*)x.d_o, (const __bf16*)x.q, (const __bf16*)x.k, (const __bf16*)x.v, x.stat,
-                  (__bf16*)x.dq, (__bf16*)x.dk, (__bf16*)x.dv, x.part_q, x.part_k,
-                  {x.cu_q, x.cu_k, x.nseq, x.max_q, x.max_k, x.total_q, x.total_k}, x.H, x.n_q, x.n_k,
-                  3ll * x.max_k * x.n_k >= 4ll * x.max_q * x.n_q, x.scale, s * kLog2e};
+                  (__bf16*)x.dq, (__bf16*)x.dk, (__bf16*)x.dv, x.part_q, x.part_k, x.plan,
+                  x.total_q, x.total_k, x.H, x.n_q, x.n_k, most_q, x.scale, s * kLog2e};
   const int64_t stats = ((int64_t)x.total_q + 63) / 64 * x.H;
-  if (stats > 0)
-    bwd_stat_kernel<D><<<(unsigned)stats, 256, 0, st>>>(a.d_o, (const __bf16*)x.o, x.lse, x.stat, x.total_q, x.H, 1.0f / s);
-  const int64_t tiles_q = bwd_tiles(x.nseq, x.max_q, x.total_q, x.H), tiles_k = bwd_tiles(x.nseq, x.max_k, x.total_k, x.H);
-  const int64_t items = std::min<int64_t>(tiles_q * x.n_q + tiles_k * x.n_k, kBwdGrid);
-  if (items > 0) attn_bwd_kernel<D><<<(unsigned)items, kThreads, Bwd<D>::kLds, st>>>(a);
-  if (items > 0 && (x.n_q > 1 || x.n_k > 1)) bwd_join_kernel<D><<<(unsigned)(tiles_q + tiles_k), 256, 0, st>>>(a);
+  bwd_prepare_kernel<D><<<(unsigned)(1 + stats), kPlanThreads, 0, st>>>(
+      a.d_o, (const __bf16*)x.o, x.lse, x.stat, x.total_q, x.H, 1.0f / s, x.plan,
+      BwdOffsets{x.cu_q, x.cu_k, x.nseq, x.max_q, x.max_k, x.total_q, x.total_k}, most_q);
+  if (most_k > 0) attn_bwd_kernel<D, true><<<(unsigned)((int64_t)most_k * x.H * x.n_k), kThreads, Bwd<D>::kLds, st>>>(a);
+  if (most_q > 0) attn_bwd_kernel<D, false><<<(unsigned)((int64_t)most_q * x.H * x.n_q), kThreads, Bwd<D>::kLds, st>>>(a);
+  const int64_t join_k = x.n_k > 1 ? ((int64_t)x.total_k * x.H + kJoinRows - 1) / kJoinRows : 0;
+  const int64_t join_q = x.n_q > 1 ? ((int64_t)x.total_q * x.H + kJoinRows - 1) / kJoinRows : 0;
+  if (join_k + join_q > 0) bwd_join_kernel<D><<<(unsigned)(join_k + join_q), 256, 0, st>>>(a, (int)join_k);
   return hipGetLastError();
 }
 
@@ -461,9 +495,11 @@ hipError_t launch_attn_bwd(const BwdArgs& a, hipStream_t st) {
 }
 
 hipError_t configure_kernels() {
-  hipError_t e = hipFuncSetAttribute((const void*)attn_bwd_kernel<64>, hipFuncAttributeMaxDynamicSharedMemorySize, Bwd<64>::kLds);
-  if (e == hipSuccess)
-    e = hipFuncSetAttribute((const void*)attn_bwd_kernel<128>, hipFuncAttributeMaxDynamicSharedMemorySize, Bwd<128>::kLds);
+  auto allow = [](const void* f, int bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); };
+  hipError_t e = allow((const void*)attn_bwd_kernel<64, true>, Bwd<64>::kLds);
+  if (e == hipSuccess) e = allow((const void*)attn_bwd_kernel<64, false>, Bwd<64>::kLds);
+  if (e == hipSuccess) e = allow((const void*)attn_bwd_kernel<128, true>, Bwd<128>::kLds);
+  if (e == hipSuccess) e = allow((const void*)attn_bwd_kernel<128, false>, Bwd<128>::kLds);
   return e;
 }
 

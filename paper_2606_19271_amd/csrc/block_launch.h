@@ -46,6 +46,24 @@ constexpr int kRopeThreads = 256;
 // The workgroups of a gradient call with weights, whatever the device: its sums' order goes by them.
 int32_t rope_bwd_blocks(int32_t T, int32_t q_heads, int32_t k_heads, int32_t d);
 
+// A tile of kBwdTile held rows of a segment (queries for dq, keys for dk and dv), and the rows that stream past it.
+// The segment's `tiles` tiles follow each other from `first` on; a tile's number is its place among them.
+struct BwdTile {
+  int32_t held0, held_len, str0, str_len;  // the segment's rows of either side
+  int32_t first, tiles;
+  int32_t unused[2];
+};
+// Ahead of the tiles of the queries' side, most_q of them at most, and those of the keys' side.
+struct BwdPlan {
+  int32_t tiles_q, tiles_k;
+  int32_t unused[6];
+};
+struct BwdOffsets {
+  const int32_t* cu_q;
+  const int32_t* cu_k;
+  int32_t nseq, max_q, max_k, total_q, total_k;
+};
+
 struct BwdArgs {
   const void* d_o;
   const void* q;
@@ -58,6 +76,7 @@ struct BwdArgs {
   void* dv;
   const int32_t* cu_q;
   const int32_t* cu_k;
+  BwdPlan* plan;
   float* stat;     // [2][H][total_q]: -lse / scale, -D
   float* part_q;   // [n_q][total_q][H][d], where n_q > 1
   float* part_k;   // [n_k][total_k][H][d] of dk, then of dv, where n_k > 1
@@ -67,19 +86,18 @@ struct BwdArgs {
 };
 
 constexpr int kBwdTile = 256;  // queries (dq) or keys (dk, dv) of a workgroup
-constexpr int64_t kBwdGrid = (int64_t)1 << 22;  // workgroups of a launch, which take more items than one where there are more
 // Rows of the other side that a workgroup holds in LDS at a time.
 constexpr int bwd_step(int d) { return d == 64 ? 128 : 64; }
 
 // How a call is divided: the keys of a query tile in n_q ranges, the queries of a key tile in n_k; the workspace's layout.
 struct BwdParts {
   int32_t n_q, n_k;
-  int64_t q_offset, k_offset, bytes;
+  int64_t stat_offset, q_offset, k_offset, bytes;  // the plan comes first
 };
 BwdParts bwd_parts(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d,
                    int32_t num_splits, int64_t workspace, int32_t cus);
-// Upper bounds of the tiles of one side over all segments and heads.
-int64_t bwd_tiles(int32_t nseq, int32_t most, int32_t total, int32_t H);
+// An upper bound of the tiles of one side over all segments: sum of ceil(len / kBwdTile).
+int64_t bwd_tiles(int32_t nseq, int32_t most, int32_t total);
 
 hipError_t configure_kernels();
 hipError_t launch_rope(const RopeArgs& a, hipStream_t st);

@@ -168,7 +168,7 @@ int check_sizes(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int
   // H < 2^24 and tiles < 2^24 from here on, so the products below are within 64 bits
   const int64_t tiles = (int64_t)max_q / tsblock::kBwdTile + max_k / tsblock::kBwdTile + 2;
   if ((int64_t)nseq * H >= (int64_t)1 << 26 || (int64_t)nseq * H * tiles >= (int64_t)1 << 26) return TS_ERR_SHAPE;
-  if (H * ((int64_t)std::max(total_q, total_k) / tsblock::kBwdTile + nseq) >= (int64_t)1 << 21) return TS_ERR_SHAPE;
+  if (H * ((int64_t)std::max(total_q, total_k) / tsblock::kBwdTile + nseq) >= (int64_t)1 << 19) return TS_ERR_SHAPE;
   return TS_OK;
 }
 
@@ -279,8 +279,8 @@ int ts_attn_bwd(const void* d_o, const void* q, const void* k, const void* v, co
     return rc;
   const tsblock::BwdParts p = parts_on(st->cus);
   char* const w = (char*)workspace;
-  return launched(tsblock::launch_attn_bwd({d_o, q, k, v, o, lse, dq, dk, dv, cu_seqlens_q, cu_seqlens_k, (float*)w,
-                                            (float*)(w + p.q_offset), (float*)(w + p.k_offset), nseq, max_seqlen_q, max_seqlen_k,
+  return launched(tsblock::launch_attn_bwd({d_o, q, k, v, o, lse, dq, dk, dv, cu_seqlens_q, cu_seqlens_k, (tsblock::BwdPlan*)w,
+                                            (float*)(w + p.stat_offset), (float*)(w + p.q_offset), (float*)(w + p.k_offset), nseq, max_seqlen_q, max_seqlen_k,
                                             total_q, total_k, H, d, p.n_q, p.n_k, scale}, s));
 }
 
