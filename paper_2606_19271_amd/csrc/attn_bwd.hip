@@ -55,7 +55,7 @@ struct BwdCall {
   float* part_q;
   float* part_k;
   const BwdPlan* plan;
-  int total_q, total_k, H, n_q, n_k, most_q;
+  int total_q, total_k, H, n_q, n_k;
   float scale, c;  // c: log2(e) times the scale, or log2(e) for a scale of 0
 };
 
@@ -67,11 +67,10 @@ struct Item {
   int held0, held_len, str0, str_len;
 };
 
-// Item `at` of one side, whose tiles each have `heads` * n items.  They go by segment, head, range and tile, so that
-// neighbours stream the same rows.
-__device__ __forceinline__ Item find_item(const BwdTile* tiles, int at, int heads, int n) {
-  const BwdTile* const t = tiles + at / (heads * n);  // (any tile of the item's segment)
-  at -= t->first * heads * n;
+// Item `at` of the list of entry t, of a side with n ranges.  Its head, range and tile go by the list's own order over the XCDs,
+// so that each of them gets an equal part of every list, and neighbours on it stream the same rows.
+__device__ __forceinline__ Item find_item(const BwdTile* t, int at, int heads, int n) {
+  at = remap_block(at - t->first * heads, t->tiles * n * heads, 32);
   Item w;
   const int j = at / t->tiles;
   w.tile = at - j * t->tiles;
@@ -342,18 +341,21 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
     }
 }
 
-template <int D, bool kKeys>
+template <int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_bwd_kernel(BwdCall a) {
   extern __shared__ char smem[];
-  const int n = kKeys ? a.n_k : a.n_q;
-  const int total = (kKeys ? a.plan->tiles_k : a.plan->tiles_q) * a.H * n;
+  const int total = a.plan->tiles * a.H;
   if ((int)blockIdx.x >= total) return;
-  const BwdTile* const tiles = (const BwdTile*)(a.plan + 1) + (kKeys ? a.most_q : 0);
-  run_item<D, kKeys>(a, find_item(tiles, remap_block(blockIdx.x, total, 32), a.H, n), (lds_char*)smem);
+  const int item = blockIdx.x;
+  const BwdTile* const t = (const BwdTile*)(a.plan + 1) + item / a.H;  // (any of the item's list)
+  if (t->keys) run_item<D, true>(a, find_item(t, item, a.H, a.n_k), (lds_char*)smem);
+  else run_item<D, false>(a, find_item(t, item, a.H, a.n_q), (lds_char*)smem);
 }
 
-// The tiles of both sides (see BwdPlan), by one workgroup.  A side's segments are taken longest streamed side first, up to
-// kSorted of them; more keep their order.  Offsets that break the rules leave a plan without tiles.
+// The plan: the tiles of all segments' queries (for dq) and keys (for dk and dv), each once for every range of its
+// streamed side.  Of these lists, one for each segment and side, the one with the longest items comes first, where
+// there are up to kSorted of them; more keep their order.  One workgroup makes it.  Offsets that break the rules leave it
+// empty.
 constexpr int kPlanThreads = 256, kSorted = 1024;
 
 __device__ __forceinline__ int wave_sum_to(int x, int lane) {  // inclusive prefix sum over the lanes
@@ -365,64 +367,77 @@ __device__ __forceinline__ int wave_sum_to(int x, int lane) {  // inclusive pref
   return x;
 }
 
-__device__ __forceinline__ void plan_side(const int32_t* cu_held, const int32_t* cu_str, int nseq, BwdTile* to, int32_t* count,
-                                          int* len, int* order, int* part) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const bool sorted = nseq > 1 && nseq <= kSorted;
-  if (sorted) {
-    for (int s = tid; s < nseq; s += kPlanThreads) len[s] = cu_str[s + 1] - cu_str[s];
+__device__ void make_plan(BwdPlan* plan, BwdOffsets f, int n_q, int n_k) {
+  __shared__ int cost[kSorted], order[kSorted], part[kPlanThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lists = 2 * f.nseq;
+  bool bad = false;
+  for (int s = tid; s < f.nseq; s += kPlanThreads) {
+    const int q0 = f.cu_q[s], q1 = f.cu_q[s + 1], k0 = f.cu_k[s], k1 = f.cu_k[s + 1];
+    // (differences of offsets within 0 and the totals do not overflow)
+    bad |= q0 < 0 || q1 < q0 || q1 > f.total_q || k0 < 0 || k1 < k0 || k1 > f.total_k;
+    if (!bad) {
+      bad |= q1 - q0 > f.max_q || k1 - k0 > f.max_k;
+      bad |= s == 0 && (q0 != 0 || k0 != 0);
+      bad |= s == f.nseq - 1 && (q1 != f.total_q || k1 != f.total_k);
+    }
+  }
+  if (__syncthreads_or(bad)) {
+    if (tid == 0) plan->tiles = 0;
+    return;
+  }
+  // list i: the keys of segment i / 2 for an even i, else its queries
+  auto list = [&](int i, BwdTile& t) {
+    const int s = i >> 1;
+    t.keys = !(i & 1);
+    t.held0 = t.keys ? f.cu_k[s] : f.cu_q[s];
+    t.str0 = t.keys ? f.cu_q[s] : f.cu_k[s];
+    t.held_len = (t.keys ? f.cu_k[s + 1] : f.cu_q[s + 1]) - t.held0;
+    t.str_len = (t.keys ? f.cu_q[s + 1] : f.cu_k[s + 1]) - t.str0;
+    t.tiles = (t.held_len + kBwdTile - 1) / kBwdTile;
+  };
+  const bool sorted = lists <= kSorted;
+  if (sorted) {  // by the products of an item: four of a step's rows for dk and dv, three for dq
+    for (int i = tid; i < lists; i += kPlanThreads) {
+      BwdTile t;
+      list(i, t);
+      cost[i] = t.tiles ? t.keys ? 4 * (t.str_len / n_k) : 3 * (t.str_len / n_q) : -1;
+    }
     __syncthreads();
-    for (int s = tid; s < nseq; s += kPlanThreads) {
-      const int mine = len[s];
+    for (int i = tid; i < lists; i += kPlanThreads) {
+      const int mine = cost[i];
       int rank = 0;
-      for (int i = 0; i < nseq; ++i) rank += len[i] > mine || (len[i] == mine && i < s);
-      order[rank] = s;
+      for (int j = 0; j < lists; ++j) rank += cost[j] > mine || (cost[j] == mine && j < i);
+      order[rank] = i;
     }
     __syncthreads();
   }
-  int before = 0;  // tiles of the segments before this round's
-  for (int i0 = 0; i0 < nseq; i0 += kPlanThreads) {
-    const int i = i0 + tid, s = i < nseq ? sorted ? order[i] : i : 0;
-    const int held0 = cu_held[s], n = i < nseq ? cu_held[s + 1] - held0 : 0, tiles = (n + kBwdTile - 1) / kBwdTile;
-    const int upto = wave_sum_to(tiles, lane);
+  BwdTile* const to = (BwdTile*)(plan + 1);
+  int before = 0;  // tiles of the lists before this round's
+  for (int i0 = 0; i0 < lists; i0 += kPlanThreads) {
+    const int i = i0 + tid;
+    BwdTile t{};
+    if (i < lists) list(sorted ? order[i] : i, t);
+    const int n = t.tiles * (t.keys ? n_k : n_q);
+    const int upto = wave_sum_to(n, lane);
     __syncthreads();  // (the round before has read its sums)
     if (lane == 63) part[wave] = upto;
     __syncthreads();
-    int first = before + upto - tiles;
-    for (int w = 0; w < wave; ++w) first += part[w];
-    for (int w = 0; w < kPlanThreads / 64; ++w) before += part[w];
-    const int str0 = cu_str[s];
-    for (int t = 0; t < tiles; ++t) to[first + t] = BwdTile{held0, n, str0, cu_str[s + 1] - str0, first, tiles, {}};
+    t.first = before + upto - n;
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
+      if (w < wave) t.first += part[w];
+      before += part[w];
+    }
+    for (int j = 0; j < n; ++j) to[t.first + j] = t;
   }
-  if (tid == 0) *count = before;
-}
-
-__device__ void make_plan(BwdPlan* plan, BwdOffsets f, int most_q) {
-  __shared__ int len[kSorted], order[kSorted], part[kPlanThreads / 64];
-  bool bad = false;
-  for (int s = threadIdx.x; s < f.nseq; s += kPlanThreads) {
-    const int q0 = f.cu_q[s], q1 = f.cu_q[s + 1], k0 = f.cu_k[s], k1 = f.cu_k[s + 1];
-    // (differences of ascending offsets from 0 to the totals do not overflow; others are bad by themselves)
-    bad |= q0 < 0 || q1 < q0 || q1 > f.total_q || q1 - q0 > f.max_q || k0 < 0 || k1 < k0 || k1 > f.total_k || k1 - k0 > f.max_k;
-    bad |= s == 0 && (q0 != 0 || k0 != 0);
-    bad |= s == f.nseq - 1 && (q1 != f.total_q || k1 != f.total_k);
-  }
-  if (__syncthreads_or(bad)) {
-    if (threadIdx.x == 0) plan->tiles_q = plan->tiles_k = 0;
-    return;
-  }
-  BwdTile* const tiles = (BwdTile*)(plan + 1);
-  plan_side(f.cu_q, f.cu_k, f.nseq, tiles, &plan->tiles_q, len, order, part);
-  __syncthreads();
-  plan_side(f.cu_k, f.cu_q, f.nseq, tiles + most_q, &plan->tiles_k, len, order, part);
+  if (tid == 0) plan->tiles = before;
 }
 
 // Before the gradients: the plan, by workgroup 0, and by the others -lse / scale and -D of every query and head,
 // [2][H][total_q], 64 tokens of one head to a workgroup and a row of d bf16 to d / 8 lanes.
 template <int D>
 __global__ __launch_bounds__(kPlanThreads) void bwd_prepare_kernel(const __bf16* d_o, const __bf16* o, const float* lse, float* stat,
-                                                                   int T, int H, float inv, BwdPlan* plan, BwdOffsets f, int most_q) {
-  if (blockIdx.x == 0) return make_plan(plan, f, most_q);
+                                                                   int T, int H, float inv, BwdPlan* plan, BwdOffsets f, int n_q, int n_k) {
+  if (blockIdx.x == 0) return make_plan(plan, f, n_q, n_k);
   constexpr int kLanes = D / 8, kRows = kPlanThreads / kLanes;
   const int h = (blockIdx.x - 1) % H, t0 = (blockIdx.x - 1) / H * 64;
   const int r = threadIdx.x / kLanes, i = threadIdx.x % kLanes;
@@ -444,29 +459,40 @@ __global__ __launch_bounds__(kPlanThreads) void bwd_prepare_kernel(const __bf16*
   }
 }
 
-// Sums of the ranges' partial gradients, in order: 16 rows of a head to a workgroup.  (Rows are those of the plan's segments,
-// which are all rows, or none.)
+// Sums of the ranges' partial gradients, in order: 16 rows of a head to a workgroup, 4 channels to a thread.  (A plan that is not empty
+// covers all rows.)
 constexpr int kJoinRows = 16;
 
 template <int D>
 __global__ __launch_bounds__(256) void bwd_join_kernel(BwdCall a, int blocks_k) {
-  if (a.plan->tiles_q + a.plan->tiles_k == 0) return;
+  if (a.plan->tiles == 0) return;
   const bool keys = (int)blockIdx.x < blocks_k;
   const int b = keys ? blockIdx.x : blockIdx.x - blocks_k, n = keys ? a.n_k : a.n_q;
   const int64_t all = (int64_t)(keys ? a.total_k : a.total_q) * a.H, row0 = (int64_t)b * kJoinRows;
-  constexpr int kLanes = D / 4;
+  constexpr int kLanes = D / 4, kRows = 256 / kLanes;
+  const int64_t step = all * D;
+  auto sum = [&](const float* p) {
+    f32x4 x = *(const f32x4*)p;
+    int i = 1;
+    for (; i + 3 < n; i += 4) {  // four reads under way
+      const f32x4 y0 = *(const f32x4*)(p + i * step), y1 = *(const f32x4*)(p + (i + 1) * step),
+                  y2 = *(const f32x4*)(p + (i + 2) * step), y3 = *(const f32x4*)(p + (i + 3) * step);
+      x = x + y0 + y1 + y2 + y3;
+    }
+    for (; i < n; ++i) x += *(const f32x4*)(p + i * step);
+    return x;
+  };
+  auto narrow = [](f32x4 x, float f) { return bf16x4{(__bf16)(x[0] * f), (__bf16)(x[1] * f), (__bf16)(x[2] * f), (__bf16)(x[3] * f)}; };
 #pragma unroll
-  for (int u = 0; u < kJoinRows * kLanes / 256; ++u) {
-    const int64_t row = row0 + 256 / kLanes * u + threadIdx.x / kLanes;
+  for (int u = 0; u < kJoinRows / kRows; ++u) {
+    const int64_t row = row0 + kRows * u + threadIdx.x / kLanes;
     if (row >= all) return;
     const int64_t at = row * D + 4 * (threadIdx.x % kLanes);
-    for (int which = 0; which < (keys ? 2 : 1); ++which) {
-      const float* p = (keys ? a.part_k + which * n * all * D : a.part_q) + at;
-      f32x4 sum = *(const f32x4*)p;
-      for (int i = 1; i < n; ++i) sum += *(const f32x4*)(p + i * all * D);
-      const float f = which == 1 ? 1.0f : a.scale;
-      __bf16* const to = !keys ? a.dq : which == 1 ? a.dv : a.dk;
-      *(bf16x4*)(to + at) = bf16x4{(__bf16)(sum[0] * f), (__bf16)(sum[1] * f), (__bf16)(sum[2] * f), (__bf16)(sum[3] * f)};
+    if (keys) {
+      *(bf16x4*)(a.dk + at) = narrow(sum(a.part_k + at), a.scale);
+      *(bf16x4*)(a.dv + at) = narrow(sum(a.part_k + n * step + at), 1.0f);
+    } else {
+      *(bf16x4*)(a.dq + at) = narrow(sum(a.part_q + at), a.scale);
     }
   }
 }
@@ -474,16 +500,15 @@ __global__ __launch_bounds__(256) void bwd_join_kernel(BwdCall a, int blocks_k) 
 template <int D>
 hipError_t launch(const BwdArgs& x, hipStream_t st) {
   const float s = x.scale == 0.0f ? 1.0f : x.scale;
-  const int most_q = (int)bwd_tiles(x.nseq, x.max_q, x.total_q), most_k = (int)bwd_tiles(x.nseq, x.max_k, x.total_k);
   const BwdCall a{(const __bf16*)x.d_o, (const __bf16*)x.q, (const __bf16*)x.k, (const __bf16*)x.v, x.stat,
                   (__bf16*)x.dq, (__bf16*)x.dk, (__bf16*)x.dv, x.part_q, x.part_k, x.plan,
-                  x.total_q, x.total_k, x.H, x.n_q, x.n_k, most_q, x.scale, s * kLog2e};
+                  x.total_q, x.total_k, x.H, x.n_q, x.n_k, x.scale, s * kLog2e};
   const int64_t stats = ((int64_t)x.total_q + 63) / 64 * x.H;
   bwd_prepare_kernel<D><<<(unsigned)(1 + stats), kPlanThreads, 0, st>>>(
       a.d_o, (const __bf16*)x.o, x.lse, x.stat, x.total_q, x.H, 1.0f / s, x.plan,
-      BwdOffsets{x.cu_q, x.cu_k, x.nseq, x.max_q, x.max_k, x.total_q, x.total_k}, most_q);
-  if (most_k > 0) attn_bwd_kernel<D, true><<<(unsigned)((int64_t)most_k * x.H * x.n_k), kThreads, Bwd<D>::kLds, st>>>(a);
-  if (most_q > 0) attn_bwd_kernel<D, false><<<(unsigned)((int64_t)most_q * x.H * x.n_q), kThreads, Bwd<D>::kLds, st>>>(a);
+      BwdOffsets{x.cu_q, x.cu_k, x.nseq, x.max_q, x.max_k, x.total_q, x.total_k}, x.n_q, x.n_k);
+  const int64_t items = x.H * (bwd_tiles(x.nseq, x.max_q, x.total_q) * x.n_q + bwd_tiles(x.nseq, x.max_k, x.total_k) * x.n_k);
+  if (items > 0) attn_bwd_kernel<D><<<(unsigned)items, kThreads, Bwd<D>::kLds, st>>>(a);
   const int64_t join_k = x.n_k > 1 ? ((int64_t)x.total_k * x.H + kJoinRows - 1) / kJoinRows : 0;
   const int64_t join_q = x.n_q > 1 ? ((int64_t)x.total_q * x.H + kJoinRows - 1) / kJoinRows : 0;
   if (join_k + join_q > 0) bwd_join_kernel<D><<<(unsigned)(join_k + join_q), 256, 0, st>>>(a, (int)join_k);
@@ -496,10 +521,8 @@ hipError_t launch_attn_bwd(const BwdArgs& a, hipStream_t st) {
 
 hipError_t configure_kernels() {
   auto allow = [](const void* f, int bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); };
-  hipError_t e = allow((const void*)attn_bwd_kernel<64, true>, Bwd<64>::kLds);
-  if (e == hipSuccess) e = allow((const void*)attn_bwd_kernel<64, false>, Bwd<64>::kLds);
-  if (e == hipSuccess) e = allow((const void*)attn_bwd_kernel<128, true>, Bwd<128>::kLds);
-  if (e == hipSuccess) e = allow((const void*)attn_bwd_kernel<128, false>, Bwd<128>::kLds);
+  hipError_t e = allow((const void*)attn_bwd_kernel<64>, Bwd<64>::kLds);
+  if (e == hipSuccess) e = allow((const void*)attn_bwd_kernel<128>, Bwd<128>::kLds);
   return e;
 }
 

@@ -46,17 +46,17 @@ constexpr int kRopeThreads = 256;
 // The workgroups of a gradient call with weights, whatever the device: its sums' order goes by them.
 int32_t rope_bwd_blocks(int32_t T, int32_t q_heads, int32_t k_heads, int32_t d);
 
-// A tile of kBwdTile held rows of a segment (queries for dq, keys for dk and dv), and the rows that stream past it.
-// The segment's `tiles` tiles follow each other from `first` on; a tile's number is its place among them.
+// What a call's workgroups do, in the order of the plan: a list of tiles for each segment and side, a tile being kBwdTile
+// held rows (keys for dk and dv, queries for dq) and one range of the rows that stream past them.  Each entry of a list
+// says the same; the list's items are its tiles and ranges for every head, from first * H on: head, range, tile.
 struct BwdTile {
   int32_t held0, held_len, str0, str_len;  // the segment's rows of either side
-  int32_t first, tiles;
-  int32_t unused[2];
+  int32_t first, tiles;                    // the list's first entry; tiles of one range
+  int32_t keys, unused;
 };
-// Ahead of the tiles of the queries' side, most_q of them at most, and those of the keys' side.
-struct BwdPlan {
-  int32_t tiles_q, tiles_k;
-  int32_t unused[6];
+struct BwdPlan {  // ahead of its entries
+  int32_t tiles;
+  int32_t unused[7];
 };
 struct BwdOffsets {
   const int32_t* cu_q;
@@ -96,6 +96,9 @@ struct BwdParts {
 };
 BwdParts bwd_parts(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d,
                    int32_t num_splits, int64_t workspace, int32_t cus);
+// What the call needs at least: of forced ranges, or of the undivided call that the library falls back to.
+int64_t bwd_least_workspace(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d,
+                            int32_t num_splits);
 // An upper bound of the tiles of one side over all segments: sum of ceil(len / kBwdTile).
 int64_t bwd_tiles(int32_t nseq, int32_t most, int32_t total);
 

@@ -25,36 +25,84 @@ int64_t bwd_tiles(int32_t nseq, int32_t most, int32_t total) {
 }
 
 namespace {
-BwdParts layout(int32_t n_q, int32_t n_k, int64_t tiles, int64_t rows_q, int64_t rows_k, int32_t d) {
+struct Call {
+  int64_t tiles_q, tiles_k, rows_q, rows_k;
+  int32_t d;
+};
+BwdParts layout(const Call& c, int32_t n_q, int32_t n_k) {
   BwdParts p{n_q, n_k, 0, 0, 0, 0};
-  p.stat_offset = align256((int64_t)sizeof(BwdPlan) + tiles * (int64_t)sizeof(BwdTile));
-  p.q_offset = p.stat_offset + align256(2 * rows_q * 4);
-  p.k_offset = p.q_offset + (n_q > 1 ? align256(n_q * rows_q * d * 4) : 0);
-  p.bytes = p.k_offset + (n_k > 1 ? align256(2 * n_k * rows_k * d * 4) : 0);
+  p.stat_offset = align256((int64_t)sizeof(BwdPlan) + (c.tiles_q * n_q + c.tiles_k * n_k) * (int64_t)sizeof(BwdTile));
+  p.q_offset = p.stat_offset + align256(2 * c.rows_q * 4);
+  p.k_offset = p.q_offset + (n_q > 1 ? align256(n_q * c.rows_q * c.d * 4) : 0);
+  p.bytes = p.k_offset + (n_k > 1 ? align256(2 * n_k * c.rows_k * c.d * 4) : 0);
   return p;
 }
 }  // namespace
 
+namespace {
+// When the last of `cus` workgroups ends that take a_items of a us, then b_items of b us (a >= b), the next one when one is
+// done.  In closed form: it is asked for up to 64 times in a call of 20 us.
+double ends(int64_t cus, int64_t a_items, double a, int64_t b_items, double b) {
+  const int64_t rounds = a_items / cus, more = a_items % cus, rest = cus - more;  // `more` have one of a's more
+  const double ratio = a / b, upto = (double)(rounds + (more > 0)) * a;
+  if (b_items == 0) return upto;
+  // the end is that of a b after b's from `rounds` a's on, i of them, or from one a more, j of them
+  auto by_i = [&](int64_t i) { return rest * i + more * (int64_t)std::max(0.0, (double)i - ratio); };
+  auto by_j = [&](int64_t j) { return more * j + rest * (int64_t)((double)j + ratio); };
+  int64_t i = (int64_t)((double)(b_items + more * ratio) / (double)cus);
+  while (by_i(i) < b_items) ++i;
+  while (i > 0 && by_i(i - 1) >= b_items) --i;
+  double t = (double)rounds * a + (double)i * b;
+  if (more > 0) {
+    int64_t j = (int64_t)std::max(0.0, (double)(b_items - rest * ratio) / (double)cus);
+    while (by_j(j) < b_items) ++j;
+    while (j > 0 && by_j(j - 1) >= b_items) --j;
+    t = std::min(t, (double)(rounds + 1) * a + (double)j * b);
+  }
+  return std::max(t, upto);
+}
+}  // namespace
+
+// The ranges that the library takes: those whose call ends first by an estimate, in us as measured.  A product of a tile and a
+// step takes kProduct of them where all CUs are at work (three to a step for dq, four for dk and dv); a workgroup kItem beside its
+// steps; joining ranges kJoin and, to write and read them, kMegabyte each.  32760 x 32760 x 12 heads (d = 128) are not
+// divided; 1560 x 32760 x 12 takes 1050 with one range of keys and 930 with three, 1024 x 1024 x 2 heads (d = 64) 36 and 25
+// with four.
 BwdParts bwd_parts(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d,
                    int32_t num_splits, int64_t workspace, int32_t cus) {
-  const int64_t rows_q = (int64_t)total_q * H, rows_k = (int64_t)total_k * H;
-  const int64_t tiles_q = bwd_tiles(nseq, max_q, total_q), tiles_k = bwd_tiles(nseq, max_k, total_k), tiles = tiles_q + tiles_k;
-  if (num_splits > 0) return layout(num_splits, num_splits, tiles, rows_q, rows_k, d);
-  // costs in products of a tile and a step: three for dq, four for dk and dv
-  const int64_t steps_k = ceil_div(max_k, bwd_step(d)), steps_q = ceil_div(max_q, bwd_step(d));
-  const int64_t share = H * (3 * tiles_q * steps_k + 4 * tiles_k * steps_q) / std::max(1, cus);  // of a CU
-  auto ranges = [&](int64_t cost, int64_t steps) {  // so that an item is at most half of a CU's share
-    return (int32_t)std::max<int64_t>(1, std::min({(int64_t)16, ceil_div(2 * cost, std::max<int64_t>(share, 1)), steps}));
-  };
-  int32_t n_q = ranges(3 * steps_k, steps_k), n_k = ranges(4 * steps_q, steps_q);
-  if (tiles * H >= 4 * (int64_t)cus) n_q = n_k = 1;
-  BwdParts p = layout(n_q, n_k, tiles, rows_q, rows_k, d);
-  while (p.bytes > workspace && (n_q > 1 || n_k > 1)) {
-    n_q = std::max(1, n_q / 2);
-    n_k = std::max(1, n_k / 2);
-    p = layout(n_q, n_k, tiles, rows_q, rows_k, d);
+  const Call c{bwd_tiles(nseq, max_q, total_q), bwd_tiles(nseq, max_k, total_k), (int64_t)total_q * H, (int64_t)total_k * H, d};
+  if (num_splits > 0) return layout(c, num_splits, num_splits);
+  const double kProduct = d == 128 ? 0.8 : 0.92, kItem = 4.0, kJoin = 8.0, kMegabyte = 0.43;
+  const int64_t items_q = c.tiles_q * H, items_k = c.tiles_k * H;
+  if (items_q == 0 || items_k == 0 || items_q + items_k >= 16 * (int64_t)cus) return layout(c, 1, 1);  // (the last ones matter little)
+  // rows that stream past a tile: of uneven segments, between the longest's and the mean
+  const int32_t step = bwd_step(d);
+  auto steps = [&](int32_t most, int32_t total) { return (int32_t)ceil_div(((int64_t)most + std::min(most, total / nseq)) / 2, step); };
+  const int32_t steps_k = std::max(1, steps(max_k, total_k)), steps_q = std::max(1, steps(max_q, total_q));
+  const double part = kMegabyte * 4e-6 * d;
+  double least = 0;
+  int32_t best_q = 1, best_k = 1;
+  for (int32_t n_q : {1, 2, 3, 4, 6, 8, 12, 16}) {
+    if (n_q > steps_k) break;
+    for (int32_t n_k : {1, 2, 3, 4, 6, 8, 12, 16}) {
+      if (n_k > steps_q) break;
+      const double q = 3 * kProduct * ((steps_k + n_q - 1) / n_q) + kItem, k = 4 * kProduct * ((steps_q + n_k - 1) / n_k) + kItem;
+      double t = q > k ? ends(cus, items_q * n_q, q, items_k * n_k, k) : ends(cus, items_k * n_k, k, items_q * n_q, q);
+      if (n_q * n_k > 1) t += kJoin + part * (double)((n_q > 1 ? n_q * c.rows_q : 0) + (n_k > 1 ? 2 * n_k * c.rows_k : 0));
+      if (least != 0 && t >= 0.97 * least) continue;
+      if (n_q * n_k > 1 && layout(c, n_q, n_k).bytes > workspace) continue;
+      least = t;
+      best_q = n_q;
+      best_k = n_k;
+    }
   }
-  return p;
+  return layout(c, best_q, best_k);
+}
+
+int64_t bwd_least_workspace(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d,
+                            int32_t num_splits) {
+  const Call c{bwd_tiles(nseq, max_q, total_q), bwd_tiles(nseq, max_k, total_k), (int64_t)total_q * H, (int64_t)total_k * H, d};
+  return layout(c, std::max(1, num_splits), std::max(1, num_splits)).bytes;
 }
 
 }  // namespace tsblock

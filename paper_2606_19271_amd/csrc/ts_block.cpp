@@ -266,18 +266,16 @@ int ts_attn_bwd(const void* d_o, const void* q, const void* k, const void* v, co
                        flat(o, bytes_q),   flat(lse, (int64_t)total_q * H * 4), flat(cu_seqlens_q, bytes_cu), flat(cu_seqlens_k, bytes_cu)};
   const bool in_place[4][8] = {};
   if (aliased(written, read, in_place)) return TS_ERR_ALIAS;
-  auto parts_on = [&](int32_t cus) {
-    return tsblock::bwd_parts(nseq, max_seqlen_q, max_seqlen_k, total_q, total_k, H, d, num_splits, workspace_bytes, cus);
-  };
-  // (forced ranges, and the undivided call that the library falls back to, need the same on any device)
-  if (parts_on(1 << 30).bytes > workspace_bytes) return TS_ERR_SCRATCH;
+  if (tsblock::bwd_least_workspace(nseq, max_seqlen_q, max_seqlen_k, total_q, total_k, H, d, num_splits) > workspace_bytes)
+    return TS_ERR_SCRATCH;
   const hipStream_t s = (hipStream_t)stream;
   DeviceState* st = current_device(&rc, s);
   if (!st) return rc;
   if (validate_mode() && !capturing(s) &&
       (rc = validate(cu_seqlens_q, cu_seqlens_k, nseq, max_seqlen_q, max_seqlen_k, total_q, total_k, s)) != TS_OK)
     return rc;
-  const tsblock::BwdParts p = parts_on(st->cus);
+  const tsblock::BwdParts p =
+      tsblock::bwd_parts(nseq, max_seqlen_q, max_seqlen_k, total_q, total_k, H, d, num_splits, workspace_bytes, st->cus);
   char* const w = (char*)workspace;
   return launched(tsblock::launch_attn_bwd({d_o, q, k, v, o, lse, dq, dk, dv, cu_seqlens_q, cu_seqlens_k, (tsblock::BwdPlan*)w,
                                             (float*)(w + p.stat_offset), (float*)(w + p.q_offset), (float*)(w + p.k_offset), nseq, max_seqlen_q, max_seqlen_k,
