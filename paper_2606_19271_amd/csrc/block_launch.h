@@ -43,6 +43,7 @@ struct RopeBwdArgs {
 };
 
 constexpr int kRopeThreads = 256;
+constexpr int kRopeBwdBlocks = 512;  // at most: as many as 256 CUs hold at once
 // The workgroups of a gradient call with weights, whatever the device: its sums' order goes by them.
 int32_t rope_bwd_blocks(int32_t T, int32_t q_heads, int32_t k_heads, int32_t d);
 

@@ -16,7 +16,7 @@ int64_t align256(int64_t x) { return (x + 255) / 256 * 256; }
 int32_t rope_bwd_blocks(int32_t T, int32_t q_heads, int32_t k_heads, int32_t d) {
   const int per = 64 / (d / 16);  // heads of a wave's step
   const int64_t steps = (int64_t)T * (ceil_div(q_heads, per) + ceil_div(k_heads, per));
-  return (int32_t)std::min<int64_t>(1024, ceil_div(steps, kRopeThreads / 64));
+  return (int32_t)std::min<int64_t>(kRopeBwdBlocks, ceil_div(steps, kRopeThreads / 64));
 }
 
 int64_t bwd_tiles(int32_t nseq, int32_t most, int32_t total) {

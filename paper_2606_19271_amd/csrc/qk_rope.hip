@@ -54,18 +54,41 @@ __device__ __forceinline__ constexpr int member(int i, int which) {
   return kPairs ? 2 * i + which : i + 8 * which;
 }
 
-// cos and sin of the lane's eight angles.  A turn's fraction is exact to 2^-53 of the angle in 64 bits, and what is left
+// cos and sin of a token's angles.  Each lane forms those of one of the wave's d / 2 pairs and leaves them in the wave's LDS,
+// where it finds the eight of its own pairs.  A turn's fraction is exact to 2^-53 of the angle in 64 bits, and what is left
 // of it, half a turn at most, fits 32.
+constexpr int kAngleRow = 64 + 4;  // floats
+
+// A token's place on the axis of the lane's pair, and the lane's frequency.  (All three places are read, by scalar loads.)
+struct Place {
+  int32_t p0, p1, p2;
+};
+__device__ __forceinline__ Place place(const Rope& rope, int t) {
+  if (!rope.freq) return Place{0, 0, 0};
+  const int32_t* const pos = rope.pos + 3 * (int64_t)t;
+  return Place{pos[0], pos[1], pos[2]};
+}
+
 template <int D, bool kPairs>
-__device__ __forceinline__ void angles(const Rope& rope, int t, int j, float (&c)[8], float (&s)[8]) {
-  const int32_t p0 = rope.pos[3 * (int64_t)t], p1 = rope.pos[3 * (int64_t)t + 1], p2 = rope.pos[3 * (int64_t)t + 2];
+__device__ __forceinline__ void angles(const Rope& rope, const Place& at, int lane, double freq, float* lds, float (&c)[8],
+                                       float (&s)[8]) {
+  const int pair = lane % (D / 2);
+  const int32_t p = pair < rope.n0 ? at.p0 : pair < rope.n01 ? at.p1 : at.p2;
+  double turns = (double)p * (freq * 0.15915494309189535);
+  turns -= __builtin_rint(turns);
+  float sine, cosine;
+  sincospif(2.0f * (float)turns, &sine, &cosine);
+  __builtin_amdgcn_wave_barrier();  // (the token before has read its angles)
+  lds[pair] = cosine;  // (at d = 64 by two lanes alike)
+  lds[kAngleRow + pair] = sine;
+  __builtin_amdgcn_wave_barrier();
+  const int j = lane % Geo<D>::kLanes, lo = kPairs ? 4 * j : 8 * j, hi = kPairs ? D / 4 + 4 * j : 8 * j + 4;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int pair = !kPairs ? 8 * j + i : i < 4 ? 4 * j + i : D / 4 + 4 * j + i - 4;
-    const int32_t p = pair < rope.n0 ? p0 : pair < rope.n01 ? p1 : p2;
-    double turns = (double)p * (rope.freq[pair] * 0.15915494309189535);
-    turns -= __builtin_rint(turns);
-    sincospif(2.0f * (float)turns, &s[i], &c[i]);
+  for (int i = 0; i < 4; ++i) {
+    c[i] = lds[lo + i];
+    c[4 + i] = lds[hi + i];
+    s[i] = lds[kAngleRow + lo + i];
+    s[4 + i] = lds[kAngleRow + hi + i];
   }
 }
 
@@ -103,10 +126,17 @@ __device__ __forceinline__ float inverse_rms(const float (&x)[16], float eps) {
   return (float)(y == 0 ? y : z);
 }
 
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
 template <int D>
 __device__ __forceinline__ void load_weights(const float* w, int j, float (&x)[16]) {
+  if (!w) return;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = w ? w[8 * j + i] : 1.0f, x[8 + i] = w ? w[D / 2 + 8 * j + i] : 1.0f;
+  for (int u = 0; u < 4; ++u) {
+    const f32x4_any y = *(const f32x4_any*)(w + 8 * j + 4 * (u & 1) + (u >> 1) * (D / 2));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[4 * u + i] = y[i];
+  }
 }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -137,9 +167,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int grou
   const int j = lane % G::kLanes, r = lane / G::kLanes;
   Steps at(wave, per, steps, groups);
   if (at.left <= 0) return;
+  __shared__ float lds[kWaves][2 * kAngleRow];
   float wq[16], wk[16], c[8], s[8];
-  load_weights<D>(a.q_weight, j, wq);
-  load_weights<D>(a.k_weight, j, wk);
   auto rows = [&](const Rows& q, const Rows& k, const Steps& at, bool& live) {
     const bool is_k = at.g >= groups_q;
     const Rows& x = is_k ? k : q;
@@ -150,9 +179,12 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int grou
   bool live;
   const __bf16* from = rows(a.q, a.k, at, live);
   Head in = load_head<D>(from, live);
+  const double freq = a.rope.freq ? a.rope.freq[lane % (D / 2)] : 0.0;
+  load_weights<D>(a.q_weight, j, wq);
+  load_weights<D>(a.k_weight, j, wk);
   bool fresh = true;
   while (true) {
-    if (fresh && a.rope.freq) angles<D, kPairs>(a.rope, at.t, j, c, s);
+    if (fresh && a.rope.freq) angles<D, kPairs>(a.rope, place(a.rope, at.t), lane, freq, lds[threadIdx.x >> 6], c, s);
     const Steps here = at;
     Head after = in;
     fresh = at.next(groups);
@@ -193,9 +225,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(RopeBwdArgs a, i
   const int lane = threadIdx.x & 63, wave = uniform(blockIdx.x * kWaves + (threadIdx.x >> 6));
   const int j = lane % G::kLanes, r = lane / G::kLanes;
   Steps at(wave, per, steps, groups);
+  __shared__ float lds[kWaves][2 * kAngleRow];
   float wq[16], wk[16], c[8], s[8], sum_q[16] = {}, sum_k[16] = {};
-  load_weights<D>(a.q_weight, j, wq);
-  load_weights<D>(a.k_weight, j, wk);
   auto rows = [&](const Rows& q, const Rows& k, const Steps& at, bool& live) {
     const bool is_k = at.g >= groups_q;
     const Rows& x = is_k ? k : q;
@@ -213,8 +244,11 @@ __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(RopeBwdArgs a, i
   };
   Head dy_in{}, x_in{};
   if (at.left > 0) load(dy_in, x_in);
+  const double freq = a.rope.freq ? a.rope.freq[lane % (D / 2)] : 0.0;
+  load_weights<D>(a.q_weight, j, wq);
+  load_weights<D>(a.k_weight, j, wk);
   while (at.left > 0) {
-    if (fresh && a.rope.freq) angles<D, kPairs>(a.rope, at.t, j, c, s);
+    if (fresh && a.rope.freq) angles<D, kPairs>(a.rope, place(a.rope, at.t), lane, freq, lds[threadIdx.x >> 6], c, s);
     const Steps here = at;
     Head dy_next = dy_in, x_next = x_in;
     fresh = at.next(groups);
@@ -277,20 +311,27 @@ __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(RopeBwdArgs a, i
   }
 }
 
-// The weights' gradients: 16 channels to a workgroup, the workgroups' sums dealt to 16 threads each, in 64 bits.
+// The weights' gradients: 16 channels to a workgroup, the workgroups' sums dealt to 64 threads of each, in 64 bits.
 template <int D>
-__global__ __launch_bounds__(256) void rope_bwd_join_kernel(const float* part, int blocks, float* dq_weight, float* dk_weight) {
-  __shared__ double sums[16][17];
-  const int ch = blockIdx.x * 16 + (threadIdx.x & 15), u = threadIdx.x >> 4;
+__global__ __launch_bounds__(1024) void rope_bwd_join_kernel(const float* part, int blocks, float* dq_weight, float* dk_weight) {
+  __shared__ double sums[64][17];
+  const int i = threadIdx.x & 15, ch = blockIdx.x * 16 + i, u = threadIdx.x >> 4;
   double x = 0;
-  for (int b = u; b < blocks; b += 16) x += part[(int64_t)b * 2 * D + ch];
-  sums[u][threadIdx.x & 15] = x;
-  __syncthreads();
-  if (u != 0) return;
+  for (int b = u; b < blocks; b += 64 * 8) {
+    float y[8];  // eight reads under way
 #pragma unroll
-  for (int i = 1; i < 16; ++i) x += sums[i][threadIdx.x];
+    for (int k = 0; k < 8; ++k) y[k] = b + 64 * k < blocks ? part[(int64_t)(b + 64 * k) * 2 * D + ch] : 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x += y[k];
+  }
+  sums[u][i] = x;
+  __syncthreads();
+  for (int n = 32; n > 0; n >>= 1) {
+    if (u < n) sums[u][i] += sums[u + n][i];
+    __syncthreads();
+  }
   float* const to = ch < D ? dq_weight : dk_weight;
-  if (to) to[ch < D ? ch : ch - D] = (float)x;
+  if (u == 0 && to) to[ch < D ? ch : ch - D] = (float)sums[0][i];
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return a / b + (a % b != 0); }
@@ -299,7 +340,7 @@ template <int D>
 hipError_t rope(const RopeArgs& a, hipStream_t st) {
   const int gq = (int)ceil_div(a.q.heads, Geo<D>::kHeads), groups = gq + (int)ceil_div(a.k.heads, Geo<D>::kHeads);
   const int steps = a.T * groups;
-  const int per = (int)std::max({(int64_t)1, std::min<int64_t>(groups, steps / 8192), ceil_div(steps, (int64_t)1 << 24)});
+  const int per = (int)std::max({(int64_t)1, std::min<int64_t>(groups, ceil_div(steps, 4096)), ceil_div(steps, (int64_t)1 << 24)});
   const unsigned blocks = (unsigned)ceil_div(ceil_div(steps, per), kWaves);
   if (a.rope.interleaved) rope_kernel<D, true><<<blocks, kRopeThreads, 0, st>>>(a, gq, groups, steps, per);
   else rope_kernel<D, false><<<blocks, kRopeThreads, 0, st>>>(a, gq, groups, steps, per);
@@ -316,7 +357,7 @@ hipError_t rope_bwd(const RopeBwdArgs& a, hipStream_t st) {
     if (a.rope.interleaved) rope_bwd_kernel<D, true><<<blocks, kRopeThreads, 0, st>>>(a, gq, groups, steps, per);
     else rope_bwd_kernel<D, false><<<blocks, kRopeThreads, 0, st>>>(a, gq, groups, steps, per);
   }
-  if (a.dq_weight || a.dk_weight) rope_bwd_join_kernel<D><<<2 * D / 16, 256, 0, st>>>(a.part, blocks, a.dq_weight, a.dk_weight);
+  if (a.dq_weight || a.dk_weight) rope_bwd_join_kernel<D><<<2 * D / 16, 1024, 0, st>>>(a.part, blocks, a.dq_weight, a.dk_weight);
   return hipGetLastError();
 }
 
