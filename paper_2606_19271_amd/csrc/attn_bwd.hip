@@ -14,30 +14,41 @@ namespace tsblock {
 using namespace tsattn;
 
 // The rows of one side are held in registers (dq: queries and d_o; dk, dv: keys and values), 32 by a wave, and those of
-// the other stream through LDS, `kBN` of them at a time.  With X1, X2 the streamed pair (dq: k, v; dk, dv: q, d_o)
+// the other stream through LDS, kBN of them at a time.  With X1, X2 the streamed pair (dq: k, v; dk, dv: q, d_o)
 // and Y1, Y2 the held one, a wave computes for 32 streamed rows
-//   S = X1 Y1^T,  T = X2 Y2^T           (32 x 32: streamed rows in registers, held ones over the lanes)
-//   P = exp(scale S - lse),  R = P (T - D)
+//   S = X1 Y1^T,  T = X2 Y2^T - D       (32 x 32: streamed rows in registers, held ones over the lanes)
+//   P = exp(scale S - lse),  R = P T
 //   acc1^T += X1^T R   (dq or dk),      acc2^T += X2^T P   (dv)
 // where P and R, as they lie, are the B operands of the last two products, whose A operands are transposed reads of
-// the same LDS rows.
+// the same LDS rows.  Where the streamed rows are queries, S and T start at their -lse / scale and -D, which come with them.
+//
+// Both gradients of a score tile recompute S and T: seven products of a tile in all where five would do if dq were added up
+// in memory across the key tiles.  Those sums would have to be atomic, in no fixed order, or wait for each other, and the scores
+// would have to be laid out anew for them through LDS, which has no time to spare (a read of 1 KiB feeds one MFMA of a SIMD:
+// 8 clocks of the LDS' 8).
 //
 // LDS layout of a streamed tile: rows in groups of four, so that both the row reads (b128: 16 rows, the same 16-byte
 // chunk) and the transposed ones (b64: 4 rows x 64 bytes) fall on distinct banks, with offsets that are sums of a
-// lane's own and an immediate.  At d = 128 the four rows are 320 bytes apart, at d = 64 at 0, 128, 320 and 448.
-template <int D>
+// lane's own and an immediate.  At d = 128 the four rows are 320 bytes apart, at d = 64 at 0, 128, 320 and 448.  (No bank
+// conflicts were counted.)
+template <int D, int W>  // W waves to a workgroup
 struct Bwd {
-  static constexpr int kBN = bwd_step(D);
+  static constexpr int kWaves = W;
+  static constexpr int kThreads = 64 * W;
+  static constexpr int kTileRows = 32 * W;
+  static constexpr int kBN = bwd_step(D, kTileRows);
   static constexpr int kGroup = D == 128 ? 1232 : 592;  // bytes of a group of four rows, 16 mod 64
   static constexpr int kTile = (kBN / 4 * kGroup + 1023) / 1024 * 1024;
   static constexpr int kDma = kTile / 1024;  // DMA instructions of a tile
-  static constexpr int kDmaMax = (kDma + kWaves - 1) / kWaves, kDmaMin = kDma / kWaves;  // of a wave
-  static constexpr int kStat = 2 * kTile;  // [2][kBN] floats, after X1 and X2
-  static constexpr int kStage = 2 * kTile + 2 * kBN * 4;
-  static constexpr int kStages = 3;
+  static constexpr int kDmaMax = (kDma + W - 1) / W, kDmaMin = kDma / W;  // of a wave
+  static constexpr int kStat = 2 * kTile;  // the two statistics, after X1 and X2
+  static constexpr int kStatRow = kBN < 64 ? 256 : kBN * 4;  // bytes of one: a DMA instruction fills 256
+  static constexpr int kStatDma = kStatRow / 256;
+  static constexpr int kStage = 2 * kTile + 2 * kStatRow;
+  static constexpr int kStages = D == 64 ? 2 : 3;
   static constexpr int kLds = kStages * kStage;
-  static constexpr int kStatDma = kBN / 64;  // 4-byte DMA instructions of each statistic
-  static_assert(kLds <= 160 * 1024, "LDS of a CU");
+  static_assert(bwd_groups(D, kTileRows) * kLds <= 160 * 1024, "LDS of a CU");
+  static_assert(2 * kStatDma <= W, "a wave fetches one part of the statistics");
   __host__ __device__ static constexpr int row_offset(int r) {
     return (r >> 2) * kGroup + (D == 128 ? 320 * (r & 3) : 128 * (r & 1) + 320 * ((r >> 1) & 1));
   }
@@ -88,25 +99,15 @@ typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
 // The LDS reads of a step take their address as a restrict pointer: the compiler then knows that they do not wait for the
 // DMA of the steps ahead.
 
-// to += x y^T for a block of 32 rows of X1 or X2.
-template <int D>
-__device__ __forceinline__ void rows_product(const lds_char* __restrict__ x, const bf16x8 (&y)[D / 16], f32x16& to) {
-#pragma unroll
-  for (int kk = 0; kk < D / 16; ++kk) to = mfma32(*(const lds_bf16x8*)(x + 32 * kk), y[kk], to);
-}
+// A operand of a product with 32 rows of X1 or X2: 16 of their channels.
+__device__ __forceinline__ bf16x8 rows_operand(const lds_char* __restrict__ x) { return *(const lds_bf16x8*)x; }
 
-// acc^T += x^T w for a block's 32 rows of X1 or X2.
-template <int D>
-__device__ __forceinline__ void columns_product(const lds_char* __restrict__ x, const bf16x8 (&w)[2], f32x16 (&acc)[D / 32]) {
-#pragma unroll
-  for (int u = 0; u < 2; ++u)
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) {
-      const lds_char* const at = x + 4 * u * Bwd<D>::kGroup + 64 * db;
-      const bf16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)at);
-      const bf16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + 2 * Bwd<D>::kGroup));
-      acc[db] = mfma32(bf16x8{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]}, w[u], acc[db]);
-    }
+// A operand of a product with the columns of X1 or X2: 32 channels of 16 rows.
+template <int kGroup>
+__device__ __forceinline__ bf16x8 columns_operand(const lds_char* __restrict__ x) {
+  const bf16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)x);
+  const bf16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(x + 2 * kGroup));
+  return bf16x8{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
 }
 
 // The statistics of a block's 32 queries, as the rows of an accumulator.
@@ -121,21 +122,24 @@ __device__ __forceinline__ f32x16 row_statistics(const lds_char* __restrict__ x,
   return to;
 }
 
+__device__ __forceinline__ f32x16 splat(float x) { return f32x16{x, x, x, x, x, x, x, x, x, x, x, x, x, x, x, x}; }
+
 // One item of the dq (kKeys = false) or the dk, dv side.
-template <int D, bool kKeys>
+template <int D, int W, bool kKeys>
 __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_char* lds) {
-  using G = Bwd<D>;
+  using G = Bwd<D, W>;
   constexpr int kBN = G::kBN;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int col = lane & 31, hb = lane >> 5;
   const int row_bytes = a.H * D * 2;
   const int held_len = w.held_len, len = w.str_len;  // rows of the segment
   const int64_t held0 = ((int64_t)w.held0 * a.H + w.h) * D, str0 = ((int64_t)w.str0 * a.H + w.h) * D;
-  const int row0 = w.tile * kBwdTile + 32 * wave;  // this wave's first held row
+  const int row0 = w.tile * G::kTileRows + 32 * wave;  // this wave's first held row
 
-  // the range of steps
-  const int steps_all = (len + kBN - 1) / kBN, n = kKeys ? a.n_k : a.n_q;
-  const int begin = (int)((int64_t)steps_all * w.split / n), end = (int)((int64_t)steps_all * (w.split + 1) / n);
+  // the range's steps; ranges are of 64 rows, whatever a step has, so that their sums do not go by the tile
+  const int steps_all = (len + kBN - 1) / kBN, n = kKeys ? a.n_k : a.n_q, units = (len + 63) / 64;
+  const int begin = (int)((int64_t)units * w.split / n) * (64 / kBN);
+  const int end = min((int)((int64_t)units * (w.split + 1) / n) * (64 / kBN), steps_all);
   const int steps = end - begin;
 
   f32x16 acc1[D / 32], acc2[kKeys ? D / 32 : 1];
@@ -157,12 +161,12 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
     const __amdgpu_buffer_rsrc_t ra = make_rsrc(stat, stat_bytes);
     const __amdgpu_buffer_rsrc_t rd = make_rsrc(stat + (int64_t)a.H * a.total_q, stat_bytes);
 
-    // DMA: instruction i = wave + 8 u of a tile fills LDS bytes [1024 i, 1024 i + 1024), lane l 16 of them; lanes of the
+    // DMA: instruction i = wave + W u of a tile fills LDS bytes [1024 i, 1024 i + 1024), lane l 16 of them; lanes of the
     // pads fetch a row's first chunk again
     int off[G::kDmaMax];
 #pragma unroll
     for (int u = 0; u < G::kDmaMax; ++u) {
-      const int b = 1024 * (wave + kWaves * u) + 16 * lane;
+      const int b = 1024 * (wave + W * u) + 16 * lane;
       const int g = b / G::kGroup, rem = b % G::kGroup;
       int r, byte;
       if (D == 128) {
@@ -182,7 +186,7 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
       const int step = min(begin + j, steps_all), skip = step * kBN * row_bytes;
 #pragma unroll
       for (int u = 0; u < G::kDmaMax; ++u) {
-        const int i = wave + kWaves * u;
+        const int i = wave + W * u;
         if (u < G::kDmaMin || i < G::kDma) {
           __builtin_amdgcn_raw_ptr_buffer_load_lds(rx1, (lds_void*)(stage + 1024 * i), 16, off[u] + skip, 0, 0, 0);
           __builtin_amdgcn_raw_ptr_buffer_load_lds(rx2, (lds_void*)(stage + G::kTile + 1024 * i), 16, off[u] + skip, 0, 0, 0);
@@ -194,8 +198,8 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
                                                  (step * kBN + 64 * part + lane) * 4, 0, 0, 0);
       }
     };
-    fetch(0, lds);
-    fetch(1, lds + G::kStage);
+#pragma unroll
+    for (int j = 0; j < G::kStages - 1; ++j) fetch(j, lds + j * G::kStage);
 
     // held rows as B operands: row col, channels 16 kk + 8 hb + 0..7
     bf16x8 y1[D / 16], y2[D / 16];
@@ -218,80 +222,98 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
     const float c = a.c;
     const bool active = row0 < held_len;
 
-    // s becomes P.  kRagged: rows from `left` on are past the segment's end, their P is 0 (and so is R below).
-    auto weights = [&](f32x16& s, auto ragged, int left) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[r] = __builtin_amdgcn_exp2f(kKeys ? s[r] * c : __builtin_fmaf(s[r], c, la));
-        if (decltype(ragged)::value && 8 * (r >> 2) + 4 * hb + (r & 3) >= left) s[r] = 0.0f;
-      }
-    };
-    auto pack = [&](const f32x16& x, bf16x8 (&to)[2]) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) to[r >> 3][r & 7] = (__bf16)x[r];
-    };
-    auto residuals = [&](const f32x16& p, const f32x16& t, bf16x8 (&to)[2], auto ragged, int left) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float x = p[r] * t[r];
-        if (decltype(ragged)::value && 8 * (r >> 2) + 4 * hb + (r & 3) >= left) x = 0.0f;
-        to[r >> 3][r & 7] = (__bf16)x;
-      }
-    };
-    // One step.  The order is such that the vector work of a block runs under matrix work that does not wait for it.
+    // One step.  The order of its products and reads is pinned: each operand is read a product before it is used (more ahead
+    // measured the same), and the vector work on a product's result goes between products that do not wait for it.  Left to the
+    // compiler's order 32760 x 32760 x 12 heads took 17.75 ms instead of 17.4, 16380 x 16380 x 24 heads of d = 64 5.1 instead of
+    // 5.0.  ragged: rows from `left` on are past the segment's end; their P and R are 0.
+    constexpr int kM = D / 16;  // MFMAs of a product
+        constexpr bool kPair = !kKeys && kBN >= 64;  // dq: two blocks at a time
+    constexpr int kBlocks = kBN / (kPair ? 64 : 32), kPer = (kKeys ? 4 : kPair ? 6 : 3) * kM, kAll = kBlocks * kPer;
     auto step_of = [&](const lds_char* stage, auto ragged, int left) {
-      const lds_char* xr = stage + row_lane;
-      const lds_char* xt = stage + tr_lane;
-      if constexpr (kKeys) {
-        const lds_char* st = stage + G::kStat;
-#pragma unroll 1
-        for (int b = 0; b < kBN / 32; ++b) {
-          f32x16 s = row_statistics(st, hb), t = row_statistics(st + kBN * 4, hb);
-          bf16x8 p[2], ds[2];
-          rows_product<D>(xr, y1, s);
-          rows_product<D>(xr + G::kTile, y2, t);
-          weights(s, ragged, left);
-          pack(s, p);
-          columns_product<D>(xt + G::kTile, p, acc2);
-          residuals(s, t, ds, ragged, left);
-          columns_product<D>(xt, ds, acc1);
-          xr += 8 * G::kGroup;
-          xt += 8 * G::kGroup;
-          st += 128;
-          left -= 32;
+      const lds_char* const xr = stage + row_lane;
+      const lds_char* const xt = stage + tr_lane;
+      const lds_char* const st = stage + G::kStat;
+      auto operand = [&](int i) {
+        const int b = i / kPer, phase = i % kPer / kM, m = i % kM;
+        const int column = 4 * (m / (D / 32)) * G::kGroup + 64 * (m % (D / 32));
+        if (kKeys) {
+          const int block = 8 * b * G::kGroup;
+          if (phase < 2) return rows_operand(xr + block + phase * G::kTile + 32 * m);
+          return columns_operand<G::kGroup>(xt + block + (phase == 2 ? G::kTile : 0) + column);
         }
-      } else {
-#pragma unroll 1
-        for (int b = 0; b < kBN / 64; ++b) {
-          f32x16 s0 = {}, s1 = {}, t0, t1;
-          bf16x8 ds0[2], ds1[2];
+        const int block = (8 * (kPair ? 2 : 1) * b + (kPair && (phase == 2 || phase == 3 || phase == 5) ? 8 : 0)) * G::kGroup;
+        if (phase < (kPair ? 4 : 2)) return rows_operand(xr + block + (phase & 1) * G::kTile + 32 * m);
+        return columns_operand<G::kGroup>(xt + block + column);
+      };
+      f32x16 s[kKeys ? 1 : 2], t[kKeys ? 1 : 2];
+      bf16x8 p[2], ds[kKeys ? 1 : 2][2];
+      auto weight = [&](int w, int r, int row) {  // s becomes P
+        float x = s[w][r];
+        x = __builtin_amdgcn_exp2f(kKeys ? x * c : __builtin_fmaf(x, c, la));
+        if (decltype(ragged)::value && row + 8 * (r >> 2) + 4 * hb + (r & 3) >= left) x = 0.0f;
+        s[w][r] = x;
+        if (kKeys) p[r >> 3][r & 7] = (__bf16)x;
+      };
+      auto residual = [&](int w, int r, int row) {
+        float x = s[w][r] * t[w][r];
+        if (decltype(ragged)::value && row + 8 * (r >> 2) + 4 * hb + (r & 3) >= left) x = 0.0f;
+        ds[w][r >> 3][r & 7] = (__bf16)x;
+      };
+      // element range of slot m of a phase: nothing in the first, whose product waits for the result
+      auto from = [](int m) { return m < 1 ? 0 : 2 * ((8 * (m - 1) + kM - 2) / (kM - 1)); };
+      if (kKeys) {
+        s[0] = row_statistics(st, hb);
+        t[0] = row_statistics(st + G::kStatRow, hb);
+      }
+      bf16x8 next = operand(0);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) t0[r] = ld, t1[r] = ld;
-          rows_product<D>(xr, y1, s0);
-          rows_product<D>(xr + G::kTile, y2, t0);
-          weights(s0, ragged, left);
-          rows_product<D>(xr + 8 * G::kGroup, y1, s1);
-          residuals(s0, t0, ds0, ragged, left);
-          rows_product<D>(xr + G::kTile + 8 * G::kGroup, y2, t1);
-          weights(s1, ragged, left - 32);
-          columns_product<D>(xt, ds0, acc1);
-          residuals(s1, t1, ds1, ragged, left - 32);
-          columns_product<D>(xt + 8 * G::kGroup, ds1, acc1);
-          xr += 16 * G::kGroup;
-          xt += 16 * G::kGroup;
-          left -= 64;
+      for (int i = 0; i < kAll; ++i) {
+        const int b = i / kPer, phase = i % kPer / kM, m = i % kM;
+        const bf16x8 x = next;
+        if (i + 1 < kAll) next = operand(i + 1);
+        if constexpr (kKeys) {
+          if (phase == 0) s[0] = mfma32(x, y1[m], s[0]);
+          else if (phase == 1) t[0] = mfma32(x, y2[m], t[0]);
+          else if (phase == 2) acc2[m % (D / 32)] = mfma32(x, p[m / (D / 32)], acc2[m % (D / 32)]);
+          else acc1[m % (D / 32)] = mfma32(x, ds[0][m / (D / 32)], acc1[m % (D / 32)]);
+#pragma unroll
+          for (int r = from(m); r < from(m + 1); ++r) {
+            if (phase == 1) weight(0, r, 32 * b);
+            if (phase == 2) residual(0, r, 32 * b);
+          }
+          if (phase == 3 && b + 1 < kBlocks) {
+            if (m == 0) s[0] = row_statistics(st + 128 * (b + 1), hb);
+            if (m == 1) t[0] = row_statistics(st + 128 * (b + 1) + G::kStatRow, hb);
+          }
+        } else {
+          const int w = kPair && (phase == 2 || phase == 3 || phase == 5);
+          if (phase == 0 || (kPair && phase == 2)) s[w] = mfma32(x, y1[m], m == 0 ? f32x16{} : s[w]);
+          else if (phase == 1 || (kPair && phase == 3)) t[w] = mfma32(x, y2[m], m == 0 ? splat(ld) : t[w]);
+          else acc1[m % (D / 32)] = mfma32(x, ds[w][m / (D / 32)], acc1[m % (D / 32)]);
+#pragma unroll
+          for (int r = from(m); r < from(m + 1); ++r) {
+            if (phase == 1) weight(0, r, (kPair ? 64 : 32) * b);
+            if (kPair && phase == 2) residual(0, r, 64 * b);
+            if (kPair && phase == 3) weight(1, r, 64 * b + 32);
+            if (kPair && phase == 4) residual(1, r, 64 * b + 32);
+          }
+          if (!kPair && phase == 1 && m == kM - 1) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) residual(0, r, 32 * b);
+          }
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
     };
 
     int slot = 0;
-    auto open_step = [&](int j) {  // step j's stage, complete; the fetch of step j + 2
+    auto open_step = [&](int j) {  // step j's stage, complete; the next fetch, into the stage that step j - 1 was read from
       wait_lds();
-      wait_vmem<2 * G::kDmaMin>();  // step j is here, step j + 1 may be on its way
+      wait_vmem<(G::kStages - 2) * 2 * G::kDmaMin>();  // step j is here, step j + 1 of three may be on its way
       block_sync();
       const lds_char* const stage = lds + slot * G::kStage;
-      fetch(j + 2, lds + (slot == 0 ? 2 : slot - 1) * G::kStage);
-      slot = slot == 2 ? 0 : slot + 1;
+      fetch(j + G::kStages - 1, lds + (slot == 0 ? G::kStages - 1 : slot - 1) * G::kStage);
+      slot = slot == G::kStages - 1 ? 0 : slot + 1;
       return stage;
     };
     const int whole = min(steps, len / kBN - begin);  // steps without rows past the segment's end: all but the last one
@@ -341,15 +363,14 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
     }
 }
 
-template <int D>
-__global__ __launch_bounds__(kThreads, 2) void attn_bwd_kernel(BwdCall a) {
+template <int D, int W>
+__global__ __launch_bounds__(64 * W, bwd_groups(D, 32 * W) * W / 4) void attn_bwd_kernel(BwdCall a) {
   extern __shared__ char smem[];
-  const int total = a.plan->tiles * a.H;
-  if ((int)blockIdx.x >= total) return;
-  const int item = blockIdx.x;
+  const int total = a.plan->tiles * a.H, item = blockIdx.x;
+  if (item >= total) return;
   const BwdTile* const t = (const BwdTile*)(a.plan + 1) + item / a.H;  // (any of the item's list)
-  if (t->keys) run_item<D, true>(a, find_item(t, item, a.H, a.n_k), (lds_char*)smem);
-  else run_item<D, false>(a, find_item(t, item, a.H, a.n_q), (lds_char*)smem);
+  if (t->keys) run_item<D, W, true>(a, find_item(t, item, a.H, a.n_k), (lds_char*)smem);
+  else run_item<D, W, false>(a, find_item(t, item, a.H, a.n_q), (lds_char*)smem);
 }
 
 // The plan: the tiles of all segments' queries (for dq) and keys (for dk and dv), each once for every range of its
@@ -367,7 +388,7 @@ __device__ __forceinline__ int wave_sum_to(int x, int lane) {  // inclusive pref
   return x;
 }
 
-__device__ void make_plan(BwdPlan* plan, BwdOffsets f, int n_q, int n_k) {
+__device__ void make_plan(BwdPlan* plan, BwdOffsets f, int n_q, int n_k, int tile) {
   __shared__ int cost[kSorted], order[kSorted], part[kPlanThreads / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lists = 2 * f.nseq;
   bool bad = false;
@@ -393,7 +414,7 @@ __device__ void make_plan(BwdPlan* plan, BwdOffsets f, int n_q, int n_k) {
     t.str0 = t.keys ? f.cu_q[s] : f.cu_k[s];
     t.held_len = (t.keys ? f.cu_k[s + 1] : f.cu_q[s + 1]) - t.held0;
     t.str_len = (t.keys ? f.cu_q[s + 1] : f.cu_k[s + 1]) - t.str0;
-    t.tiles = (t.held_len + kBwdTile - 1) / kBwdTile;
+    t.tiles = (t.held_len + tile - 1) / tile;
   };
   const bool sorted = lists <= kSorted;
   if (sorted) {  // by the products of an item: four of a step's rows for dk and dv, three for dq
@@ -436,8 +457,8 @@ __device__ void make_plan(BwdPlan* plan, BwdOffsets f, int n_q, int n_k) {
 // [2][H][total_q], 64 tokens of one head to a workgroup and a row of d bf16 to d / 8 lanes.
 template <int D>
 __global__ __launch_bounds__(kPlanThreads) void bwd_prepare_kernel(const __bf16* d_o, const __bf16* o, const float* lse, float* stat,
-                                                                   int T, int H, float inv, BwdPlan* plan, BwdOffsets f, int n_q, int n_k) {
-  if (blockIdx.x == 0) return make_plan(plan, f, n_q, n_k);
+                                                                   int T, int H, float inv, BwdPlan* plan, BwdOffsets f, int n_q, int n_k, int tile) {
+  if (blockIdx.x == 0) return make_plan(plan, f, n_q, n_k, tile);
   constexpr int kLanes = D / 8, kRows = kPlanThreads / kLanes;
   const int h = (blockIdx.x - 1) % H, t0 = (blockIdx.x - 1) / H * 64;
   const int r = threadIdx.x / kLanes, i = threadIdx.x % kLanes;
@@ -506,9 +527,11 @@ hipError_t launch(const BwdArgs& x, hipStream_t st) {
   const int64_t stats = ((int64_t)x.total_q + 63) / 64 * x.H;
   bwd_prepare_kernel<D><<<(unsigned)(1 + stats), kPlanThreads, 0, st>>>(
       a.d_o, (const __bf16*)x.o, x.lse, x.stat, x.total_q, x.H, 1.0f / s, x.plan,
-      BwdOffsets{x.cu_q, x.cu_k, x.nseq, x.max_q, x.max_k, x.total_q, x.total_k}, x.n_q, x.n_k);
-  const int64_t items = x.H * (bwd_tiles(x.nseq, x.max_q, x.total_q) * x.n_q + bwd_tiles(x.nseq, x.max_k, x.total_k) * x.n_k);
-  if (items > 0) attn_bwd_kernel<D><<<(unsigned)items, kThreads, Bwd<D>::kLds, st>>>(a);
+      BwdOffsets{x.cu_q, x.cu_k, x.nseq, x.max_q, x.max_k, x.total_q, x.total_k}, x.n_q, x.n_k, x.tile);
+  const int64_t items = x.H * (bwd_tiles(x.nseq, x.max_q, x.total_q, x.tile) * x.n_q + bwd_tiles(x.nseq, x.max_k, x.total_k, x.tile) * x.n_k);
+  if (items > 0 && x.tile == 128) attn_bwd_kernel<D, 4><<<(unsigned)items, 256, Bwd<D, 4>::kLds, st>>>(a);
+  if constexpr (D == 128)
+    if (items > 0 && x.tile == 256) attn_bwd_kernel<D, 8><<<(unsigned)items, 512, Bwd<D, 8>::kLds, st>>>(a);
   const int64_t join_k = x.n_k > 1 ? ((int64_t)x.total_k * x.H + kJoinRows - 1) / kJoinRows : 0;
   const int64_t join_q = x.n_q > 1 ? ((int64_t)x.total_q * x.H + kJoinRows - 1) / kJoinRows : 0;
   if (join_k + join_q > 0) bwd_join_kernel<D><<<(unsigned)(join_k + join_q), 256, 0, st>>>(a, (int)join_k);
@@ -521,8 +544,9 @@ hipError_t launch_attn_bwd(const BwdArgs& a, hipStream_t st) {
 
 hipError_t configure_kernels() {
   auto allow = [](const void* f, int bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); };
-  hipError_t e = allow((const void*)attn_bwd_kernel<64>, Bwd<64>::kLds);
-  if (e == hipSuccess) e = allow((const void*)attn_bwd_kernel<128>, Bwd<128>::kLds);
+  hipError_t e = allow((const void*)attn_bwd_kernel<64, 4>, Bwd<64, 4>::kLds);
+  if (e == hipSuccess) e = allow((const void*)attn_bwd_kernel<128, 4>, Bwd<128, 4>::kLds);
+  if (e == hipSuccess) e = allow((const void*)attn_bwd_kernel<128, 8>, Bwd<128, 8>::kLds);
   return e;
 }
 

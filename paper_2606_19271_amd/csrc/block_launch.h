@@ -47,8 +47,8 @@ constexpr int kRopeBwdBlocks = 512;  // at most: as many as 256 CUs hold at once
 // The workgroups of a gradient call with weights, whatever the device: its sums' order goes by them.
 int32_t rope_bwd_blocks(int32_t T, int32_t q_heads, int32_t k_heads, int32_t d);
 
-// What a call's workgroups do, in the order of the plan: a list of tiles for each segment and side, a tile being kBwdTile
-// held rows (keys for dk and dv, queries for dq) and one range of the rows that stream past them.  Each entry of a list
+// What a call's workgroups do, in the order of the plan: a list of tiles for each segment and side, a tile being the
+// held rows of a workgroup (keys for dk and dv, queries for dq) and one range of the rows that stream past them.  Each entry of a list
 // says the same; the list's items are its tiles and ranges for every head, from first * H on: head, range, tile.
 struct BwdTile {
   int32_t held0, held_len, str0, str_len;  // the segment's rows of either side
@@ -82,17 +82,18 @@ struct BwdArgs {
   float* part_q;   // [n_q][total_q][H][d], where n_q > 1
   float* part_k;   // [n_k][total_k][H][d] of dk, then of dv, where n_k > 1
   int32_t nseq, max_q, max_k, total_q, total_k, H, d;
-  int32_t n_q, n_k;
+  int32_t n_q, n_k, tile;
   float scale;
 };
 
-constexpr int kBwdTile = 256;  // queries (dq) or keys (dk, dv) of a workgroup
-// Rows of the other side that a workgroup holds in LDS at a time.
-constexpr int bwd_step(int d) { return d == 64 ? 128 : 64; }
+// A workgroup of ts_attn_bwd holds `tile` queries (dq) or keys (dk, dv), 32 a wave; the rows of the other side come into LDS
+// bwd_step at a time; a CU runs bwd_groups of them at once.
+constexpr int bwd_step(int d, int tile) { return d == 128 && tile == 128 ? 32 : 64; }
+constexpr int bwd_groups(int d, int tile) { return d == 64 ? 3 : tile == 128 ? 2 : 1; }
 
-// How a call is divided: the keys of a query tile in n_q ranges, the queries of a key tile in n_k; the workspace's layout.
+// How a call is divided: its tiles, the keys of a query tile in n_q ranges, the queries of a key tile in n_k; the workspace's layout.
 struct BwdParts {
-  int32_t n_q, n_k;
+  int32_t n_q, n_k, tile;
   int64_t stat_offset, q_offset, k_offset, bytes;  // the plan comes first
 };
 BwdParts bwd_parts(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d,
@@ -100,8 +101,8 @@ BwdParts bwd_parts(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, 
 // What the call needs at least: of forced ranges, or of the undivided call that the library falls back to.
 int64_t bwd_least_workspace(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d,
                             int32_t num_splits);
-// An upper bound of the tiles of one side over all segments: sum of ceil(len / kBwdTile).
-int64_t bwd_tiles(int32_t nseq, int32_t most, int32_t total);
+// An upper bound of the tiles of one side over all segments: sum of ceil(len / tile).
+int64_t bwd_tiles(int32_t nseq, int32_t most, int32_t total, int32_t tile);
 
 hipError_t configure_kernels();
 hipError_t launch_rope(const RopeArgs& a, hipStream_t st);

@@ -19,18 +19,30 @@ int32_t rope_bwd_blocks(int32_t T, int32_t q_heads, int32_t k_heads, int32_t d) 
   return (int32_t)std::min<int64_t>(kRopeBwdBlocks, ceil_div(steps, kRopeThreads / 64));
 }
 
-int64_t bwd_tiles(int32_t nseq, int32_t most, int32_t total) {
+int64_t bwd_tiles(int32_t nseq, int32_t most, int32_t total, int32_t tile) {
   // each segment fills all its tiles but the last, and has one more at most
-  return std::min<int64_t>(nseq * ceil_div(most, kBwdTile), (int64_t)total / kBwdTile + std::min(nseq, total));
+  return std::min<int64_t>(nseq * ceil_div(most, tile), (int64_t)total / tile + std::min(nseq, total));
 }
 
 namespace {
 struct Call {
   int64_t tiles_q, tiles_k, rows_q, rows_k;
-  int32_t d;
+  int32_t d, tile;
 };
+
+// d = 64 has tiles of 128 rows, three workgroups of four waves to a CU: 16380 x 16380 x 24 heads 4.79 ms, in tiles of 256 (two waves to a
+// SIMD) 5.03.  At d = 128 tiles of 256 rows read the other side half as often (32768 x 32768 x 12 heads 17.4 ms instead of
+// 18.4); where these are fewer than the CUs of an MI355X, those of 128 end sooner: 1024 x 1024 x 12 heads 42 us
+// instead of 49, 256 x 256 x 12 heads 20 instead of 28, 1560 x 1560 x 12 77 instead of 80 (8190 x 8190 x 4, 256 tiles, 398
+// instead of 390).
+Call call(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d) {
+  const bool large = d == 128 && H * (bwd_tiles(nseq, max_q, total_q, 256) + bwd_tiles(nseq, max_k, total_k, 256)) >= 256;
+  const int32_t tile = large ? 256 : 128;
+  return {bwd_tiles(nseq, max_q, total_q, tile), bwd_tiles(nseq, max_k, total_k, tile), (int64_t)total_q * H, (int64_t)total_k * H, d, tile};
+}
+
 BwdParts layout(const Call& c, int32_t n_q, int32_t n_k) {
-  BwdParts p{n_q, n_k, 0, 0, 0, 0};
+  BwdParts p{n_q, n_k, c.tile, 0, 0, 0, 0};
   p.stat_offset = align256((int64_t)sizeof(BwdPlan) + (c.tiles_q * n_q + c.tiles_k * n_k) * (int64_t)sizeof(BwdTile));
   p.q_offset = p.stat_offset + align256(2 * c.rows_q * 4);
   p.k_offset = p.q_offset + (n_q > 1 ? align256(n_q * c.rows_q * c.d * 4) : 0);
@@ -63,21 +75,20 @@ double ends(int64_t cus, int64_t a_items, double a, int64_t b_items, double b) {
 }
 }  // namespace
 
-// The ranges that the library takes: those whose call ends first by an estimate, in us as measured.  A product of a tile and a
-// step takes kProduct of them where all CUs are at work (three to a step for dq, four for dk and dv); a workgroup kItem beside its
-// steps; joining ranges kJoin and, to write and read them, kMegabyte each.  32760 x 32760 x 12 heads (d = 128) are not
-// divided; 1560 x 32760 x 12 takes 1050 with one range of keys and 930 with three, 1024 x 1024 x 2 heads (d = 64) 36 and 25
-// with four.
+// The ranges that the library takes: those whose call ends first by an estimate, in us as measured.  A CU takes `product` of them for
+// the product of a tile and 64 rows (three for dq, four for dk and dv), and at least `alone` of them pass in a workgroup, or as
+// many as those that share its CU take; beside its products an item takes kItem; joining ranges kJoin and, to write and read them, kMegabyte each.  1560 x 32760 x 12
+// heads (d = 128) take 1090 with one range of keys and 950 with three, 1560 x 1560 x 2 heads (d = 64) 34 and 25 with four.
 BwdParts bwd_parts(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d,
                    int32_t num_splits, int64_t workspace, int32_t cus) {
-  const Call c{bwd_tiles(nseq, max_q, total_q), bwd_tiles(nseq, max_k, total_k), (int64_t)total_q * H, (int64_t)total_k * H, d};
+  const Call c = call(nseq, max_q, max_k, total_q, total_k, H, d);
   if (num_splits > 0) return layout(c, num_splits, num_splits);
-  const double kProduct = d == 128 ? 0.8 : 0.92, kItem = 4.0, kJoin = 8.0, kMegabyte = 0.43;
+  const double product = d == 64 ? 0.23 : c.tile == 256 ? 0.81 : 0.43, alone = d == 64 ? 0.27 : c.tile == 256 ? 0.81 : 0.64;
+  const double kItem = 3.0, kJoin = 8.0, kMegabyte = 0.43;
   const int64_t items_q = c.tiles_q * H, items_k = c.tiles_k * H;
   if (items_q == 0 || items_k == 0 || items_q + items_k >= 16 * (int64_t)cus) return layout(c, 1, 1);  // (the last ones matter little)
-  // rows that stream past a tile: of uneven segments, between the longest's and the mean
-  const int32_t step = bwd_step(d);
-  auto steps = [&](int32_t most, int32_t total) { return (int32_t)ceil_div(((int64_t)most + std::min(most, total / nseq)) / 2, step); };
+  // steps of 64 rows that stream past a tile: of uneven segments, between the longest's and the mean
+  auto steps = [&](int32_t most, int32_t total) { return (int32_t)ceil_div(((int64_t)most + std::min(most, total / nseq)) / 2, 64); };
   const int32_t steps_k = std::max(1, steps(max_k, total_k)), steps_q = std::max(1, steps(max_q, total_q));
   const double part = kMegabyte * 4e-6 * d;
   double least = 0;
@@ -86,8 +97,11 @@ BwdParts bwd_parts(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, 
     if (n_q > steps_k) break;
     for (int32_t n_k : {1, 2, 3, 4, 6, 8, 12, 16}) {
       if (n_k > steps_q) break;
-      const double q = 3 * kProduct * ((steps_k + n_q - 1) / n_q) + kItem, k = 4 * kProduct * ((steps_q + n_k - 1) / n_k) + kItem;
-      double t = q > k ? ends(cus, items_q * n_q, q, items_k * n_k, k) : ends(cus, items_k * n_k, k, items_q * n_q, q);
+      const int32_t in_q = 3 * ((steps_k + n_q - 1) / n_q), in_k = 4 * ((steps_q + n_k - 1) / n_k);  // products of an item
+      const double q = product * in_q + kItem, k = product * in_k + kItem;
+      double t = in_q > in_k ? ends(cus, items_q * n_q, q, items_k * n_k, k) : ends(cus, items_k * n_k, k, items_q * n_q, q);
+      const int64_t beside = std::min<int64_t>(bwd_groups(d, c.tile), (items_q * n_q + items_k * n_k) / cus + 1);
+      t = std::max(t, std::max(alone, product * (double)beside) * std::max(in_q, in_k) + kItem);
       if (n_q * n_k > 1) t += kJoin + part * (double)((n_q > 1 ? n_q * c.rows_q : 0) + (n_k > 1 ? 2 * n_k * c.rows_k : 0));
       if (least != 0 && t >= 0.97 * least) continue;
       if (n_q * n_k > 1 && layout(c, n_q, n_k).bytes > workspace) continue;
@@ -101,8 +115,7 @@ BwdParts bwd_parts(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, 
 
 int64_t bwd_least_workspace(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d,
                             int32_t num_splits) {
-  const Call c{bwd_tiles(nseq, max_q, total_q), bwd_tiles(nseq, max_k, total_k), (int64_t)total_q * H, (int64_t)total_k * H, d};
-  return layout(c, std::max(1, num_splits), std::max(1, num_splits)).bytes;
+  return layout(call(nseq, max_q, max_k, total_q, total_k, H, d), std::max(1, num_splits), std::max(1, num_splits)).bytes;
 }
 
 }  // namespace tsblock

@@ -158,6 +158,8 @@ int validate(const int32_t* cu_q, const int32_t* cu_k, int32_t nseq, int32_t max
 
 constexpr float kLeastScale = 0x1p-100f, kMostScale = 0x1p100f;
 
+constexpr int kLeastTile = 128;  // held rows of a workgroup, at least
+
 // Sizes of an attention gradient call.
 int check_sizes(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d, int32_t num_splits) {
   if (d != 64 && d != 128) return TS_ERR_HEAD_DIM;
@@ -166,9 +168,9 @@ int check_sizes(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int
   const int64_t row_bytes = (int64_t)H * d * 2;
   if (row_bytes >= kByteLimit || std::max(max_q, max_k) + (int64_t)256 > (kByteLimit - 1) / row_bytes) return TS_ERR_SHAPE;
   // H < 2^24 and tiles < 2^24 from here on, so the products below are within 64 bits
-  const int64_t tiles = (int64_t)max_q / tsblock::kBwdTile + max_k / tsblock::kBwdTile + 2;
+  const int64_t tiles = (int64_t)max_q / kLeastTile + max_k / kLeastTile + 2;
   if ((int64_t)nseq * H >= (int64_t)1 << 26 || (int64_t)nseq * H * tiles >= (int64_t)1 << 26) return TS_ERR_SHAPE;
-  if (H * ((int64_t)std::max(total_q, total_k) / tsblock::kBwdTile + nseq) >= (int64_t)1 << 19) return TS_ERR_SHAPE;
+  if (H * ((int64_t)std::max(total_q, total_k) / kLeastTile + nseq) >= (int64_t)1 << 19) return TS_ERR_SHAPE;
   return TS_OK;
 }
 
@@ -279,7 +281,7 @@ int ts_attn_bwd(const void* d_o, const void* q, const void* k, const void* v, co
   char* const w = (char*)workspace;
   return launched(tsblock::launch_attn_bwd({d_o, q, k, v, o, lse, dq, dk, dv, cu_seqlens_q, cu_seqlens_k, (tsblock::BwdPlan*)w,
                                             (float*)(w + p.stat_offset), (float*)(w + p.q_offset), (float*)(w + p.k_offset), nseq, max_seqlen_q, max_seqlen_k,
-                                            total_q, total_k, H, d, p.n_q, p.n_k, scale}, s));
+                                            total_q, total_k, H, d, p.n_q, p.n_k, p.tile, scale}, s));
 }
 
 int64_t ts_attn_bwd_workspace(int32_t nseq, int32_t max_seqlen_q, int32_t max_seqlen_k, int32_t total_q,
