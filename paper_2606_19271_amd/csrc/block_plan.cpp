@@ -102,8 +102,8 @@ BwdParts bwd_parts(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, 
       double t = in_q > in_k ? ends(cus, items_q * n_q, q, items_k * n_k, k) : ends(cus, items_k * n_k, k, items_q * n_q, q);
       const int64_t beside = std::min<int64_t>(bwd_groups(d, c.tile), (items_q * n_q + items_k * n_k) / cus + 1);
       t = std::max(t, std::max(alone, product * (double)beside) * std::max(in_q, in_k) + kItem);
-      if (n_q * n_k > 1) t += kJoin + part * (double)((n_q > 1 ? n_q * c.rows_q : 0) + (n_k > 1 ? 2 * n_k * c.rows_k : 0));
-      if (least != 0 && t >= 0.97 * least) continue;
+      if (n_q * n_k > 1) t += 0.03 * t + kJoin + part * (double)((n_q > 1 ? n_q * c.rows_q : 0) + (n_k > 1 ? 2 * n_k * c.rows_k : 0));
+      if (least != 0 && t >= least) continue;
       if (n_q * n_k > 1 && layout(c, n_q, n_k).bytes > workspace) continue;
       least = t;
       best_q = n_q;

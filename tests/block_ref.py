@@ -10,6 +10,7 @@ HALF = 2.0 ** -8  # half a bfloat16 step, relative to the value
 # of sums and functions in 32 bits, relative to the sum of their terms' magnitudes: 2^-24 a rounding, at most 256 of
 # them in a chain (128 channels, each a product and a sum)
 FINE = 2.0 ** -16
+LEAST = 2.0 ** -126  # the least normal number of both types
 
 
 def angles(pos, freq, axes):
@@ -76,7 +77,9 @@ def attn(q, k, v, scale):
 
 
 def attn_bwd(d_o, q, k, v, o, lse, scale):
-    """(dq, dk, dv) of one segment and head and how far each element may be off.  P and S = P (d_o v - D) are rounded to
+    """(dq, dk, dv) of one segment and head and how far each element may be off.  What is below 2^-126 in 32 bits or bfloat16 may
+    count as 0 (the GPU's exp2 and matrix products have no smaller numbers): P by 2^-126, S by that times what it is P times
+    of, and by 2^-126.  P and S = P (d_o v - D) are rounded to
     bfloat16 (each off by HALF at most, one way or the other: of n such terms t the sum is off by HALF sum |t| at the very most, and
     by 6 sqrt(sum t^2) HALF in one of 10^7 cases), all before that are sums in 32 bits, the results are rounded
     once more."""
@@ -89,6 +92,7 @@ def attn_bwd(d_o, q, k, v, o, lse, scale):
     # off before the rounding: the exponent's argument, and t's two sums
     arg = FINE * (abs(scale) * (q.abs() @ k.abs().T) + lse.abs()[:, None]) + FINE
     ps, ss = p * arg, s.abs() * arg + p * FINE * (d_o.abs() @ v.abs().T + (d_o * o).abs().sum(1, keepdim=True))
+    ps, ss = ps + LEAST, ss + LEAST * (1 + t.abs())
 
     def product(w, slack, x):  # w^T x
         terms = torch.minimum(w.abs().T @ x.abs(), 6 * torch.sqrt((w * w).T @ (x * x)))
@@ -99,7 +103,7 @@ def attn_bwd(d_o, q, k, v, o, lse, scale):
     dq, e_q = product(s.T, ss.T * (1 + HALF), k)
     got = [scale * dq, scale * dk, dv]
     off = [abs(scale) * e_q, abs(scale) * e_k, e_v]
-    return got, [HALF * x.abs() + (1 + HALF) * e + 2.0 ** -133 for x, e in zip(got, off)]
+    return got, [HALF * x.abs() + (1 + HALF) * e + LEAST for x, e in zip(got, off)]
 
 
 def segments(cu_q, cu_k):
