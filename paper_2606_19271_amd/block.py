@@ -68,40 +68,58 @@ _Words = {n: ctypes.c_int64 * n for n in (10, 16, 22)}
 _NO_ROWS = (0, 0, 0)
 
 
-def _rows(name, t, shape, index):
-    """The words of a tensor [T, heads, d] whose tokens may be any distance apart."""
+_TOP = (1 << 31) - 1
+
+
+def _refuse_rows(name, t, shape):
     if not isinstance(t, Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
-    if t.dtype is not _BF16 or t.dim() != 3 or t.get_device() != index:
-        raise ValueError("%s must be a bfloat16 [T, heads, d] tensor on q's GPU" % name)
-    if t.shape != shape:
+    if shape is not None and t.shape != shape:
         raise ValueError("%s must be %s" % (name, list(shape)))
+    raise ValueError("%s must be a bfloat16 [T, heads, d] tensor on q's GPU" % name)
+
+
+def _rows(name, t, shape, index):
+    """The words of a tensor [T, heads, d] whose tokens may be any distance apart."""
+    if not isinstance(t, Tensor) or t.dtype is not _BF16 or t.shape != shape or t.get_device() != index:
+        _refuse_rows(name, t, shape)
     T, heads, d = shape
     stride, head, channel = t.stride()
     if T < 2:  # (the stride of a single token says nothing)
         stride = max(heads * d, 1)
-    if T and ((heads > 1 and head != d) or (d > 1 and channel != 1) or stride < heads * d):
+    if (channel != 1 and d > 1 or head != d and heads > 1 or stride < heads * d) and T:
         raise ValueError("%s must have the heads of a token side by side" % name)
     return t.data_ptr(), stride, heads
 
 
+def _out_rows(name, out, like, shape, index):
+    """An output tensor, new or as given, and its words."""
+    if out is None:
+        out = like.new_empty(shape)
+        _, heads, d = shape
+        return out, (out.data_ptr(), heads * d, heads)
+    return out, _rows(name, out, shape, index)
+
+
 def _first(name, t):
-    """Shape, device and its index of the tensor that the others have to match."""
-    if not isinstance(t, Tensor):
-        raise TypeError("%s must be a torch.Tensor" % name)
-    if not t.is_cuda or t.dim() != 3:
-        raise ValueError("%s must be a bfloat16 [T, heads, d] GPU tensor" % name)
+    """Shape, device and its index of the tensor that the others have to match, which is of rows of heads."""
+    if not isinstance(t, Tensor) or t.dtype is not _BF16 or t.dim() != 3 or not t.is_cuda:
+        _refuse_rows(name, t, None)
+    shape = t.shape
+    if max(shape) > _TOP:
+        raise ValueError("%s = %s does not fit the C ABI's int32" % (name, list(shape)))
     dev = t.device
-    return t.shape, dev, dev.index
+    return shape, dev, dev.index
 
 
 def _beside(name, t, shape):
     """The shape of q's companion: its T and d, any heads."""
     if not isinstance(t, Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
-    if t.dim() != 3 or t.shape[0] != shape[0] or t.shape[2] != shape[2]:
+    other = t.shape
+    if len(other) != 3 or other[0] != shape[0] or other[2] != shape[2] or other[1] > _TOP:
         raise ValueError("%s must be [%d, heads, %d]" % (name, shape[0], shape[2]))
-    return t.shape
+    return other
 
 
 def _weight(name, w, d, index):
@@ -137,23 +155,21 @@ def ts_qk_rope(q, k, pos=None, rope=None, q_weight=None, k_weight=None, eps=1e-6
     shape, dev, index = _first("q", q)
     T, _, d = shape
     k_at = ko_at = None
-    if q_out is None:
-        q_out = q.new_empty(shape, dtype=_BF16)
+    q_out, out = _out_rows("q_out", q_out, q, shape, index)
+    head = *_rows("q", q, shape, index), *out, *_rope_words(pos, rope, T, d, index)
     if k is not None:
         k_shape = _beside("k", k, shape)
-        if k_out is None:
-            k_out = q.new_empty(k_shape, dtype=_BF16)
-        words = _Words[16](*_rows("q", q, shape, index), *_rows("q_out", q_out, shape, index), *_rope_words(pos, rope, T, d, index),
-                           *_rows("k", k, k_shape, index), *_rows("k_out", k_out, k_shape, index))
+        k_out, out = _out_rows("k_out", k_out, q, k_shape, index)
+        words = _Words[16](*head, *_rows("k", k, k_shape, index), *out)
         at = ctypes.addressof(words)
         k_at, ko_at = at + 80, at + 104
     else:
         if k_out is not None or k_weight is not None:
             raise ValueError("k_out and k_weight need k")
-        words = _Words[10](*_rows("q", q, shape, index), *_rows("q_out", q_out, shape, index), *_rope_words(pos, rope, T, d, index))
+        words = _Words[10](*head)
         at = ctypes.addressof(words)
     _call(load_block().ts_qk_rope, dev, at, k_at, at + 24, ko_at, _weight("q_weight", q_weight, d, index),
-          _weight("k_weight", k_weight, d, index), None if rope is None else at + 48, *_lib.i32s(T=T, d=d), eps)
+          _weight("k_weight", k_weight, d, index), None if rope is None else at + 48, T, d, eps)
     return q_out, k_out
 
 
@@ -165,16 +181,14 @@ def ts_qk_rope_bwd(dq_out, dk_out, q, k, pos=None, rope=None, q_weight=None, k_w
     shape, dev, index = _first("dq_out", dq_out)
     T, Hq, d = shape
     Hk = 0
-    if dq is None:
-        dq = dq_out.new_empty(shape, dtype=_BF16)
-    go, gq = _rows("dq_out", dq_out, shape, index), _rows("dq", dq, shape, index)
+    go = _rows("dq_out", dq_out, shape, index)
+    dq, gq = _out_rows("dq", dq, dq_out, shape, index)
     ho = hk = k_rows = q_rows = _NO_ROWS
     if dk_out is not None:
         k_shape = _beside("dk_out", dk_out, shape)
         Hk = k_shape[1]
-        if dk is None:
-            dk = dq_out.new_empty(k_shape, dtype=_BF16)
-        ho, hk = _rows("dk_out", dk_out, k_shape, index), _rows("dk", dk, k_shape, index)
+        ho = _rows("dk_out", dk_out, k_shape, index)
+        dk, hk = _out_rows("dk", dk, dq_out, k_shape, index)
     elif k is not None or dk is not None or k_weight is not None:
         raise ValueError("k, dk and k's weight need dk_out")
     if q_weight is not None:
@@ -199,14 +213,13 @@ def ts_qk_rope_bwd(dq_out, dk_out, q, k, pos=None, rope=None, q_weight=None, k_w
         wk = gwk = None
     words = _Words[22](*go, *gq, *_rope_words(pos, rope, T, d, index), *ho, *hk, *q_rows, *k_rows)
     at = ctypes.addressof(words)
-    sizes = _lib.i32s(T=T, d=d)
     lib = load_block()
     need = lib.ts_qk_rope_bwd_workspace(T, Hq, Hk, d) if wq or wk else 0
     # from torch's allocator: the memory goes back to the current stream's pool (or, while a graph is
     # captured, the graph's own) when the call is enqueued, so no other work meets it
     work = dq_out.new_empty(need, dtype=_U8) if need > 0 else None
     _call(lib.ts_qk_rope_bwd, dev, at, at + 80 if Hk else None, at + 128 if wq else None, at + 152 if wk else None, at + 24,
-          at + 104 if Hk else None, wq, wk, gwq, gwk, None if rope is None else at + 48, *sizes, eps,
+          at + 104 if Hk else None, wq, wk, gwq, gwk, None if rope is None else at + 48, T, d, eps,
           None if work is None else work.data_ptr(), need)
     return dq, dk, dq_weight, dk_weight
 
