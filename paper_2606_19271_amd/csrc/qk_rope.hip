@@ -1,4 +1,11 @@
 // qk_rope.hip -- norm and rotation of queries and keys in one pass (ts_qk_rope), and its gradients.
+//
+// Both are bound by memory, each row read and written once: 23400 tokens x 80 heads (d = 128) 181 us, 5.3 TB/s read and
+// written, the gradients of 32760 x 80 heads 400 us, 5.0 TB/s with two thirds of it reads (a copy of 1 GB by torch: 5.0).
+// Small calls are bound by the latency of launch, positions and rows: 4 tokens 3.7 us, 1560 x 24 heads 8.0 us.
+// A wave has one step's loads under way while it works on the one before; every 8 to 16 heads share a token's angles,
+// which cost each lane one sine and cosine.  (With the eight of its pairs formed by each lane, and the loads one
+// after the other, 1560 x 24 heads took 17.8 us.)
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -27,20 +34,27 @@ struct Head {
   bf16x8 lo, hi;
 };
 
-template <int D>
+// kFar: past the caches (see `far`).
+template <int D, bool kFar>
 __device__ __forceinline__ Head load_head(const __bf16* p, bool live) {
   if (!live) return Head{};
-  return Head{*(const bf16x8*)p, *(const bf16x8*)(p + D / 2)};
+  const bf16x8 *const lo = (const bf16x8*)p, *const hi = (const bf16x8*)(p + D / 2);
+  return kFar ? Head{__builtin_nontemporal_load(lo), __builtin_nontemporal_load(hi)} : Head{*lo, *hi};
 }
 
-template <int D>
+template <int D, bool kFar>
 __device__ __forceinline__ void store_head(__bf16* p, const float (&x)[16], bool live) {
   if (!live) return;
   bf16x8 lo, hi;
 #pragma unroll
   for (int i = 0; i < 8; ++i) lo[i] = (__bf16)x[i], hi[i] = (__bf16)x[8 + i];
-  *(bf16x8*)p = lo;
-  *(bf16x8*)(p + D / 2) = hi;
+  if (kFar) {
+    __builtin_nontemporal_store(lo, (bf16x8*)p);
+    __builtin_nontemporal_store(hi, (bf16x8*)(p + D / 2));
+  } else {
+    *(bf16x8*)p = lo;
+    *(bf16x8*)(p + D / 2) = hi;
+  }
 }
 
 __device__ __forceinline__ void widen(const Head& h, float (&x)[16]) {
@@ -160,7 +174,7 @@ struct Steps {
   }
 };
 
-template <int D, bool kPairs>
+template <int D, bool kPairs, bool kFar>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int groups_q, int groups, int steps, int per) {
   using G = Geo<D>;
   const int lane = threadIdx.x & 63, wave = uniform(blockIdx.x * kWaves + (threadIdx.x >> 6));
@@ -178,7 +192,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int grou
   };
   bool live;
   const __bf16* from = rows(a.q, a.k, at, live);
-  Head in = load_head<D>(from, live);
+  Head in = load_head<D, kFar>(from, live);
   const double freq = a.rope.freq ? a.rope.freq[lane % (D / 2)] : 0.0;
   load_weights<D>(a.q_weight, j, wq);
   load_weights<D>(a.k_weight, j, wk);
@@ -191,7 +205,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int grou
     if (at.left > 0) {
       bool next_live;
       from = rows(a.q, a.k, at, next_live);
-      after = load_head<D>(from, next_live);
+      after = load_head<D, kFar>(from, next_live);
     }
     float x[16];
     widen(in, x);
@@ -210,16 +224,17 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int grou
       }
     }
     __bf16* const to = rows(a.q_out, a.k_out, here, live);
-    store_head<D>(to, x, live);
+    store_head<D, kFar>(to, x, live);
     if (at.left <= 0) return;
     in = after;
   }
 }
 
-// Gradients.  With g the result's gradient turned back, n = x r the normalised row:
+// Gradients.  As many workgroups as the device holds at once take equal parts of the steps, whatever their number, so that the sums'
+// order is the call's own.  With g the result's gradient turned back, n = x r the normalised row:
 //   dw = sum g n,   dx = r (g w - n mean(g w n))
 // Each wave sums dw over its steps, the workgroup its waves' sums, and rope_bwd_join_kernel those of the workgroups.
-template <int D, bool kPairs>
+template <int D, bool kPairs, bool kFar>
 __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(RopeBwdArgs a, int groups_q, int groups, int steps, int per) {
   using G = Geo<D>;
   const int lane = threadIdx.x & 63, wave = uniform(blockIdx.x * kWaves + (threadIdx.x >> 6));
@@ -238,9 +253,9 @@ __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(RopeBwdArgs a, i
   auto load = [&](Head& dy, Head& x) {
     bool live;
     const __bf16* p = rows(a.dq_out, a.dk_out, at, live);
-    dy = load_head<D>(p, live);
+    dy = load_head<D, kFar>(p, live);
     p = rows(a.q, a.k, at, live);
-    x = load_head<D>(p, live && (at.g >= groups_q ? a.k_weight : a.q_weight));
+    x = load_head<D, kFar>(p, live && (at.g >= groups_q ? a.k_weight : a.q_weight));
   };
   Head dy_in{}, x_in{};
   if (at.left > 0) load(dy_in, x_in);
@@ -283,7 +298,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(RopeBwdArgs a, i
     }
     bool live;
     __bf16* const to = rows(a.dq, a.dk, here, live);
-    store_head<D>(to, g, live);
+    store_head<D, kFar>(to, g, live);
     dy_in = dy_next;
     x_in = x_next;
   }
@@ -336,14 +351,21 @@ __global__ __launch_bounds__(1024) void rope_bwd_join_kernel(const float* part, 
 
 int64_t ceil_div(int64_t a, int64_t b) { return a / b + (a % b != 0); }
 
+// Whether a call of so many bytes reads and writes past the caches, which do not hold them for another reader then: 40 + 40 heads (d = 128),
+// plain and past the caches, us: 6000 tokens (246 MB) 40 and 48, 8000 (328 MB) 63 and 60, 24000 (983 MB) 182 and 172,
+// their gradients of 24000 (1.5 GB) 308 and 300.
+bool far(int64_t bytes) { return bytes > (int64_t)256 << 20; }
+
 template <int D>
 hipError_t rope(const RopeArgs& a, hipStream_t st) {
   const int gq = (int)ceil_div(a.q.heads, Geo<D>::kHeads), groups = gq + (int)ceil_div(a.k.heads, Geo<D>::kHeads);
   const int steps = a.T * groups;
   const int per = (int)std::max({(int64_t)1, std::min<int64_t>(groups, ceil_div(steps, 4096)), ceil_div(steps, (int64_t)1 << 24)});
   const unsigned blocks = (unsigned)ceil_div(ceil_div(steps, per), kWaves);
-  if (a.rope.interleaved) rope_kernel<D, true><<<blocks, kRopeThreads, 0, st>>>(a, gq, groups, steps, per);
-  else rope_kernel<D, false><<<blocks, kRopeThreads, 0, st>>>(a, gq, groups, steps, per);
+  const bool pairs = a.rope.interleaved, past = far((int64_t)a.T * (a.q.heads + a.k.heads) * D * 4);
+  auto kernel = pairs ? past ? rope_kernel<D, true, true> : rope_kernel<D, true, false>
+                      : past ? rope_kernel<D, false, true> : rope_kernel<D, false, false>;
+  kernel<<<blocks, kRopeThreads, 0, st>>>(a, gq, groups, steps, per);
   return hipGetLastError();
 }
 
@@ -354,8 +376,10 @@ hipError_t rope_bwd(const RopeBwdArgs& a, hipStream_t st) {
   const int blocks = rope_bwd_blocks(a.T, a.dq.heads, a.dk.heads, D);
   const int per = blocks ? (int)ceil_div(steps, (int64_t)blocks * kWaves) : 1;
   if (blocks > 0) {
-    if (a.rope.interleaved) rope_bwd_kernel<D, true><<<blocks, kRopeThreads, 0, st>>>(a, gq, groups, steps, per);
-    else rope_bwd_kernel<D, false><<<blocks, kRopeThreads, 0, st>>>(a, gq, groups, steps, per);
+    const bool pairs = a.rope.interleaved, past = far((int64_t)a.T * (a.dq.heads + a.dk.heads) * D * 6);
+    auto kernel = pairs ? past ? rope_bwd_kernel<D, true, true> : rope_bwd_kernel<D, true, false>
+                        : past ? rope_bwd_kernel<D, false, true> : rope_bwd_kernel<D, false, false>;
+    kernel<<<blocks, kRopeThreads, 0, st>>>(a, gq, groups, steps, per);
   }
   if (a.dq_weight || a.dk_weight) rope_bwd_join_kernel<D><<<2 * D / 16, 1024, 0, st>>>(a.part, blocks, a.dq_weight, a.dk_weight);
   return hipGetLastError();
