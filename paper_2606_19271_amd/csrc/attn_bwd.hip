@@ -180,10 +180,9 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
       const int row = 4 * g + r;
       off[u] = (row < kBN ? row : 0) * row_bytes + (byte < D * 2 ? byte : 0);
     }
-    // Rows past the segment's end read as zeros.  Fetches past the range's last step stop at the segment's end, so that
-    // no offset exceeds (len + 2 kBN - 1) rows.
+    // Rows past the segment's end read as zeros.  The fetches after the range's last step bring its first one again.
     auto fetch = [&](int j, lds_char* stage) {
-      const int step = min(begin + j, steps_all), skip = step * kBN * row_bytes;
+      const int step = begin + (j < steps ? j : 0), skip = step * kBN * row_bytes;
 #pragma unroll
       for (int u = 0; u < G::kDmaMax; ++u) {
         const int i = wave + W * u;
@@ -222,10 +221,19 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
     const float c = a.c;
     const bool active = row0 < held_len;
 
+    // dq: the sums over the keys of R as it is and as it is rounded.  Rounding makes dq off by the sum of (rounded R - R) k; keys that
+    // have much in common, as those of a trained model's outlier channels do, add that part up while the gradient, whose
+    // R sum to next to nothing, loses it.  So the difference of the two sums times a mean of keys is taken off again at the end.
+    // Of keys whose mean is as large as they spread, dq is then off by 0.0024 of its norm instead of 0.0029 (0.0017 is its own
+    // rounding).  It costs 2 % at d = 128 and 4 % at d = 64.
+    float exact = 0;
+    f32x4 rounded = {};  // (every element: the lane's query's, by the matrix core)
+    const bf16x8 sel = row_sum_selector(lane);
+
     // One step.  The order of its products and reads is pinned: each operand is read a product before it is used (more ahead
     // measured the same), and the vector work on a product's result goes between products that do not wait for it.  Left to the
     // compiler's order 32760 x 32760 x 12 heads took 17.75 ms instead of 17.4, 16380 x 16380 x 24 heads of d = 64 5.1 instead of
-    // 5.0.  ragged: rows from `left` on are past the segment's end; their P and R are 0.
+    // 5.0 (both without the sums of R below).  ragged: rows from `left` on are past the segment's end; their P and R are 0.
     constexpr int kM = D / 16;  // MFMAs of a product
         constexpr bool kPair = !kKeys && kBN >= 64;  // dq: two blocks at a time
     constexpr int kBlocks = kBN / (kPair ? 64 : 32), kPer = (kKeys ? 4 : kPair ? 6 : 3) * kM, kAll = kBlocks * kPer;
@@ -258,6 +266,7 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
         float x = s[w][r] * t[w][r];
         if (decltype(ragged)::value && row + 8 * (r >> 2) + 4 * hb + (r & 3) >= left) x = 0.0f;
         ds[w][r >> 3][r & 7] = (__bf16)x;
+        if (!kKeys) exact = __builtin_fmaf(s[w][r], t[w][r], exact);  // (P is 0 past the end)
       };
       // element range of slot m of a phase: nothing in the first, whose product waits for the result
       auto from = [](int m) { return m < 1 ? 0 : 2 * ((8 * (m - 1) + kM - 2) / (kM - 1)); };
@@ -290,6 +299,10 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
           if (phase == 0 || (kPair && phase == 2)) s[w] = mfma32(x, y1[m], m == 0 ? f32x16{} : s[w]);
           else if (phase == 1 || (kPair && phase == 3)) t[w] = mfma32(x, y2[m], m == 0 ? splat(ld) : t[w]);
           else acc1[m % (D / 32)] = mfma32(x, ds[w][m / (D / 32)], acc1[m % (D / 32)]);
+          if (phase >= (kPair ? 4 : 2) && m == kM - 1) {
+            rounded = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sel, ds[w][0], rounded, 0, 0, 0);
+            rounded = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sel, ds[w][1], rounded, 0, 0, 0);
+          }
 #pragma unroll
           for (int r = from(m); r < from(m + 1); ++r) {
             if (phase == 1) weight(0, r, (kPair ? 64 : 32) * b);
@@ -325,7 +338,25 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
     }
     wait_lds();
     wait_vmem<0>();
-    block_sync();  // the next item's fetches come into stages that nobody reads or fills any more
+    block_sync();
+    if (!kKeys && active) {
+      // the mean of the range's first 32 keys, which have come again after its last step
+      const lds_char* const first = lds + slot * G::kStage + tr_lane;
+      const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3d003d00u, 0x3d003d00u, 0x3d003d00u, 0x3d003d00u});  // 1 / 32
+      const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(exact), __float_as_uint(exact), false, false);
+      exact = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
+      float off = (rounded[0] - exact) * (32.0f / (float)min(32, len - begin * kBN));
+      // that product has query l + 16 beside query l, times 0: where the one is not finite, the other keeps its rounding
+      if (fabsf(exact) < INFINITY && !(fabsf(off) < INFINITY)) off = 0;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        f32x16 mean = {};
+        mean = mfma32(columns_operand<G::kGroup>(first + 64 * db), ones, mean);
+        mean = mfma32(columns_operand<G::kGroup>(first + 4 * G::kGroup + 64 * db), ones, mean);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc1[db][r] = __builtin_fmaf(-off, mean[r], acc1[db][r]);
+      }
+    }
   }
 
   // accumulator register 4 g + r of block db: channel 32 db + 8 g + 4 hb + r of the lane's row

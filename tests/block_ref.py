@@ -100,7 +100,10 @@ def attn_bwd(d_o, q, k, v, o, lse, scale):
 
     dv, e_v = product(p, ps * (1 + HALF), d_o)
     dk, e_k = product(s, ss * (1 + HALF), q)
-    dq, e_q = product(s.T, ss.T * (1 + HALF), k)
+    # dq may be formed of the keys less a vector m within their own range, the mean of some (the sum of S less its rounded values'
+    # is known in 32 bits and goes back to m): |k - m| then is |k| and the largest |k| of the channel at most
+    dq, e_q = product(s.T, ss.T * (1 + HALF), k.abs() + k.abs().amax(0))
+    dq = s @ k
     got = [scale * dq, scale * dk, dv]
     off = [abs(scale) * e_q, abs(scale) * e_k, e_v]
     return got, [HALF * x.abs() + (1 + HALF) * e + LEAST for x, e in zip(got, off)]
