@@ -80,18 +80,10 @@ struct Item {
 
 // Item `at` of the list of entry t, of a side with n ranges.  Its head, range and tile go by the list's own order over the XCDs,
 // so that each of them gets an equal part of every list, and neighbours on it stream the same rows.
-__device__ __forceinline__ Item find_item(const BwdTile* t, int at, int heads, int n) {
-  at = remap_block(at - t->first * heads, t->tiles * n * heads, 32);
-  Item w;
-  const int j = at / t->tiles;
-  w.tile = at - j * t->tiles;
-  w.h = j / n;
-  w.split = j - w.h * n;
-  w.held0 = t->held0;
-  w.held_len = t->held_len;
-  w.str0 = t->str0;
-  w.str_len = t->str_len;
-  return w;
+__device__ __forceinline__ Item find_item(const BwdTile& t, int at, int heads, int n) {
+  at = remap_block(at - t.first * heads, t.tiles * n * heads, 32);
+  const int j = at / t.tiles;
+  return Item{j / n, at - j * t.tiles, j % n, t.held0, t.held_len, t.str0, t.str_len};
 }
 
 typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
@@ -124,6 +116,63 @@ __device__ __forceinline__ f32x16 row_statistics(const lds_char* __restrict__ x,
 
 __device__ __forceinline__ f32x16 splat(float x) { return f32x16{x, x, x, x, x, x, x, x, x, x, x, x, x, x, x, x}; }
 
+// A wave's 32 rows of results leave through LDS, in pieces of 128 bytes a row: straight from the accumulators every
+// store would touch 32 rows with 16 bytes each.  Rows past the segment's end are dropped by the range check.
+constexpr int kOutRow = 128 + 16;  // bytes
+constexpr int kOutWave = 32 * kOutRow;
+
+template <int D>
+__device__ __forceinline__ void write_rows(const f32x16 (&acc)[D / 32], float f, __bf16* to, int row0, int len, int H, lds_char* out,
+                                           int lane) {
+  const int row_bytes = H * D * 2, hb = lane >> 5, r = lane >> 3, chunk = lane & 7;
+  const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(to, (uint32_t)(len - 1) * (uint32_t)row_bytes + D * 2);
+  lds_char* const put = out + (lane & 31) * kOutRow + 8 * hb;
+  const lds_char* const get = out + r * kOutRow + 16 * chunk;
+  auto in_order = [] { __asm__ volatile("" ::: "memory"); };  // (the accesses of a wave are in order in the LDS)
+#pragma unroll
+  for (int d0 = 0; d0 < D / 32; d0 += 2) {
+#pragma unroll
+    for (int db = d0; db < d0 + 2; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 x = {acc[db][4 * g] * f, acc[db][4 * g + 1] * f, acc[db][4 * g + 2] * f, acc[db][4 * g + 3] * f};
+        *(lds_u32x2*)(put + 64 * (db - d0) + 16 * g) = __builtin_bit_cast(u32x2, __builtin_convertvector(x, bf16x4));
+      }
+    in_order();
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      __builtin_amdgcn_raw_buffer_store_b128(*(const lds_u32x4*)(get + 8 * u * kOutRow), rsrc,
+                                             (row0 + r + 8 * u) * row_bytes + 64 * d0 + 16 * chunk, 0, 0);
+    in_order();
+  }
+}
+
+// The same in 32 bits, of one range.
+template <int D>
+__device__ __forceinline__ void write_part(const f32x16 (&acc)[D / 32], float* to, int row0, int len, int H, lds_char* out, int lane) {
+  // (offsets of up to twice those of 16-bit rows, unsigned)
+  const uint32_t row_bytes = (uint32_t)(H * D) * 4u;
+  const int hb = lane >> 5, r = lane >> 3, chunk = lane & 7;
+  const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(to, (uint32_t)(len - 1) * row_bytes + D * 4);
+  lds_char* const put = out + (lane & 31) * kOutRow + 16 * hb;
+  const lds_char* const get = out + r * kOutRow + 16 * chunk;
+  auto in_order = [] { __asm__ volatile("" ::: "memory"); };
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 x = {acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]};
+      *(lds_u32x4*)(put + 32 * g) = __builtin_bit_cast(u32x4, x);
+    }
+    in_order();
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      __builtin_amdgcn_raw_buffer_store_b128(*(const lds_u32x4*)(get + 8 * u * kOutRow), rsrc,
+                                             __builtin_bit_cast(int, (uint32_t)(row0 + r + 8 * u) * row_bytes + 128u * db + 16u * chunk), 0, 0);
+    in_order();
+  }
+}
+
 // One item of the dq (kKeys = false) or the dk, dv side.
 template <int D, int W, bool kKeys>
 __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_char* lds) {
@@ -148,6 +197,7 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
 #pragma unroll
   for (int i = 0; i < (kKeys ? D / 32 : 1); ++i) acc2[i] = f32x16{};
 
+  int slot = 0;  // stage of the step to come
   if (steps > 0) {
     const uint32_t held_bytes = (uint32_t)(held_len - 1) * (uint32_t)row_bytes + D * 2;
     const uint32_t str_bytes = (uint32_t)(len - 1) * (uint32_t)row_bytes + D * 2;
@@ -319,7 +369,6 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
       }
     };
 
-    int slot = 0;
     auto open_step = [&](int j) {  // step j's stage, complete; the next fetch, into the stage that step j - 1 was read from
       wait_lds();
       wait_vmem<(G::kStages - 2) * 2 * G::kDmaMin>();  // step j is here, step j + 1 of three may be on its way
@@ -359,48 +408,28 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
     }
   }
 
-  // accumulator register 4 g + r of block db: channel 32 db + 8 g + 4 hb + r of the lane's row
-  const int row = row0 + col;
-  if (row >= held_len) return;
-  const float scale = a.scale;
+  // The results: registers 4 g + r of block db are channels 32 db + 8 g + 4 hb + r of the lane's row.  (Where there were steps, LDS
+  // is free but for the stage `slot`, which may still be read.)
+  lds_char* const out = lds + (slot == 0 ? 1 : 0) * G::kStage + wave * kOutWave;
+  static_assert(W * kOutWave <= G::kStage, "the waves' output fits a stage");
   if (n > 1) {
     const int64_t rows = (int64_t)(kKeys ? a.total_k : a.total_q) * a.H * D;
-    float* const to = (kKeys ? a.part_k : a.part_q) + w.split * rows + held0 + (int64_t)row * a.H * D + 4 * hb;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        *(f32x4*)(to + 32 * db + 8 * g) = f32x4{acc1[db][4 * g], acc1[db][4 * g + 1], acc1[db][4 * g + 2], acc1[db][4 * g + 3]};
-        if (kKeys)
-          *(f32x4*)(to + a.n_k * rows + 32 * db + 8 * g) =
-              f32x4{acc2[db][4 * g], acc2[db][4 * g + 1], acc2[db][4 * g + 2], acc2[db][4 * g + 3]};
-      }
-    return;
+    const int64_t at = w.split * rows + held0;
+    write_part<D>(acc1, (kKeys ? a.part_k : a.part_q) + at, row0, held_len, a.H, out, lane);
+    if constexpr (kKeys) write_part<D>(acc2, a.part_k + a.n_k * rows + at, row0, held_len, a.H, out, lane);
+  } else {
+    write_rows<D>(acc1, a.scale, (kKeys ? a.dk : a.dq) + held0, row0, held_len, a.H, out, lane);
+    if constexpr (kKeys) write_rows<D>(acc2, 1.0f, a.dv + held0, row0, held_len, a.H, out, lane);
   }
-  const int64_t to = held0 + (int64_t)row * a.H * D + 4 * hb;
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      bf16x4 x;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) x[r] = (__bf16)(acc1[db][4 * g + r] * scale);
-      *(bf16x4*)((kKeys ? a.dk : a.dq) + to + 32 * db + 8 * g) = x;
-      if (kKeys) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = (__bf16)acc2[db][4 * g + r];
-        *(bf16x4*)(a.dv + to + 32 * db + 8 * g) = x;
-      }
-    }
 }
 
 template <int D, int W>
 __global__ __launch_bounds__(64 * W, bwd_groups(D, 32 * W) * W / 4) void attn_bwd_kernel(BwdCall a) {
   extern __shared__ char smem[];
-  const int total = a.plan->tiles * a.H, item = blockIdx.x;
-  if (item >= total) return;
-  const BwdTile* const t = (const BwdTile*)(a.plan + 1) + item / a.H;  // (any of the item's list)
-  if (t->keys) run_item<D, W, true>(a, find_item(t, item, a.H, a.n_k), (lds_char*)smem);
+  const int item = blockIdx.x;
+  const BwdTile t = ((const BwdTile*)(a.plan + 1))[item / a.H];  // (any of the item's list; read with the plan's length)
+  if (item >= a.plan->tiles * a.H) return;
+  if (t.keys) run_item<D, W, true>(a, find_item(t, item, a.H, a.n_k), (lds_char*)smem);
   else run_item<D, W, false>(a, find_item(t, item, a.H, a.n_q), (lds_char*)smem);
 }
 
