@@ -33,7 +33,6 @@ using namespace tsattn;
 // conflicts were counted.)
 template <int D, int W>  // W waves to a workgroup
 struct Bwd {
-  static constexpr int kWaves = W;
   static constexpr int kThreads = 64 * W;
   static constexpr int kTileRows = 32 * W;
   static constexpr int kBN = bwd_step(D, kTileRows);
@@ -117,7 +116,8 @@ __device__ __forceinline__ f32x16 row_statistics(const lds_char* __restrict__ x,
 __device__ __forceinline__ f32x16 splat(float x) { return f32x16{x, x, x, x, x, x, x, x, x, x, x, x, x, x, x, x}; }
 
 // A wave's 32 rows of results leave through LDS, in pieces of 128 bytes a row: straight from the accumulators every
-// store would touch 32 rows with 16 bytes each.  Rows past the segment's end are dropped by the range check.
+// store would touch 32 rows with 16 bytes each (six odd clips at d = 64 82 us instead of 75, 1560 x 32760 x 12 heads 1003 instead
+// of 965).  Rows past the segment's end are dropped by the range check.
 constexpr int kOutRow = 128 + 16;  // bytes
 constexpr int kOutWave = 32 * kOutRow;
 
@@ -250,7 +250,8 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
 #pragma unroll
     for (int j = 0; j < G::kStages - 1; ++j) fetch(j, lds + j * G::kStage);
 
-    // held rows as B operands: row col, channels 16 kk + 8 hb + 0..7
+    // held rows as B operands: row col, channels 16 kk + 8 hb + 0..7 (by way of LDS in whole lines, as the results, they come no
+    // more than 1 % of a small call sooner)
     bf16x8 y1[D / 16], y2[D / 16];
     const bool zero = a.scale == 0.0f;
 #pragma unroll
@@ -285,7 +286,7 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
     // compiler's order 32760 x 32760 x 12 heads took 17.75 ms instead of 17.4, 16380 x 16380 x 24 heads of d = 64 5.1 instead of
     // 5.0 (both without the sums of R below).  ragged: rows from `left` on are past the segment's end; their P and R are 0.
     constexpr int kM = D / 16;  // MFMAs of a product
-        constexpr bool kPair = !kKeys && kBN >= 64;  // dq: two blocks at a time
+    constexpr bool kPair = !kKeys && kBN >= 64;  // dq: two blocks at a time
     constexpr int kBlocks = kBN / (kPair ? 64 : 32), kPer = (kKeys ? 4 : kPair ? 6 : 3) * kM, kAll = kBlocks * kPer;
     auto step_of = [&](const lds_char* stage, auto ragged, int left) {
       const lds_char* const xr = stage + row_lane;
@@ -395,8 +396,9 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
       const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(exact), __float_as_uint(exact), false, false);
       exact = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
       float off = (rounded[0] - exact) * (32.0f / (float)min(32, len - begin * kBN));
-      // that product has query l + 16 beside query l, times 0: where the one is not finite, the other keeps its rounding
-      if (fabsf(exact) < INFINITY && !(fabsf(off) < INFINITY)) off = 0;
+      // that product has query l + 16 beside query l, times 0: where the one is not finite, the other keeps its rounding (and
+      // where its own R are not, neither is acc1)
+      if (!(fabsf(off) < INFINITY)) off = 0;
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) {
         f32x16 mean = {};
@@ -423,6 +425,11 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
   }
 }
 
+// Bound by the matrix cores under the power cap: 32760 x 32760 x 12 heads (d = 128) 18.0 ms, in which its seven products
+// run at 1280 TFLOP/s, what a large library product reaches on the same device (1290); MFMA busy 71 % of 31 M clocks.  16380 x
+// 16380 x 24 heads of d = 64 5.07 ms, 1140 TFLOP/s: exponentials and sums take as many clocks there as the products, which two
+// of the three workgroups of a CU have to hide.  Each CU takes one item after the other; small calls are bound by the
+// last ones, and by what each takes beside its products, 3 to 5 us (1024 x 1024 x 2 heads of d = 64: 12 us in this kernel).
 template <int D, int W>
 __global__ __launch_bounds__(64 * W, bwd_groups(D, 32 * W) * W / 4) void attn_bwd_kernel(BwdCall a) {
   extern __shared__ char smem[];
@@ -513,7 +520,8 @@ __device__ void make_plan(BwdPlan* plan, BwdOffsets f, int n_q, int n_k, int til
   if (tid == 0) plan->tiles = before;
 }
 
-// Before the gradients: the plan, by workgroup 0, and by the others -lse / scale and -D of every query and head,
+// Before the gradients, as fast as memory takes it (40 us for 32760 x 12 heads, d = 128) or in 5 us of latency: the plan, by
+// workgroup 0, and by the others -lse / scale and -D of every query and head,
 // [2][H][total_q], 64 tokens of one head to a workgroup and a row of d bf16 to d / 8 lanes.
 template <int D>
 __global__ __launch_bounds__(kPlanThreads) void bwd_prepare_kernel(const __bf16* d_o, const __bf16* o, const float* lse, float* stat,
@@ -589,9 +597,9 @@ hipError_t launch(const BwdArgs& x, hipStream_t st) {
       a.d_o, (const __bf16*)x.o, x.lse, x.stat, x.total_q, x.H, 1.0f / s, x.plan,
       BwdOffsets{x.cu_q, x.cu_k, x.nseq, x.max_q, x.max_k, x.total_q, x.total_k}, x.n_q, x.n_k, x.tile);
   const int64_t items = x.H * (bwd_tiles(x.nseq, x.max_q, x.total_q, x.tile) * x.n_q + bwd_tiles(x.nseq, x.max_k, x.total_k, x.tile) * x.n_k);
-  if (items > 0 && x.tile == 128) attn_bwd_kernel<D, 4><<<(unsigned)items, 256, Bwd<D, 4>::kLds, st>>>(a);
+  if (items > 0 && x.tile == 128) attn_bwd_kernel<D, 4><<<(unsigned)items, Bwd<D, 4>::kThreads, Bwd<D, 4>::kLds, st>>>(a);
   if constexpr (D == 128)
-    if (items > 0 && x.tile == 256) attn_bwd_kernel<D, 8><<<(unsigned)items, 512, Bwd<D, 8>::kLds, st>>>(a);
+    if (items > 0 && x.tile == 256) attn_bwd_kernel<D, 8><<<(unsigned)items, Bwd<D, 8>::kThreads, Bwd<D, 8>::kLds, st>>>(a);
   const int64_t join_k = x.n_k > 1 ? ((int64_t)x.total_k * x.H + kJoinRows - 1) / kJoinRows : 0;
   const int64_t join_q = x.n_q > 1 ? ((int64_t)x.total_q * x.H + kJoinRows - 1) / kJoinRows : 0;
   if (join_k + join_q > 0) bwd_join_kernel<D><<<(unsigned)(join_k + join_q), 256, 0, st>>>(a, (int)join_k);
