@@ -30,7 +30,7 @@ using namespace tsattn;
 // LDS layout of a streamed tile: rows in groups of four, so that both the row reads (b128: 16 rows, the same 16-byte
 // chunk) and the transposed ones (b64: 4 rows x 64 bytes) fall on distinct banks, with offsets that are sums of a
 // lane's own and an immediate.  At d = 128 the four rows are 320 bytes apart, at d = 64 at 0, 128, 320 and 448.  (No bank
-// conflicts were counted.)
+// conflicts were counted in these reads.)
 template <int D, int W>  // W waves to a workgroup
 struct Bwd {
   static constexpr int kThreads = 64 * W;
