@@ -111,6 +111,37 @@ def test_what_is_not_finite_stays_in_its_head():
     assert torch.equal(~dx.isfinite().all(-1), bad)
 
 
+@pytest.mark.parametrize("interleaved", [True, False])
+@pytest.mark.parametrize("d", [64, 128])
+def test_calls_larger_than_the_caches(d, interleaved):
+    """More than 256 MB read and written, which go past the caches: bit for bit what the halves' calls give (but the weights'
+    gradients, whose sums go by the sizes)."""
+    say("large", d, interleaved)
+    Hq, Hk = 20, 12
+    T = (300 << 20) // ((Hq + Hk) * d * 4) + 1
+    g = rng(45)
+    q, k, dq, dk = (normal(g, T, H, d).bfloat16() for H in (Hq, Hk, Hq, Hk))
+    wq, wk = 1 + 0.3 * normal(g, d), 1 + 0.3 * normal(g, d)
+    r, pos = ts.rope(AXES[d], interleaved=interleaved), torch.randint(0, 99, (T, 3), generator=g, device="cuda").int()
+    cut = T // 2
+    parts = [slice(0, cut), slice(cut, T)]
+    whole = ts.ts_qk_rope(q, k, pos, r, wq, wk)
+    back = ts.ts_qk_rope_bwd(dq, dk, q, k, pos, r, wq, wk)
+    mag = [torch.zeros(d, dtype=torch.double, device="cuda") for _ in range(2)]
+    dw = [torch.zeros(d, dtype=torch.double, device="cuda") for _ in range(2)]
+    for at in parts:
+        got = ts.ts_qk_rope(q[at], k[at], pos[at], r, wq, wk)
+        assert all(same_bits(a[at], b) for a, b in zip(whole, got))
+        got = ts.ts_qk_rope_bwd(dq[at], dk[at], q[at], k[at], pos[at], r, wq, wk)
+        assert all(same_bits(a[at], b) for a, b in zip(back[:2], got))
+        for i, (dy, x, w) in enumerate(((dq, q, wq), (dk, k, wk))):
+            _, part, _, m = R.rope_bwd(dy[at].double(), x[at].double(), w.double(), R.angles(pos[at], r.freq, AXES[d]), interleaved, 1e-6)
+            dw[i] += part
+            mag[i] += m
+    for i in range(2):
+        near("dw", back[2 + i], dw[i], R.FINE * mag[i])
+
+
 def test_no_tokens():
     x = torch.zeros(0, 4, 64, dtype=torch.bfloat16, device="cuda")
     w = torch.ones(64, device="cuda")
@@ -185,6 +216,31 @@ def test_memory_past_32_bits(d):
     ref, tol = R.packed_attn_bwd(*(x[at][:, :2].double() for x in (d_o, q, k, v, o, lse)), [0, L], [0, L], ts.default_scale(d))
     for name, x, y, t in zip(("dq", "dk", "dv"), one, ref, tol):
         near(name, x[:, :2], y, t)
+
+
+@pytest.mark.parametrize("splits", [0, 1, 2])
+@pytest.mark.parametrize("d", [64, 128])
+def test_more_segments_than_the_plan_sorts(d, splits):
+    say("many segments", d, splits)
+    g = np.random.default_rng(46)
+    lq, lk = ([int(x) for x in g.integers(0, 40, 700)] for _ in range(2))
+    lq[300], lk[301], lk[699] = 150, 290, 129
+    args = attn_inputs(lq, lk, 2, d, None, seed=46)
+    got = ts.ts_attn_bwd(*args, num_splits=splits)
+    check_attn(lq, lk, 2, d, ts.default_scale(d), got, args)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_longest_lengths_that_are_only_bounds(d):
+    """Maxima far above the lengths, as a program that does not read its offsets states them: more workgroups are started than
+    have work, and of forced ranges the bits are the same."""
+    say("bounds", d)
+    lq, lk = [130, 0, 700, 1], [200, 40, 333, 1]
+    args = attn_inputs(lq, lk, 3, d, None, seed=47)
+    want = ts.ts_attn_bwd(*args, num_splits=2)
+    got = ts.ts_attn_bwd(*args[:8], 5000, 70000, num_splits=2)
+    assert all(same_bits(a, b) for a, b in zip(got, want))
+    check_attn(lq, lk, 3, d, ts.default_scale(d), ts.ts_attn_bwd(*args[:8], 5000, 70000), args)
 
 
 BAD = [  # cu_q, cu_k, for 150 queries and 400 keys, at most 100 and 400 of a segment
