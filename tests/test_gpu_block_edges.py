@@ -520,3 +520,31 @@ def test_a_serving_step():
             ref, _ = R.attn(a[s:s + 1, h].double(), got[:, h // G], val[:, h // G], ts.default_scale(d))
             off = (o[s:s + 1, h].double() - ref).abs().max().item()
             assert off <= 2e-2, off
+
+
+# ---- workspaces of the C calls
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_smaller_workspace_divides_the_work_less(d):
+    """From the least that the call takes to more than it makes use of: the gradients hold, and what lies behind the stated bytes stays as it
+    is, as the gradients' neighbours do."""
+    say("workspace", d)
+    lib = ts.load_block()
+    lq, lk, H = [300, 70], [1500, 900], 2
+    args = attn_inputs(lq, lk, H, d, None, seed=50)
+    sizes = (2, 300, 1500, 370, 2400, H, d)
+    most, least = (lib.ts_attn_bwd_workspace(*sizes, n) for n in (0, 1))
+    assert 0 < least < most
+    room = 4096
+    for given in (least, (least + most) // 2 // 256 * 256, most, most + 65536):
+        work = torch.full((given + room,), 0xA5, dtype=torch.uint8, device="cuda")
+        outs = [torch.full((x.shape[0] + 2, H, d), 7.0, dtype=torch.bfloat16, device="cuda") for x in (args[1], args[2], args[3])]
+        rc = lib.ts_attn_bwd(*(x.data_ptr() for x in args[:6]), *(x[1:].data_ptr() for x in outs), *(x.data_ptr() for x in args[6:8]), *sizes,
+                             ts.default_scale(d), 0, work.data_ptr(), given, torch.cuda.current_stream().cuda_stream)
+        assert rc == 0
+        check_attn(lq, lk, H, d, ts.default_scale(d), [x[1:-1] for x in outs], args)
+        assert bool((work[given:] == 0xA5).all())
+        assert all(bool((x[[0, -1]] == 7.0).all()) for x in outs)
+    assert lib.ts_attn_bwd(*(x.data_ptr() for x in args[:6]), *(x[1:].data_ptr() for x in outs), *(x.data_ptr() for x in args[6:8]), *sizes,
+                           ts.default_scale(d), 0, work.data_ptr(), least - 1, torch.cuda.current_stream().cuda_stream) == 13  # TS_ERR_SCRATCH
