@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "attn_tile.h"
 #include "block_launch.h"
@@ -86,6 +87,7 @@ __device__ __forceinline__ Item find_item(const BwdTile& t, int at, int heads, i
 }
 
 typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+typedef __attribute__((address_space(3))) f32x2 lds_f32x2;
 
 // The LDS reads of a step take their address as a restrict pointer: the compiler then knows that they do not wait for the
 // DMA of the steps ahead.
@@ -112,6 +114,33 @@ __device__ __forceinline__ f32x16 row_statistics(const lds_char* __restrict__ x,
   }
   return to;
 }
+
+// Of bfloat16 values, as 16-bit integers with a sign, the least and the most, of two channels at once.  Of positive ones these are the
+// smallest and the largest; negative ones come before them, those nearest to 0 first.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) s16x2 lds_s16x2;
+struct Extremes {
+  s16x2 least = {32767, 32767}, most = {-32768, -32768};
+  __device__ __forceinline__ void add(s16x2 x) { add(x, x); }
+  __device__ __forceinline__ void add(s16x2 x, s16x2 y) {
+    least = __builtin_elementwise_min(least, x);
+    most = __builtin_elementwise_max(most, y);
+  }
+};
+
+__device__ __forceinline__ s16x2 two_channels(const lds_char* __restrict__ x) { return *(const lds_s16x2*)x; }
+
+// m of a channel from its extremes: 0 where there are both signs; else `least` is the nearest to 0.
+__device__ __forceinline__ float common_part(short least, short most) {
+  if ((least ^ most) < 0) return 0.0f;
+  const float s = __uint_as_float((unsigned)(unsigned short)least << 16), l = __uint_as_float((unsigned)(unsigned short)most << 16);
+  const float middle = 0.5f * s + 0.5f * l;
+  return fabsf(middle) < fabsf(2.0f * s) ? middle : 2.0f * s;
+}
+
+// f(0), f(1) .. f(N - 1), each a constant of its type, for a loop that is too long to be unrolled by the compiler.
+template <int... I, typename F>
+__device__ __forceinline__ void for_each(std::integer_sequence<int, I...>, F&& f) { (f(std::integral_constant<int, I>{}), ...); }
 
 __device__ __forceinline__ f32x16 splat(float x) { return f32x16{x, x, x, x, x, x, x, x, x, x, x, x, x, x, x, x}; }
 
@@ -274,12 +303,27 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
 
     // dq: the sums over the keys of R as it is and as it is rounded.  Rounding makes dq off by the sum of (rounded R - R) k; keys that
     // have much in common, as those of a trained model's outlier channels do, add that part up while the gradient, whose
-    // R sum to next to nothing, loses it.  So the difference of the two sums times a mean of keys is taken off again at the end.
-    // Of keys whose mean is as large as they spread, dq is then off by 0.0024 of its norm instead of 0.0029 (0.0017 is its own
-    // rounding).  It costs 2 % at d = 128 and 4 % at d = 64.
+    // R sum to next to nothing, loses it.  So the difference of the two sums times a vector m is taken off again at the end, which
+    // leaves the sum of (rounded R - R) (k - m).  No m may bring in keys that a query gives no weight: a mean of few or of all of them does,
+    // where some stand far out (32 keys 8 times the spread away: dq off by 0.014 of its norm instead of 0.0024).  So a channel
+    // has an m only where all keys of the range have one sign: the middle of its smallest and its largest, but twice the
+    // smallest at most, which makes |k - m| <= |k| for every key.  Of keys whose mean is 8 times their spread dq is off by 0.0024 of
+    // its norm instead of 0.013 (0.0017 is its own rounding), of 4 times by 0.005 instead of 0.007; where signs are mixed, as with
+    // a mean like the spread, it is off by what it would be, 0.0029.  The sums cost 2 % at d = 128 and 4 % at d = 64, the smallest
+    // and largest 2 % (32760 x 32760 x 12 heads 18.2 ms instead of 17.9).
     float exact = 0;
     f32x4 rounded = {};  // (every element: the lane's query's, by the matrix core)
     const bf16x8 sel = row_sum_selector(lane);
+    Extremes least_most;
+    // a thread looks at two channels of the same eight of a step's keys
+    constexpr int kTwos = D / 2, kApart = G::kThreads / kTwos;
+    static_assert(8 * kApart == kBN && kApart % 4 == 0, "a workgroup's threads take a step's keys in eight");
+    const int key = threadIdx.x / kTwos, key_lane = G::row_offset(key) + 4 * (threadIdx.x % kTwos);
+    auto of_key = [&](const lds_char* stage, int u) { return two_channels(stage + key_lane + u * (kApart / 4 * G::kGroup)); };
+    auto add_key = [&](s16x2 x, int u, auto ragged, int left) {
+      const bool is = !decltype(ragged)::value || key + u * kApart < left;
+      least_most.add(is ? x : least_most.least, is ? x : least_most.most);
+    };
 
     // One step.  The order of its products and reads is pinned: each operand is read a product before it is used (more ahead
     // measured the same), and the vector work on a product's result goes between products that do not wait for it.  Left to the
@@ -288,6 +332,7 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
     constexpr int kM = D / 16;  // MFMAs of a product
     constexpr bool kPair = !kKeys && kBN >= 64;  // dq: two blocks at a time
     constexpr int kBlocks = kBN / (kPair ? 64 : 32), kPer = (kKeys ? 4 : kPair ? 6 : 3) * kM, kAll = kBlocks * kPer;
+    static_assert(kKeys || kBlocks == 1, "dq: a step's keys are one block, or two at a time");
     auto step_of = [&](const lds_char* stage, auto ragged, int left) {
       const lds_char* const xr = stage + row_lane;
       const lds_char* const xt = stage + tr_lane;
@@ -325,10 +370,10 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
         s[0] = row_statistics(st, hb);
         t[0] = row_statistics(st + G::kStatRow, hb);
       }
+      s16x2 of_keys[2];
       bf16x8 next = operand(0);
-#pragma unroll
-      for (int i = 0; i < kAll; ++i) {
-        const int b = i / kPer, phase = i % kPer / kM, m = i % kM;
+      for_each(std::make_integer_sequence<int, kAll>{}, [&](auto at) __attribute__((always_inline)) {
+        constexpr int i = at, b = i / kPer, phase = i % kPer / kM, m = i % kM;
         const bf16x8 x = next;
         if (i + 1 < kAll) next = operand(i + 1);
         if constexpr (kKeys) {
@@ -365,9 +410,16 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
 #pragma unroll
             for (int r = 0; r < 16; ++r) residual(0, r, 32 * b);
           }
+          // the keys' extremes, in the last phase, which has no other vector work; read a product before their use too
+          if (i + kM >= kAll) add_key(of_keys[0], m, ragged, left);
+          if (kM == 4 && i + kM >= kAll) add_key(of_keys[1], m + 4, ragged, left);
+          if (i + kM + 1 >= kAll && i + 1 < kAll) {
+            of_keys[0] = of_key(stage, (i + 1) % kM);
+            if (kM == 4) of_keys[1] = of_key(stage, (i + 1) % kM + 4);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
-      }
+      });
     };
 
     auto open_step = [&](int j) {  // step j's stage, complete; the next fetch, into the stage that step j - 1 was read from
@@ -384,28 +436,47 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
       for (int j = 0; j < whole; ++j) step_of(open_step(j), std::false_type{}, kBN);
       if (whole < steps) step_of(open_step(whole), std::true_type{}, len - (begin + whole) * kBN);
     } else {
-      for (int j = 0; j < steps; ++j) open_step(j);
+      for (int j = 0; j < steps; ++j) {
+        const lds_char* const stage = open_step(j);
+        if (!kKeys) {
+#pragma unroll
+          for (int u = 0; u < 8; ++u) add_key(of_key(stage, u), u, std::true_type{}, len - (begin + j) * kBN);
+        }
+      }
     }
     wait_lds();
     wait_vmem<0>();
     block_sync();
-    if (!kKeys && active) {
-      // the mean of the range's first 32 keys, which have come again after its last step
-      const lds_char* const first = lds + slot * G::kStage + tr_lane;
-      const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3d003d00u, 0x3d003d00u, 0x3d003d00u, 0x3d003d00u});  // 1 / 32
-      const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(exact), __float_as_uint(exact), false, false);
-      exact = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
-      float off = (rounded[0] - exact) * (32.0f / (float)min(32, len - begin * kBN));
-      // that product has query l + 16 beside query l, times 0: where the one is not finite, the other keeps its rounding (and
-      // where its own R are not, neither is acc1)
-      if (!(fabsf(off) < INFINITY)) off = 0;
+    if constexpr (!kKeys) {
+      // m, in the stage that no results go through: every thread's extremes, then those of all, and m of two channels to a thread
+      lds_char* const shared = lds + slot * G::kStage;
+      static_assert(G::kThreads * 8 + D * 4 <= G::kStage, "extremes and m fit a stage");
+      *(lds_s16x2*)(shared + 4 * threadIdx.x) = least_most.least;
+      *(lds_s16x2*)(shared + 4 * (G::kThreads + threadIdx.x)) = least_most.most;
+      lds_char* const m_at = shared + 8 * G::kThreads;
+      __syncthreads();
+      if (threadIdx.x < kTwos) {
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) {
-        f32x16 mean = {};
-        mean = mfma32(columns_operand<G::kGroup>(first + 64 * db), ones, mean);
-        mean = mfma32(columns_operand<G::kGroup>(first + 4 * G::kGroup + 64 * db), ones, mean);
+        for (int i = 1; i < kApart; ++i) {
+          const lds_char* const x = shared + 4 * (threadIdx.x + i * kTwos);
+          least_most.add(two_channels(x), two_channels(x + 4 * G::kThreads));
+        }
+        *(lds_f32x2*)(m_at + 8 * threadIdx.x) = f32x2{common_part(least_most.least[0], least_most.most[0]), common_part(least_most.least[1], least_most.most[1])};
+      }
+      __syncthreads();
+      if (active) {
+        const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(exact), __float_as_uint(exact), false, false);
+        exact = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
+        float off = rounded[0] - exact;
+        // that product has query l + 16 beside query l, times 0: where the one is not finite, the other keeps its rounding (and
+        // where its own R are not, neither is acc1)
+        if (!(fabsf(off) < INFINITY)) off = 0;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc1[db][r] = __builtin_fmaf(-off, mean[r], acc1[db][r]);
+        for (int db = 0; db < D / 32; ++db) {
+          const f32x16 m = row_statistics(m_at + 128 * db, hb);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc1[db][r] = __builtin_fmaf(-off, m[r], acc1[db][r]);
+        }
       }
     }
   }
