@@ -6,7 +6,7 @@ import torch
 
 import block_bounds as B
 import block_ref as R
-from test_gpu_block import normal, rng, say
+from test_gpu_block import ATTN, attn_inputs, normal, rng, say
 
 pytestmark = pytest.mark.gpu
 
@@ -21,18 +21,42 @@ def gpu():
     ts.load_block()
 
 
-def within(lq, lk, d, q, k, v, d_o, splits, scale=None):
-    """ts_attn_bwd of these, its result and log-sum-exp from the definition; every gradient within its bounds.  Returns dq and its
-    definition."""
-    scale = ts.default_scale(d) if scale is None else scale
-    cu_q, cu_k = (torch.tensor(R.offsets(n), dtype=torch.int32, device="cuda") for n in (lq, lk))
-    o, lse = R.packed_attn(*(x.double() for x in (q, k, v)), R.offsets(lq), R.offsets(lk), scale)
-    o, lse = o.bfloat16(), lse.float()
-    got = ts.ts_attn_bwd(d_o, q, k, v, o, lse, cu_q, cu_k, max(lq), max(lk), scale=scale, num_splits=splits)
-    want = B.packed(*(x.double() for x in (d_o, q, k, v, o, lse)), R.offsets(lq), R.offsets(lk), scale)
+def bounded(lq, lk, args, scale, splits):
+    """ts_attn_bwd of these arguments: every gradient within its bounds.  Returns dq and its definition."""
+    got = ts.ts_attn_bwd(*args, scale=scale, num_splits=splits)
+    want = B.packed(*(x.double() for x in args[:6]), R.offsets(lq), R.offsets(lk), scale, splits)
     for name, x, (ref, tol, most) in zip(("dq", "dk", "dv"), got, want):
         B.check(name, x, ref, tol, most, say)
     return got[0], want[0][0]
+
+
+def within(lq, lk, d, q, k, v, d_o, splits):
+    """The same with the result and the log-sum-exp of the definition."""
+    scale = ts.default_scale(d)
+    cu_q, cu_k = (torch.tensor(R.offsets(n), dtype=torch.int32, device="cuda") for n in (lq, lk))
+    o, lse = R.packed_attn(*(x.double() for x in (q, k, v)), R.offsets(lq), R.offsets(lk), scale)
+    return bounded(lq, lk, (d_o, q, k, v, o.bfloat16(), lse.float(), cu_q, cu_k, max(lq), max(lk)), scale, splits)
+
+
+@pytest.mark.parametrize("splits", [1, 0, 3])
+@pytest.mark.parametrize("case", ATTN, ids=lambda c: "%s-%s-%d-%d" % (c[0][:6], c[1][:6], c[2], c[3]))
+def test_gradients_within_their_bounds(case, splits):
+    lq, lk, H, d = case
+    say("bounds", case, splits)
+    scale = ts.default_scale(d)
+    bounded(lq, lk, attn_inputs(lq, lk, H, d, scale, seed=63), scale, splits)
+
+
+@pytest.mark.parametrize("splits", [1, 0, 5])
+@pytest.mark.parametrize("mean", [1, 4, 8])
+@pytest.mark.parametrize("lq,lk,H,d", [([300, 500], [1000, 700], 3, 64), ([300, 500], [1000, 700], 3, 128), ([2900, 300], [2048, 2500], 12, 128)])
+def test_keys_with_a_mean(lq, lk, H, d, mean, splits):
+    """In small tiles and in large ones."""
+    say("mean", lq, lk, H, d, mean, splits)
+    g = rng(64)
+    q, v, d_o = (normal(g, sum(n), H, d) for n in (lq, lk, lq))
+    k = normal(g, sum(lk), H, d) + mean * normal(g, H, d).sign()
+    within(lq, lk, d, (0.3 * q).bfloat16(), k.bfloat16(), v.bfloat16(), d_o.bfloat16(), splits)
 
 
 @pytest.mark.parametrize("splits", [1, 0, 3])
