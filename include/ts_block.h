@@ -114,7 +114,9 @@ int64_t ts_qk_rope_bwd_workspace(int32_t T, int32_t q_heads, int32_t k_heads, in
  * The bits of a segment's gradients depend on its own rows and on the division; with n >= 1 on nothing else.
  * No output may overlap another one, an input or the workspace (TS_ERR_ALIAS).  Sizes, TS_ERR_SHAPE:
  * (max_seqlen + 256) * H * d * 2 below 2^31 for each side, and for the work items nseq * H * (max_seqlen_q / 128 +
- * max_seqlen_k / 128 + 2) below 2^26 and H * (total / 128 + nseq) below 2^19 for each side.
+ * max_seqlen_k / 128 + 2) below 2^26 and H * (total / 128 + nseq) below 2^19 for each side; of n >= 2 ranges
+ * n * H * (tiles of queries + tiles of keys) below 2^23, tiles being of 128 or 256 rows, with a last one for each segment (never
+ * reached where n * H * (total_q / 128 + total_k / 128 + 2 nseq) is below that).
  */
 #define TS_ATTN_BWD_MAX_SPLITS 16
 int ts_attn_bwd(const void* d_o, const void* q, const void* k, const void* v, const void* o, const float* lse, void* dq,

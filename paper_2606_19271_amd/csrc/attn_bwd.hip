@@ -663,17 +663,22 @@ hipError_t launch(const BwdArgs& x, hipStream_t st) {
   const BwdCall a{(const __bf16*)x.d_o, (const __bf16*)x.q, (const __bf16*)x.k, (const __bf16*)x.v, x.stat,
                   (__bf16*)x.dq, (__bf16*)x.dk, (__bf16*)x.dv, x.part_q, x.part_k, x.plan,
                   x.total_q, x.total_k, x.H, x.n_q, x.n_k, x.scale, s * kLog2e};
+  // (each kernel reads what the one before wrote: none goes out after one that was refused)
   const int64_t stats = ((int64_t)x.total_q + 63) / 64 * x.H;
   bwd_prepare_kernel<D><<<(unsigned)(1 + stats), kPlanThreads, 0, st>>>(
       a.d_o, (const __bf16*)x.o, x.lse, x.stat, x.total_q, x.H, 1.0f / s, x.plan,
       BwdOffsets{x.cu_q, x.cu_k, x.nseq, x.max_q, x.max_k, x.total_q, x.total_k}, x.n_q, x.n_k, x.tile);
-  const int64_t items = x.H * (bwd_tiles(x.nseq, x.max_q, x.total_q, x.tile) * x.n_q + bwd_tiles(x.nseq, x.max_k, x.total_k, x.tile) * x.n_k);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t items = bwd_items(x.nseq, x.max_q, x.max_k, x.total_q, x.total_k, x.H, x.n_q, x.n_k, x.tile);
   if (items > 0 && x.tile == 128) attn_bwd_kernel<D, 4><<<(unsigned)items, Bwd<D, 4>::kThreads, Bwd<D, 4>::kLds, st>>>(a);
   if constexpr (D == 128)
     if (items > 0 && x.tile == 256) attn_bwd_kernel<D, 8><<<(unsigned)items, Bwd<D, 8>::kThreads, Bwd<D, 8>::kLds, st>>>(a);
+  if (items > 0 && (e = hipGetLastError()) != hipSuccess) return e;
   const int64_t join_k = x.n_k > 1 ? ((int64_t)x.total_k * x.H + kJoinRows - 1) / kJoinRows : 0;
   const int64_t join_q = x.n_q > 1 ? ((int64_t)x.total_q * x.H + kJoinRows - 1) / kJoinRows : 0;
-  if (join_k + join_q > 0) bwd_join_kernel<D><<<(unsigned)(join_k + join_q), 256, 0, st>>>(a, (int)join_k);
+  if (join_k + join_q == 0) return hipSuccess;
+  bwd_join_kernel<D><<<(unsigned)(join_k + join_q), 256, 0, st>>>(a, (int)join_k);
   return hipGetLastError();
 }
 

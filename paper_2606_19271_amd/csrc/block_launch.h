@@ -103,6 +103,10 @@ int64_t bwd_least_workspace(int32_t nseq, int32_t max_q, int32_t max_k, int32_t 
                             int32_t num_splits);
 // An upper bound of the tiles of one side over all segments: sum of ceil(len / tile).
 int64_t bwd_tiles(int32_t nseq, int32_t most, int32_t total, int32_t tile);
+// Workgroups of the gradients' main kernel, 2 * tile threads each; and of ranges that the caller forces, as the call divides it.
+int64_t bwd_items(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t n_q, int32_t n_k,
+                  int32_t tile);
+int64_t bwd_forced_items(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d, int32_t n);
 
 hipError_t configure_kernels();
 hipError_t launch_rope(const RopeArgs& a, hipStream_t st);

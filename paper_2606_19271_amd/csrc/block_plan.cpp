@@ -113,6 +113,15 @@ BwdParts bwd_parts(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, 
   return layout(c, best_q, best_k);
 }
 
+int64_t bwd_items(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t n_q, int32_t n_k,
+                  int32_t tile) {
+  return H * (bwd_tiles(nseq, max_q, total_q, tile) * n_q + bwd_tiles(nseq, max_k, total_k, tile) * n_k);
+}
+
+int64_t bwd_forced_items(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d, int32_t n) {
+  return bwd_items(nseq, max_q, max_k, total_q, total_k, H, n, n, call(nseq, max_q, max_k, total_q, total_k, H, d).tile);
+}
+
 int64_t bwd_least_workspace(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d,
                             int32_t num_splits) {
   return layout(call(nseq, max_q, max_k, total_q, total_k, H, d), std::max(1, num_splits), std::max(1, num_splits)).bytes;

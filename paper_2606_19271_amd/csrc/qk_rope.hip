@@ -380,6 +380,8 @@ hipError_t rope_bwd(const RopeBwdArgs& a, hipStream_t st) {
     auto kernel = pairs ? past ? rope_bwd_kernel<D, true, true> : rope_bwd_kernel<D, true, false>
                         : past ? rope_bwd_kernel<D, false, true> : rope_bwd_kernel<D, false, false>;
     kernel<<<blocks, kRopeThreads, 0, st>>>(a, gq, groups, steps, per);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;  // (the sums' kernel reads what this one writes)
   }
   if (a.dq_weight || a.dk_weight) rope_bwd_join_kernel<D><<<2 * D / 16, 1024, 0, st>>>(a.part, blocks, a.dq_weight, a.dk_weight);
   return hipGetLastError();

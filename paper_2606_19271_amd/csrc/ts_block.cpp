@@ -159,6 +159,7 @@ int validate(const int32_t* cu_q, const int32_t* cu_k, int32_t nseq, int32_t max
 constexpr float kLeastScale = 0x1p-100f, kMostScale = 0x1p100f;
 
 constexpr int kLeastTile = 128;  // held rows of a workgroup, at least
+constexpr int64_t kItemLimit = (int64_t)1 << 23;  // workgroups of a launch (x 512 threads < 2^32)
 
 // Sizes of an attention gradient call.
 int check_sizes(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d, int32_t num_splits) {
@@ -171,6 +172,8 @@ int check_sizes(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int
   const int64_t tiles = (int64_t)max_q / kLeastTile + max_k / kLeastTile + 2;
   if ((int64_t)nseq * H >= (int64_t)1 << 26 || (int64_t)nseq * H * tiles >= (int64_t)1 << 26) return TS_ERR_SHAPE;
   if (H * ((int64_t)std::max(total_q, total_k) / kLeastTile + nseq) >= (int64_t)1 << 19) return TS_ERR_SHAPE;
+  // (undivided calls have less than 2^20 workgroups by that, and the library divides only those of a few rounds of the device)
+  if (num_splits > 1 && tsblock::bwd_forced_items(nseq, max_q, max_k, total_q, total_k, H, d, num_splits) >= kItemLimit) return TS_ERR_SHAPE;
   return TS_OK;
 }
 
