@@ -70,7 +70,8 @@ int ts_qk_rope(const ts_rows* q, const ts_rows* k, const ts_rows* q_out, const t
  * Its gradients.  dq_out and dk_out are those of ts_qk_rope's results, q, k, weights and rope what it was given.
  *  dq, dk        gradients of q and k; each is dq_out's or dk_out's own memory, or q's or k's, or overlaps no
  *                input and no other output
- *  dq_weight, dk_weight  float32 [d]: the sums over tokens and heads; NULL where the weight is
+ *  dq_weight, dk_weight  float32 [d]: the sums over tokens and heads, 128 terms at most in 32 bits and those sums in 64; NULL
+ *                where the weight is
  *  q, k          may be NULL where their weight is (the rotation's gradient needs no input)
  *  workspace     (256-byte aligned) ts_qk_rope_bwd_workspace bytes; less gives TS_ERR_SCRATCH.  0 bytes are
  *                needed, and it may be NULL, where there are no weights.

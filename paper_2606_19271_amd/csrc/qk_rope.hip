@@ -233,7 +233,11 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a, int grou
 // Gradients.  As many workgroups as the device holds at once take equal parts of the steps, whatever their number, so that the sums'
 // order is the call's own.  With g the result's gradient turned back, n = x r the normalised row:
 //   dw = sum g n,   dx = r (g w - n mean(g w n))
-// Each wave sums dw over its steps, the workgroup its waves' sums, and rope_bwd_join_kernel those of the workgroups.
+// Each lane sums dw over kChain steps at most, in 32 bits; what the wave's lanes have then goes into the wave's sums in LDS, in 64, as a
+// chain of all steps would lose as many bits as it is long (8192 equal terms 11, 128 of them 5).  The workgroup adds its
+// waves' sums, and rope_bwd_join_kernel those of the workgroups.
+constexpr int kChain = 128;
+
 template <int D, bool kPairs, bool kFar>
 __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(RopeBwdArgs a, int groups_q, int groups, int steps, int per) {
   using G = Geo<D>;
@@ -241,6 +245,9 @@ __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(RopeBwdArgs a, i
   const int j = lane % G::kLanes, r = lane / G::kLanes;
   Steps at(wave, per, steps, groups);
   __shared__ float lds[kWaves][2 * kAngleRow];
+  __shared__ double sums[kWaves][2 * D];
+  double* const sum = sums[threadIdx.x >> 6];
+  for (int ch = lane; ch < 2 * D; ch += 64) sum[ch] = 0;
   float wq[16], wk[16], c[8], s[8], sum_q[16] = {}, sum_k[16] = {};
   auto rows = [&](const Rows& q, const Rows& k, const Steps& at, bool& live) {
     const bool is_k = at.g >= groups_q;
@@ -262,6 +269,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(RopeBwdArgs a, i
   const double freq = a.rope.freq ? a.rope.freq[lane % (D / 2)] : 0.0;
   load_weights<D>(a.q_weight, j, wq);
   load_weights<D>(a.k_weight, j, wk);
+  int chain = 0;
   while (at.left > 0) {
     if (fresh && a.rope.freq) angles<D, kPairs>(a.rope, place(a.rope, at.t), lane, freq, lds[threadIdx.x >> 6], c, s);
     const Steps here = at;
@@ -301,28 +309,30 @@ __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(RopeBwdArgs a, i
     store_head<D, kFar>(to, g, live);
     dy_in = dy_next;
     x_in = x_next;
+    if (!a.part || (++chain < kChain && at.left > 0)) continue;
+    chain = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+#pragma unroll
+      for (int o = G::kLanes; o < 64; o <<= 1) {
+        sum_q[i] += __shfl_xor(sum_q[i], o);
+        sum_k[i] += __shfl_xor(sum_k[i], o);
+      }
+      if (r == 0) {
+        const int ch = (i < 8 ? 8 * j + i : D / 2 + 8 * j + i - 8);
+        sum[ch] += sum_q[i];
+        sum[D + ch] += sum_k[i];
+      }
+      sum_q[i] = sum_k[i] = 0;
+    }
   }
   if (!a.part) return;
-  __shared__ float sums[kWaves][2 * D];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-#pragma unroll
-    for (int o = G::kLanes; o < 64; o <<= 1) {
-      sum_q[i] += __shfl_xor(sum_q[i], o);
-      sum_k[i] += __shfl_xor(sum_k[i], o);
-    }
-    if (r == 0) {
-      const int ch = (i < 8 ? 8 * j + i : D / 2 + 8 * j + i - 8);
-      sums[threadIdx.x >> 6][ch] = sum_q[i];
-      sums[threadIdx.x >> 6][D + ch] = sum_k[i];
-    }
-  }
   __syncthreads();
   for (int ch = threadIdx.x; ch < 2 * D; ch += kRopeThreads) {
-    float x = sums[0][ch];
+    double x = sums[0][ch];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) x += sums[w][ch];
-    a.part[(int64_t)blockIdx.x * 2 * D + ch] = x;
+    a.part[(int64_t)blockIdx.x * 2 * D + ch] = (float)x;
   }
 }
 
