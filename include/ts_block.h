@@ -105,8 +105,9 @@ int64_t ts_qk_rope_bwd_workspace(int32_t T, int32_t q_heads, int32_t k_heads, in
  *                  start at 0, do not descend, end at total_q / total_k, and no segment is longer than its
  *                  max_seqlen.  Offsets that break them make the call a device-side no-op (the gradients are left
  *                  unwritten); with TS_ATTN_VALIDATE=1 the call instead synchronizes and returns
- *                  TS_ERR_SEGMENTS (not on a capturing stream).  Segments may be empty on either side: queries without
- *                  keys get dq = 0, keys without queries dk = dv = 0.
+ *                  TS_ERR_SEGMENTS (not on a capturing stream).  Without segments (nseq = 0) nothing is done either, and
+ *                  validation mode names rows that belong to none.  Segments may be empty on either side: queries
+ *                  without keys get dq = 0, keys without queries dk = dv = 0.
  *  scale           0, or a float of magnitude 2^-100 to 2^100 (TS_ERR_SCALE)
  *  num_splits      0: the library divides the work.  n in 1..16: the keys of each query tile and the queries of each key tile
  *                  are taken in n ranges, whose 32-bit sums another kernel adds up in order.

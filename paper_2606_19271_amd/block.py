@@ -255,6 +255,8 @@ def ts_attn_bwd(d_o, q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, max_seqlen_q, 
     nseq = cu_seqlens_q.numel() - 1
     if cu_seqlens_k.numel() != nseq + 1:
         raise ValueError("cu_seqlens_q and cu_seqlens_k must have the same length")
+    if nseq == 0 and (Tq or shape_k[0]):
+        raise ValueError("the offsets have no segment, and q or k have rows")
     if (not isinstance(lse, Tensor) or lse.dtype is not _F32 or lse.shape != (Tq, H) or lse.get_device() != index
             or not lse.is_contiguous()):
         raise ValueError("lse must be a contiguous float32 [Tq, H] tensor on q's device")

@@ -258,7 +258,8 @@ int ts_attn_bwd(const void* d_o, const void* q, const void* k, const void* v, co
   if (rc != TS_OK) return rc;
   if (workspace_bytes < 0) return TS_ERR_SHAPE;
   if (!isfinite(scale) || (scale != 0.0f && (fabsf(scale) < kLeastScale || fabsf(scale) > kMostScale))) return TS_ERR_SCALE;
-  if (nseq == 0 || (total_q == 0 && total_k == 0)) return TS_OK;
+  if (total_q == 0 && total_k == 0) return TS_OK;
+  if (nseq == 0) return validate_mode() && !capturing((hipStream_t)stream) ? TS_ERR_SEGMENTS : TS_OK;
   if ((total_q > 0 && (!q || !d_o || !o || !lse || !dq)) || (total_k > 0 && (!k || !v || !dk || !dv)) || !cu_seqlens_q || !cu_seqlens_k)
     return TS_ERR_NULL;
   for (const void* p : {d_o, q, k, v, o, (const void*)dq, (const void*)dk, (const void*)dv})
