@@ -131,8 +131,10 @@ int ts_attn_fwd_varlen(const void* q, const void* k, const void* v, void* o,
  * and every query attends to every key of its segment:
  *   O[t,h,c] = sum_j softmax_j(scale * <Q[t,h,:], K[j,h,:]>) * V[j,h,c]
  *   lse[t,h] = ln sum_j exp(scale * <Q[t,h,:], K[j,h,:]>)
- * A segment with queries but no keys gets O = 0 and lse = -inf.  With cu_seqlens_q ==
- * cu_seqlens_k (same tensors for q and k rows) it is the packed self-attention above.
+ * A segment with queries but no keys gets O = 0 and lse = -inf, and so does a query whose scores are
+ * all -inf (of a scale that is not 0); other keys of score -inf have a weight of 0.  A query with a
+ * score of +inf or NaN gets NaN, in lse too, and one other query of its tile may get NaN with it.
+ * With cu_seqlens_q == cu_seqlens_k (same tensors for q and k rows) it is the packed self-attention above.
  *  q, o            bf16 [total_q][H][d];  k, v  bf16 [total_k][H][d]  (DEVICE, 16-byte aligned)
  *  lse             DEVICE float32 [total_q][H] (4-byte aligned), or NULL to skip it
  *  cu_seqlens_q/k  DEVICE int32, nseq+1 entries each: start at 0, nondecreasing, end at

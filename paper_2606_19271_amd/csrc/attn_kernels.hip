@@ -149,16 +149,19 @@ __device__ __forceinline__ unsigned exp_pack(const f32x16 (&s)[NT / 2], bf16x8 (
 // m_c is not recomputed per tile.  A full tile first tries the current m_c: if every weight of
 // every lane is below 2 -- at most 2^(kBias + 1) times the largest weight so far -- the fp32
 // accumulators stay far from overflow and the tile is done; exact in real arithmetic, since the
-// final division by l cancels the common factor.  Otherwise (the first tile, where m_c = -inf, a
+// final division by l cancels the common factor.  Otherwise (the first tile, where m_c is the lowest float, a
 // score far above the running maximum, or the masked last tile) the tile's true maximum is
 // taken, m_c moves up to it (plus the bias), and the accumulators of O and l -- which hold the
 // products of the earlier tiles, relative to the old m_c -- are multiplied by
 // alpha = 2^(m_c,old - m_c,new) before the next matrix step adds these weights to them.  Doing
 // that here, in the rare slow path of the vector step, keeps the matrix step free of branches.
 constexpr float kBias = 39.0f;
+// The running maximum before any score: below every finite one, and finite itself, so that keys of score -inf
+// have a weight of 0 also where a row has seen no other yet (-inf less -inf would be NaN).
+constexpr float kNoMaximum = -3.402823466e38f;
 
 // Which tile of an item a vector step works on.  The first one's maximum is taken at once: its
-// weights against m_c = -inf are all infinite, so an attempt with the running maximum never holds
+// weights against that m_c are all infinite, so an attempt with the running maximum never holds
 // (skipping it saves 620 clocks per group at d = 128 and 1200 at d = 64, of an item's two first
 // vector steps).  The last one is masked: its keys past the segment's end score -inf, so their
 // weights are exactly 0 (c > 0).  With scale 0 (c = 0) no score can do that, because one that is not
@@ -198,7 +201,7 @@ __device__ __forceinline__ void softmax_tile(f32x16 (&s)[Geo<D>::kBN / 32],
   // c >= 0, so the max commutes with the scaling
   const float m_new = fmaxf(m_c, __builtin_fmaf(mt, c, kBias));
   if (kKind != kFirstTile) {  // nothing is accumulated before the first tile
-    const float alpha = __builtin_amdgcn_exp2f(m_c - m_new);  // 0 where m_c = -inf
+    const float alpha = __builtin_amdgcn_exp2f(m_c - m_new);  // 0 where m_c is kNoMaximum
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
@@ -310,11 +313,14 @@ __device__ __forceinline__ void dma_q(__amdgpu_buffer_rsrc_t rq, int q0, int row
   }
 }
 // The wave's Q fragments from its stage (fragment kk: query lane & 31, channels 16kk + 8hb + 0..7);
-// flip: sign bits to invert.
+// flip: sign bits to invert.  Rows after `last`, past the segment's end, are that one again: as rows of zeros
+// they would have NaN scores with keys that are not finite, and a NaN weight makes the row sum of the
+// query 16 rows away NaN too (row_sums).  (Taken care of at the DMA's addresses, the main loops moved: 32760
+// x 32760 x 12 heads 1.1 % slower.)
 template <int D>
 __device__ __forceinline__ void read_q(const lds_char* stage, bf16x8 (&qf)[D / 16], unsigned flip,
-                                       int lane) {
-  const int row = lane & 31, hb = lane >> 5;
+                                       int last, int lane) {
+  const int row = min(lane & 31, last), hb = lane >> 5;
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk) {
     const u32x4 raw = *(const lds_u32x4*)(stage + row * D * 2 + (((2 * kk + hb) ^ qswz<D>(row)) << 4));
@@ -418,7 +424,7 @@ __device__ __forceinline__ void run_item_group(const Item& it, const __bf16* __r
   bf16x8 kp[kPreReads];  // K fragments of the next matrix step's first MFMAs
   f32x4 lacc[2] = {};  // row sums of the weights, two chains (every element: the query's sum)
   const bf16x8 sel = row_sum_selector(lane);
-  float m_c = -INFINITY;
+  float m_c = kNoMaximum;
 
   const int ntiles = it.ntiles;
   // valid keys of the item's last tile: fewer than kBN only on the segment's ragged last tile
@@ -458,9 +464,13 @@ __device__ __forceinline__ void run_item_group(const Item& it, const __bf16* __r
   __asm__ volatile("" ::: "memory");
   bf16x8 qf[D / 16] = {};
   if constexpr (kActive) {
-    read_q<D>(q_stage<D>(lds, wave), qf, negate_q ? 0x80008000u : 0u, lane);
+    read_q<D>(q_stage<D>(lds, wave), qf, negate_q ? 0x80008000u : 0u,
+              it.q_len - 1 - (it.q_begin + 32 * wave), lane);
     wait_lds();
   }
+  // where the main loops start matters: with these the dense ones of d = 128 do so 52 and 4 bytes into 64,
+  // and 32760 x 32760 x 40 heads take 0.7 % less than at 56 and 8, where they are without
+  if constexpr (kGroupB && kActive) __asm__ volatile(".rept 15\n\ts_nop 0\n\t.endr");
   block_sync();
   if constexpr (kActive) k_preread<D>(ktile(0), kp, lane);
   if (kGroupB) block_sync();  // group B starts one step behind
@@ -512,8 +522,9 @@ __device__ __forceinline__ void run_item_group(const Item& it, const __bf16* __r
 
 // The epilogue of one wave: O = O / l for its 32 query rows (the first is q0, relative to the
 // segment), and the row's natural log-sum-exp lse = (m_c + log2 l) ln 2 (m_c is in log2 units of the
-// scaled scores).  l_tot = 0 marks an item without keys: O = 0 and lse = -inf.  Rows past the
-// segment end are dropped by the descriptors' range checks.
+// scaled scores).  l_tot = 0 marks an item without keys, or only such of score -inf: O = 0 and
+// lse = -inf.  Where it is NaN both are.  Rows past the segment end are dropped by the descriptors'
+// range checks.
 //
 // A lane holds 4-channel pieces of one query, so stores straight from the registers touch 32 rows
 // with 16 bytes each, and the CU's address path takes about 75 clocks for each of a workgroup's 128
@@ -527,8 +538,8 @@ __device__ __forceinline__ void write_result(const Item& it, const Out& out,
   using G = Geo<D>;
   const int col = lane & 31, hb = lane >> 5;
   const int qrow = q0 + col;
-  const float inv = l_tot > 0.0f ? 1.0f / l_tot : 0.0f;
-  const float lse = l_tot > 0.0f ? (m_c + log2f(l_tot)) * kLn2 : -INFINITY;
+  const float inv = l_tot == 0.0f ? 0.0f : 1.0f / l_tot;
+  const float lse = l_tot == 0.0f ? -INFINITY : (m_c + log2f(l_tot)) * kLn2;
   const uint32_t lse_bytes = ((uint32_t)(it.q_len - 1) * (uint32_t)H + 1) * 4;
   // After the transposition lane i holds bytes 16 (i % 8) .. + 15 of the pass's 128 of the rows
   // i / 8 + 8 u.
@@ -688,7 +699,7 @@ __device__ __forceinline__ void run_thin_item(const Item& it, const __bf16* __re
   f32x4 o[kCB];
 #pragma unroll
   for (int cb = 0; cb < kCB; ++cb) o[cb] = f32x4{};
-  float m_c = -INFINITY, l_part = 0.0f;
+  float m_c = kNoMaximum, l_part = 0.0f;
   const int ntiles = it.ntiles;
   const int last_keys = min(kBN, it.k_len - (it.tile_begin + ntiles - 1) * kBN);
 
@@ -755,7 +766,7 @@ __device__ __forceinline__ void run_thin_item(const Item& it, const __bf16* __re
       // then its maximum, and everything it has accumulated, stay as they are
       if (mt != -INFINITY) {
         const float m_new = fmaxf(m_c, __builtin_fmaf(mt, c, kBias));
-        const float alpha = __builtin_amdgcn_exp2f(m_c - m_new);  // 0 while m_c = -inf
+        const float alpha = __builtin_amdgcn_exp2f(m_c - m_new);  // 0 while m_c is kNoMaximum
         m_c = m_new;
 #pragma unroll
         for (int cb = 0; cb < kCB; ++cb) o[cb] *= alpha;
@@ -812,7 +823,7 @@ __device__ __forceinline__ void run_thin_item(const Item& it, const __bf16* __re
   float acc[kCh] = {}, lsum = 0.0f;
 #pragma unroll
   for (int k2 = 0; k2 < 4; ++k2) {
-    const float w = big == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mk[k2] - big);
+    const float w = __builtin_amdgcn_exp2f(mk[k2] - big);
     lsum += w * lk[k2];
     const lds_float* src = obuf + ((qb + 2 * k2) * 16 + i16) * D + ch0;
 #pragma unroll
@@ -822,8 +833,8 @@ __device__ __forceinline__ void run_thin_item(const Item& it, const __bf16* __re
       for (int y = 0; y < 4; ++y) acc[x + y] += w * ov[y];
     }
   }
-  const float inv = lsum > 0.0f ? 1.0f / lsum : 0.0f;
-  const float lse = lsum > 0.0f ? (big + log2f(lsum)) * kLn2 : -INFINITY;
+  const float inv = lsum == 0.0f ? 0.0f : 1.0f / lsum;
+  const float lse = lsum == 0.0f ? -INFINITY : (big + log2f(lsum)) * kLn2;
   const uint32_t lse_bytes = ((uint32_t)(it.q_len - 1) * (uint32_t)H + 1) * 4;
   if (kMode == kFinal) {
     __amdgpu_buffer_rsrc_t ro = make_rsrc(out.o + qbase, q_bytes);
@@ -988,7 +999,7 @@ __device__ __forceinline__ void run_small_item(const Item& it, const __bf16* __r
   block_sync();
 
   float l_tot[2] = {0.0f, 0.0f};  // of a summing consumer: its block's row sums
-  float m_c[2] = {-INFINITY, -INFINITY};
+  float m_c[2] = {kNoMaximum, kNoMaximum};
   f32x16 oacc[S::kQB];
 #pragma unroll
   for (int i = 0; i < S::kQB; ++i) oacc[i] = f32x16{};
@@ -1001,7 +1012,8 @@ __device__ __forceinline__ void run_small_item(const Item& it, const __bf16* __r
     bf16x8 qf[S::kUnits][D / 16];
 #pragma unroll
     for (int u = 0; u < S::kUnits; ++u)
-      read_q<D>(lds + S::kP + (uq + u) * G::kQWave, qf[u], negate_q ? 0x80008000u : 0u, lane);
+      read_q<D>(lds + S::kP + (uq + u) * G::kQWave, qf[u], negate_q ? 0x80008000u : 0u,
+                max(0, it.q_len - 1 - (it.q_begin + 32 * (uq + u))), lane);
     // K fragments of a tile's score block (fragment kk: channels 16 kk + ..)
     auto read_k = [&](int stage, bf16x8 (&kf)[D / 16]) {
 #pragma unroll
@@ -1246,7 +1258,7 @@ __device__ __forceinline__ void run_small_item(const Item& it, const __bf16* __r
 #pragma unroll
     for (int i = 0; i < S::kQB; ++i) {
       const float l = sums[(qb0 + i) * 32 + col];
-      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
       lds_char* const put = lds + (32 * (qb0 + i) + col) * kRow + 32 * cb * kEl;
 #pragma unroll
       for (int g4 = 0; g4 < 4; ++g4) {
@@ -1260,7 +1272,7 @@ __device__ __forceinline__ void run_small_item(const Item& it, const __bf16* __r
       }
       if (sum_qb == qb0 + i && hb == 0) {
         const int qrow = it.q_begin + 32 * (qb0 + i) + col;
-        const float lse = l > 0.0f ? (m_c[i] + log2f(l)) * kLn2 : -INFINITY;
+        const float lse = l == 0.0f ? -INFINITY : (m_c[i] + log2f(l)) * kLn2;
         const uint32_t lse_bytes = ((uint32_t)(it.q_len - 1) * (uint32_t)H + 1) * 4;
         float* const dst = kMode == kFinal ? out.lse : out.part_lse + (int64_t)out.split * out.tq * H;
         if (kMode != kFinal || dst != nullptr) {
@@ -1524,21 +1536,20 @@ attn_merge_kernel(const float* __restrict__ part_o, const float* __restrict__ pa
   for (int i = 0; i < n_split; ++i) m = fmaxf(m, part_lse[i * rows + row]);
   f32x4 a0 = {0.0f, 0.0f, 0.0f, 0.0f}, a1 = a0;
   float wsum = 0.0f;
-  if (m != -INFINITY) {
-    for (int i = 0; i < n_split; ++i) {
-      const float w = expf(part_lse[i * rows + row] - m);  // 0 for a range without keys
-      const f32x4* src = (const f32x4*)(part_o + (i * rows + row) * D + c8 * 8);
-      a0 += w * src[0];
-      a1 += w * src[1];
-      wsum += w;
-    }
+  for (int i = 0; i < n_split; ++i) {
+    const float part = part_lse[i * rows + row];
+    const float w = part == -INFINITY ? 0.0f : expf(part - m);  // 0 for a range without keys, or only such of score -inf
+    const f32x4* src = (const f32x4*)(part_o + (i * rows + row) * D + c8 * 8);
+    a0 += w * src[0];
+    a1 += w * src[1];
+    wsum += w;
   }
-  const float inv = wsum > 0.0f ? 1.0f / wsum : 0.0f;
+  const float inv = wsum == 0.0f ? 0.0f : 1.0f / wsum;
   f32x4 r0 = a0 * inv, r1 = a1 * inv;
   bf16x4 b0 = __builtin_convertvector(r0, bf16x4), b1 = __builtin_convertvector(r1, bf16x4);
   bf16x8 b = {b0[0], b0[1], b0[2], b0[3], b1[0], b1[1], b1[2], b1[3]};
   *(bf16x8*)(o + row * D + c8 * 8) = b;
-  if (lse != nullptr && c8 == 0) lse[row] = wsum > 0.0f ? m + logf(wsum) : -INFINITY;
+  if (lse != nullptr && c8 == 0) lse[row] = wsum == 0.0f ? -INFINITY : m + logf(wsum);
 }
 
 // ---- planning kernel: validate the offsets, order segments by key count (the cost of each of
