@@ -90,7 +90,7 @@ int64_t ts_qk_rope_bwd_workspace(int32_t T, int32_t q_heads, int32_t k_heads, in
  * queries and keys, and of ts_attn_fwd, with offsets L apart): segment s's queries
  * [cu_seqlens_q[s], cu_seqlens_q[s+1]) over its keys [cu_seqlens_k[s], cu_seqlens_k[s+1]).  From the result
  * o, its log-sum-exp lse and the gradient d_o of o:
- *   P[t,j] = exp(scale * <q[t], k[j]> - lse[t])       (computed again, never stored)
+ *   P[t,j] = exp(scale * <q[t], k[j]> - lse[t])       (computed again, never stored; 0 where lse[t] is -infinity)
  *   D[t]   = <d_o[t], o[t]>
  *   dv[j]  = sum_t P[t,j] * d_o[t]
  *   S[t,j] = P[t,j] * (<d_o[t], v[j]> - D[t])

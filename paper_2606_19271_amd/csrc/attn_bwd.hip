@@ -613,7 +613,9 @@ __global__ __launch_bounds__(kPlanThreads) void bwd_prepare_kernel(const __bf16*
 #pragma unroll
     for (int s = kLanes / 2; s > 0; s >>= 1) sum += __shfl_xor(sum, s);
     if (i == 0) {
-      stat[(int64_t)h * T + t] = -lse[(int64_t)t * H + h] * inv;
+      // of a query that saw no key, or none but of score -infinity, P is 0: its exponent is -infinity whatever the score
+      const float l = lse[(int64_t)t * H + h];
+      stat[(int64_t)h * T + t] = l == -INFINITY ? __builtin_copysignf(INFINITY, -inv) : -l * inv;
       stat[((int64_t)H + h) * T + t] = -sum;
     }
   }

@@ -143,3 +143,38 @@ def test_rows_past_the_end_are_nobody_s(d):
     q2, k2, v2 = (torch.cat([x, torch.full_like(x, math.nan)]) for x in (q, k, v))
     two = ts.ts_attn_fwd_kvcache(q2, k2, v2, cu[2], cu[3], 45, 333, return_lse=True, num_splits=1)
     assert all(same_bits(a, b[:45]) for a, b in zip(one, two)) and one[1].isfinite().all()
+
+
+@pytest.mark.parametrize("splits", [0, 1, 3])
+@pytest.mark.parametrize("scale", [None, -0.1])
+@pytest.mark.parametrize("d", [64, 128])
+def test_gradients_of_queries_that_see_nothing(d, scale, splits):
+    """A log-sum-exp of -infinity, as the forward calls give it where all scores are, or as a caller marks rows with it: the row takes part
+    in nothing.  In a segment whose keys all are hidden dk and dv are 0, and dq but in the hiding channel, where it is 0 times
+    infinity; rows that the caller marks have dq = 0 and leave the others' gradients as they are without them."""
+    say("see nothing", d, scale, splits)
+    lq, lk, H = [130, 77, 40], [190, 93, 300], 2
+    q, k, v = inputs(lq, lk, H, d, range(190, 283), 97)
+    if scale is not None:
+        q[..., 3] = -q[..., 3]
+    d_o = normal(rng(98), sum(lq), H, d).bfloat16()
+    cu_q, cu_k = (torch.tensor(R.offsets(n), dtype=torch.int32, device="cuda") for n in (lq, lk))
+    o, lse = ts.ts_attn_fwd_kvcache(q, k, v, cu_q, cu_k, 130, 300, scale=scale, return_lse=True)
+    assert (lse[130:207] == -math.inf).all() and not o[130:207].any() and lse[:130].isfinite().all() and lse[207:].isfinite().all()
+    marked = [5, 100, 129, 210]
+    o, lse = o.clone(), lse.clone()
+    o[marked], lse[marked] = 0, -math.inf
+    dq, dk, dv = ts.ts_attn_bwd(d_o, q, k, v, o, lse, cu_q, cu_k, 130, 300, scale=scale, num_splits=splits)
+    assert not dk[190:283].any() and not dv[190:283].any() and dq[130:207, :, 3].isnan().all()
+    dq = dq.clone()
+    dq[130:207, :, 3] = 0
+    assert not dq[130:207].any() and not dq[marked].any()
+    use = ts.default_scale(d) if scale is None else scale
+    keep = torch.ones(sum(lq), dtype=torch.bool, device="cuda")
+    keep[marked] = keep[130:207] = False
+    for a, b, c, e in ((0, 130, 0, 190), (207, 247, 283, 583)):
+        rows = [x[a:b][keep[a:b]].double() for x in (d_o, q, o, lse)]
+        for h in range(H):
+            ref, tol = R.attn_bwd(rows[0][:, h], rows[1][:, h], k[c:e, h].double(), v[c:e, h].double(), rows[2][:, h], rows[3][:, h], use)
+            for name, x, y, t in zip(("dq", "dk", "dv"), (dq[a:b, h][keep[a:b]], dk[c:e, h], dv[c:e, h]), ref, tol):
+                near(name, x, y, t)
