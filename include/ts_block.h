@@ -96,10 +96,8 @@ int64_t ts_qk_rope_bwd_workspace(int32_t T, int32_t q_heads, int32_t k_heads, in
  *   S[t,j] = P[t,j] * (<d_o[t], v[j]> - D[t])
  *   dq[t]  = scale * sum_j S[t,j] * k[j]
  *   dk[j]  = scale * sum_t S[t,j] * q[t]
- * per head.  P and S are formed in 32 bits and rounded to bfloat16 for the products they enter; sums are 32 bits.
- * dq is off by the sum of (rounded S - S) * k.  Of the keys' common part m that is taken off again, (sum of rounded S - S) * m:
- * m is, channel by channel, 0 if the keys of the item's range have both signs there, else the middle of those nearest to
- * and furthest from 0, or twice the nearest if that is less, so that no key is further from m than from 0.
+ * per head.  P and S are formed in 32 bits and rounded to bfloat16 for the products they enter, S of dq in two parts (its
+ * rounded value and the rounded rest); sums are 32 bits.
  *  q, o, d_o, dq   bfloat16 [total_q][H][d];  k, v, dk, dv  bfloat16 [total_k][H][d];  lse  float32 [total_q][H]
  *  cu_seqlens_q/k  int32, nseq + 1 entries each, read on the device only, under the rules of ts_attn_fwd_kvcache: they
  *                  start at 0, do not descend, end at total_q / total_k, and no segment is longer than its

@@ -23,7 +23,14 @@ using namespace tsattn;
 // where P and R, as they lie, are the B operands of the last two products, whose A operands are transposed reads of
 // the same LDS rows.  Where the streamed rows are queries, S and T start at their -lse / scale and -D, which come with them.
 //
-// Both gradients of a score tile recompute S and T: seven products of a tile in all where five would do if dq were added up
+// R is rounded to bfloat16 once for dk, and for dq taken in two parts, R and what its rounding leaves, each times the keys from the
+// same registers.  The R of a query sum to 0 but for D's rounding, so that dq loses what its keys have in common while
+// an error of R does not: with one part dq is off by 0.0029 of its norm where the keys' mean is as large as their
+// spread, by 0.013 where it is 8 times that, with two by 0.0017, its own rounding.  (Less the sum of R's errors times a mean
+// of keys it would be 0.0024, 10 % sooner, but keys of no weight that lie far out, as masked ones do, then put it off by more
+// than its norm, and with a mean that no such key can move the gain is gone where signs are mixed.)
+//
+// Both gradients of a score tile recompute S and T: eight products of a tile in all where six would do if dq were added up
 // in memory across the key tiles.  Those sums would have to be atomic, in no fixed order, or wait for each other, and the scores
 // would have to be laid out anew for them through LDS, which has no time to spare (a read of 1 KiB feeds one MFMA of a SIMD:
 // 8 clocks of the LDS' 8).
@@ -87,7 +94,6 @@ __device__ __forceinline__ Item find_item(const BwdTile& t, int at, int heads, i
 }
 
 typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
-typedef __attribute__((address_space(3))) f32x2 lds_f32x2;
 
 // The LDS reads of a step take their address as a restrict pointer: the compiler then knows that they do not wait for the
 // DMA of the steps ahead.
@@ -113,29 +119,6 @@ __device__ __forceinline__ f32x16 row_statistics(const lds_char* __restrict__ x,
     for (int r = 0; r < 4; ++r) to[4 * g + r] = y[r];
   }
   return to;
-}
-
-// Of bfloat16 values, as 16-bit integers with a sign, the least and the most, of two channels at once.  Of positive ones these are the
-// smallest and the largest; negative ones come before them, those nearest to 0 first.
-typedef short s16x2 __attribute__((ext_vector_type(2)));
-typedef __attribute__((address_space(3))) s16x2 lds_s16x2;
-struct Extremes {
-  s16x2 least = {32767, 32767}, most = {-32768, -32768};
-  __device__ __forceinline__ void add(s16x2 x) { add(x, x); }
-  __device__ __forceinline__ void add(s16x2 x, s16x2 y) {
-    least = __builtin_elementwise_min(least, x);
-    most = __builtin_elementwise_max(most, y);
-  }
-};
-
-__device__ __forceinline__ s16x2 two_channels(const lds_char* __restrict__ x) { return *(const lds_s16x2*)x; }
-
-// m of a channel from its extremes: 0 where there are both signs; else `least` is the nearest to 0.
-__device__ __forceinline__ float common_part(short least, short most) {
-  if ((least ^ most) < 0) return 0.0f;
-  const float s = __uint_as_float((unsigned)(unsigned short)least << 16), l = __uint_as_float((unsigned)(unsigned short)most << 16);
-  const float middle = 0.5f * s + 0.5f * l;
-  return fabsf(middle) < fabsf(2.0f * s) ? middle : 2.0f * s;
 }
 
 // f(0), f(1) .. f(N - 1), each a constant of its type, for a loop that is too long to be unrolled by the compiler.
@@ -301,38 +284,13 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
     const float c = a.c;
     const bool active = row0 < held_len;
 
-    // dq: the sums over the keys of R as it is and as it is rounded.  Rounding makes dq off by the sum of (rounded R - R) k; keys that
-    // have much in common, as those of a trained model's outlier channels do, add that part up while the gradient, whose
-    // R sum to next to nothing, loses it.  So the difference of the two sums times a vector m is taken off again at the end, which
-    // leaves the sum of (rounded R - R) (k - m).  No m may bring in keys that a query gives no weight: a mean of few or of all of them does,
-    // where some stand far out (32 keys 8 times the spread away: dq off by 0.014 of its norm instead of 0.0024).  So a channel
-    // has an m only where all keys of the range have one sign: the middle of its smallest and its largest, but twice the
-    // smallest at most, which makes |k - m| <= |k| for every key.  Of keys whose mean is 8 times their spread dq is off by 0.0024 of
-    // its norm instead of 0.013 (0.0017 is its own rounding), of 4 times by 0.005 instead of 0.007; where signs are mixed, as with
-    // a mean like the spread, it is off by what it would be, 0.0029.  The sums cost 2 % at d = 128 and 4 % at d = 64, the smallest
-    // and largest 2 % (32760 x 32760 x 12 heads 18.2 ms instead of 17.9).
-    float exact = 0;
-    f32x4 rounded = {};  // (every element: the lane's query's, by the matrix core)
-    const bf16x8 sel = row_sum_selector(lane);
-    Extremes least_most;
-    // a thread looks at two channels of the same eight of a step's keys
-    constexpr int kTwos = D / 2, kApart = G::kThreads / kTwos;
-    static_assert(8 * kApart == kBN && kApart % 4 == 0, "a workgroup's threads take a step's keys in eight");
-    const int key = threadIdx.x / kTwos, key_lane = G::row_offset(key) + 4 * (threadIdx.x % kTwos);
-    auto of_key = [&](const lds_char* stage, int u) { return two_channels(stage + key_lane + u * (kApart / 4 * G::kGroup)); };
-    auto add_key = [&](s16x2 x, int u, auto ragged, int left) {
-      const bool is = !decltype(ragged)::value || key + u * kApart < left;
-      least_most.add(is ? x : least_most.least, is ? x : least_most.most);
-    };
-
     // One step.  The order of its products and reads is pinned: each operand is read a product before it is used (more ahead
     // measured the same), and the vector work on a product's result goes between products that do not wait for it.  Left to the
-    // compiler's order 32760 x 32760 x 12 heads took 17.75 ms instead of 17.4, 16380 x 16380 x 24 heads of d = 64 5.1 instead of
-    // 5.0 (both without the sums of R below).  ragged: rows from `left` on are past the segment's end; their P and R are 0.
+    // compiler's order 32760 x 32760 x 12 heads took 2 % longer, as 16380 x 16380 x 24 heads of d = 64 did (before R came in two
+    // parts).  ragged: rows from `left` on are past the segment's end; their P and R are 0.
     constexpr int kM = D / 16;  // MFMAs of a product
     constexpr bool kPair = !kKeys && kBN >= 64;  // dq: two blocks at a time
     constexpr int kBlocks = kBN / (kPair ? 64 : 32), kPer = (kKeys ? 4 : kPair ? 6 : 3) * kM, kAll = kBlocks * kPer;
-    static_assert(kKeys || kBlocks == 1, "dq: a step's keys are one block, or two at a time");
     auto step_of = [&](const lds_char* stage, auto ragged, int left) {
       const lds_char* const xr = stage + row_lane;
       const lds_char* const xt = stage + tr_lane;
@@ -350,7 +308,7 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
         return columns_operand<G::kGroup>(xt + block + column);
       };
       f32x16 s[kKeys ? 1 : 2], t[kKeys ? 1 : 2];
-      bf16x8 p[2], ds[kKeys ? 1 : 2][2];
+      bf16x8 p[2], ds[kKeys ? 1 : 2][2], dl[kKeys ? 1 : 2][2];
       auto weight = [&](int w, int r, int row) {  // s becomes P
         float x = s[w][r];
         x = __builtin_amdgcn_exp2f(kKeys ? x * c : __builtin_fmaf(x, c, la));
@@ -361,8 +319,10 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
       auto residual = [&](int w, int r, int row) {
         float x = s[w][r] * t[w][r];
         if (decltype(ragged)::value && row + 8 * (r >> 2) + 4 * hb + (r & 3) >= left) x = 0.0f;
-        ds[w][r >> 3][r & 7] = (__bf16)x;
-        if (!kKeys) exact = __builtin_fmaf(s[w][r], t[w][r], exact);  // (P is 0 past the end)
+        const __bf16 hi = (__bf16)x;
+        ds[w][r >> 3][r & 7] = hi;
+        // (P is 0 past the end; a fused operation in every kernel, so that all have the same bits)
+        if (!kKeys) dl[w][r >> 3][r & 7] = (__bf16)__builtin_fmaf(s[w][r], t[w][r], -(float)hi);
       };
       // element range of slot m of a phase: nothing in the first, whose product waits for the result
       auto from = [](int m) { return m < 1 ? 0 : 2 * ((8 * (m - 1) + kM - 2) / (kM - 1)); };
@@ -370,7 +330,6 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
         s[0] = row_statistics(st, hb);
         t[0] = row_statistics(st + G::kStatRow, hb);
       }
-      s16x2 of_keys[2];
       bf16x8 next = operand(0);
       for_each(std::make_integer_sequence<int, kAll>{}, [&](auto at) __attribute__((always_inline)) {
         constexpr int i = at, b = i / kPer, phase = i % kPer / kM, m = i % kM;
@@ -394,10 +353,9 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
           const int w = kPair && (phase == 2 || phase == 3 || phase == 5);
           if (phase == 0 || (kPair && phase == 2)) s[w] = mfma32(x, y1[m], m == 0 ? f32x16{} : s[w]);
           else if (phase == 1 || (kPair && phase == 3)) t[w] = mfma32(x, y2[m], m == 0 ? splat(ld) : t[w]);
-          else acc1[m % (D / 32)] = mfma32(x, ds[w][m / (D / 32)], acc1[m % (D / 32)]);
-          if (phase >= (kPair ? 4 : 2) && m == kM - 1) {
-            rounded = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sel, ds[w][0], rounded, 0, 0, 0);
-            rounded = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sel, ds[w][1], rounded, 0, 0, 0);
+          else {
+            acc1[m % (D / 32)] = mfma32(x, ds[w][m / (D / 32)], acc1[m % (D / 32)]);
+            acc1[m % (D / 32)] = mfma32(x, dl[w][m / (D / 32)], acc1[m % (D / 32)]);
           }
 #pragma unroll
           for (int r = from(m); r < from(m + 1); ++r) {
@@ -409,13 +367,6 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
           if (!kPair && phase == 1 && m == kM - 1) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) residual(0, r, 32 * b);
-          }
-          // the keys' extremes, in the last phase, which has no other vector work; read a product before their use too
-          if (i + kM >= kAll) add_key(of_keys[0], m, ragged, left);
-          if (kM == 4 && i + kM >= kAll) add_key(of_keys[1], m + 4, ragged, left);
-          if (i + kM + 1 >= kAll && i + 1 < kAll) {
-            of_keys[0] = of_key(stage, (i + 1) % kM);
-            if (kM == 4) of_keys[1] = of_key(stage, (i + 1) % kM + 4);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -436,55 +387,16 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
       for (int j = 0; j < whole; ++j) step_of(open_step(j), std::false_type{}, kBN);
       if (whole < steps) step_of(open_step(whole), std::true_type{}, len - (begin + whole) * kBN);
     } else {
-      for (int j = 0; j < steps; ++j) {
-        const lds_char* const stage = open_step(j);
-        if (!kKeys) {
-#pragma unroll
-          for (int u = 0; u < 8; ++u) add_key(of_key(stage, u), u, std::true_type{}, len - (begin + j) * kBN);
-        }
-      }
+      for (int j = 0; j < steps; ++j) open_step(j);
     }
     wait_lds();
     wait_vmem<0>();
     block_sync();
-    if constexpr (!kKeys) {
-      // m, in the stage that no results go through: every thread's extremes, then those of all, and m of two channels to a thread
-      lds_char* const shared = lds + slot * G::kStage;
-      static_assert(G::kThreads * 8 + D * 4 <= G::kStage, "extremes and m fit a stage");
-      *(lds_s16x2*)(shared + 4 * threadIdx.x) = least_most.least;
-      *(lds_s16x2*)(shared + 4 * (G::kThreads + threadIdx.x)) = least_most.most;
-      lds_char* const m_at = shared + 8 * G::kThreads;
-      __syncthreads();
-      if (threadIdx.x < kTwos) {
-#pragma unroll
-        for (int i = 1; i < kApart; ++i) {
-          const lds_char* const x = shared + 4 * (threadIdx.x + i * kTwos);
-          least_most.add(two_channels(x), two_channels(x + 4 * G::kThreads));
-        }
-        *(lds_f32x2*)(m_at + 8 * threadIdx.x) = f32x2{common_part(least_most.least[0], least_most.most[0]), common_part(least_most.least[1], least_most.most[1])};
-      }
-      __syncthreads();
-      if (active) {
-        const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(exact), __float_as_uint(exact), false, false);
-        exact = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
-        float off = rounded[0] - exact;
-        // that product has query l + 16 beside query l, times 0: where the one is not finite, the other keeps its rounding (and
-        // where its own R are not, neither is acc1)
-        if (!(fabsf(off) < INFINITY)) off = 0;
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) {
-          const f32x16 m = row_statistics(m_at + 128 * db, hb);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc1[db][r] = __builtin_fmaf(-off, m[r], acc1[db][r]);
-        }
-      }
-    }
   }
 
-  // The results: registers 4 g + r of block db are channels 32 db + 8 g + 4 hb + r of the lane's row.  (Where there were steps, LDS
-  // is free but for the stage `slot`, which may still be read.)
-  lds_char* const out = lds + (slot == 0 ? 1 : 0) * G::kStage + wave * kOutWave;
-  static_assert(W * kOutWave <= G::kStage, "the waves' output fits a stage");
+  // The results: registers 4 g + r of block db are channels 32 db + 8 g + 4 hb + r of the lane's row.  (All of LDS is free.)
+  lds_char* const out = lds + wave * kOutWave;
+  static_assert(W * kOutWave <= G::kLds, "the waves' output fits LDS");
   if (n > 1) {
     const int64_t rows = (int64_t)(kKeys ? a.total_k : a.total_q) * a.H * D;
     const int64_t at = w.split * rows + held0;
@@ -555,11 +467,11 @@ __device__ void make_plan(BwdPlan* plan, BwdOffsets f, int n_q, int n_k, int til
     t.tiles = (t.held_len + tile - 1) / tile;
   };
   const bool sorted = lists <= kSorted;
-  if (sorted) {  // by the products of an item: four of a step's rows for dk and dv, three for dq
+  if (sorted) {  // by the rows that stream past an item (as many products of each on either side)
     for (int i = tid; i < lists; i += kPlanThreads) {
       BwdTile t;
       list(i, t);
-      cost[i] = t.tiles ? t.keys ? 4 * (t.str_len / n_k) : 3 * (t.str_len / n_q) : -1;
+      cost[i] = t.tiles ? t.str_len / (t.keys ? n_k : n_q) : -1;
     }
     __syncthreads();
     for (int i = tid; i < lists; i += kPlanThreads) {

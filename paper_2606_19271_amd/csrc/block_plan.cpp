@@ -30,11 +30,11 @@ struct Call {
   int32_t d, tile;
 };
 
-// d = 64 has tiles of 128 rows, three workgroups of four waves to a CU: 16380 x 16380 x 24 heads 4.79 ms, in tiles of 256 (two waves to a
-// SIMD) 5.03.  At d = 128 tiles of 256 rows read the other side half as often (32768 x 32768 x 12 heads 17.4 ms instead of
-// 18.4); where these are fewer than the CUs of an MI355X, those of 128 end sooner: 1024 x 1024 x 12 heads 42 us
-// instead of 49, 256 x 256 x 12 heads 20 instead of 28, 1560 x 1560 x 12 77 instead of 80 (8190 x 8190 x 4, 256 tiles, 398
-// instead of 390).
+// d = 64 has tiles of 128 rows, three workgroups of four waves to a CU (in tiles of 256, two waves to a SIMD, 16380 x 16380 x 24 heads
+// took 5 % longer).  At d = 128 tiles of 256 rows read the other side half as often: 32768 x 32768 x 12 heads 20.8 ms instead of
+// 21.3, 2048 x 2048 x 12 heads 103 us instead of 105, 8190 x 8190 x 4 (256 such tiles) 453 instead of 459; where these are
+// fewer than the CUs of an MI355X, those of 128 end sooner: 1024 x 1024 x 12 heads 42 us instead of 47, 256 x 256 x 12 heads 19
+// instead of 22.
 Call call(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d) {
   const bool large = d == 128 && H * (bwd_tiles(nseq, max_q, total_q, 256) + bwd_tiles(nseq, max_k, total_k, 256)) >= 256;
   const int32_t tile = large ? 256 : 128;
@@ -76,9 +76,11 @@ double ends(int64_t cus, int64_t a_items, double a, int64_t b_items, double b) {
 }  // namespace
 
 // The ranges that the library takes: those whose call ends first by an estimate, in us as measured.  A CU takes `product` of them for
-// the product of a tile and 64 rows (three for dq, four for dk and dv), and at least `alone` of them pass in a workgroup, or as
-// many as those that share its CU take; beside its products an item takes kItem; joining ranges kJoin and, to write and read them, kMegabyte each.  1560 x 32760 x 12
-// heads (d = 128) take 1090 with one range of keys and 950 with three, 1560 x 1560 x 2 heads (d = 64) 34 and 25 with four.
+// the product of a tile and 64 rows (four on either side: of dq the last one is two), and at least `alone` of them pass in a
+// workgroup, or as many as those that share its CU take; beside its products an item takes kItem; joining ranges kJoin and, to write
+// and read them, kMegabyte each.  1560 x 32760 x 12 heads (d = 128) take 1335 us with one range a side and 1076 as chosen, 2730 x
+// 2730 x 12 heads 248 and 192, 1560 x 1560 x 2 heads (d = 64) 33 and 25; none of eleven calls took over 10 % more than the best of eight
+// forced numbers of ranges.
 BwdParts bwd_parts(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, int32_t total_k, int32_t H, int32_t d,
                    int32_t num_splits, int64_t workspace, int32_t cus) {
   const Call c = call(nseq, max_q, max_k, total_q, total_k, H, d);
@@ -97,7 +99,7 @@ BwdParts bwd_parts(int32_t nseq, int32_t max_q, int32_t max_k, int32_t total_q, 
     if (n_q > steps_k) break;
     for (int32_t n_k : {1, 2, 3, 4, 6, 8, 12, 16}) {
       if (n_k > steps_q) break;
-      const int32_t in_q = 3 * ((steps_k + n_q - 1) / n_q), in_k = 4 * ((steps_q + n_k - 1) / n_k);  // products of an item
+      const int32_t in_q = 4 * ((steps_k + n_q - 1) / n_q), in_k = 4 * ((steps_q + n_k - 1) / n_k);  // products of an item
       const double q = product * in_q + kItem, k = product * in_k + kItem;
       double t = in_q > in_k ? ends(cus, items_q * n_q, q, items_k * n_k, k) : ends(cus, items_k * n_k, k, items_q * n_q, q);
       const int64_t beside = std::min<int64_t>(bwd_groups(d, c.tile), (items_q * n_q + items_k * n_k) / cus + 1);

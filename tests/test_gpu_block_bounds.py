@@ -24,7 +24,7 @@ def gpu():
 def bounded(lq, lk, args, scale, splits):
     """ts_attn_bwd of these arguments: every gradient within its bounds.  Returns dq and its definition."""
     got = ts.ts_attn_bwd(*args, scale=scale, num_splits=splits)
-    want = B.packed(*(x.double() for x in args[:6]), R.offsets(lq), R.offsets(lk), scale, splits)
+    want = B.packed(*(x.double() for x in args[:6]), R.offsets(lq), R.offsets(lk), scale)
     for name, x, (ref, tol, most) in zip(("dq", "dk", "dv"), got, want):
         B.check(name, x, ref, tol, most, say)
     return got[0], want[0][0]
@@ -51,7 +51,7 @@ def test_gradients_within_their_bounds(case, splits):
 @pytest.mark.parametrize("mean", [1, 4, 8])
 @pytest.mark.parametrize("lq,lk,H,d", [([300, 500], [1000, 700], 3, 64), ([300, 500], [1000, 700], 3, 128), ([2900, 300], [2048, 2500], 12, 128)])
 def test_keys_with_a_mean(lq, lk, H, d, mean, splits):
-    """In small tiles and in large ones."""
+    """In small tiles and in large ones: what the keys have in common does not go into dq's error."""
     say("mean", lq, lk, H, d, mean, splits)
     g = rng(64)
     q, v, d_o = (normal(g, sum(n), H, d) for n in (lq, lk, lq))
@@ -63,8 +63,8 @@ def test_keys_with_a_mean(lq, lk, H, d, mean, splits):
 @pytest.mark.parametrize("shift", [2, 8, 64])
 @pytest.mark.parametrize("d", [64, 128])
 def test_first_keys_that_stand_apart(d, shift, splits):
-    """The first 32 keys of a segment lie far from the others in every channel and have next to no weight: what dq is off by is the
-    rounding of S times the keys that have weight, not times those."""
+    """The first 32 keys of a segment lie far from the others in every channel and have next to no weight: dq is off by its own
+    rounding whatever they are."""
     say("first keys", d, shift, splits)
     lq, lk, H = [256, 100], [3120, 700], 2
     g = rng(60)
@@ -75,8 +75,8 @@ def test_first_keys_that_stand_apart(d, shift, splits):
     q = 0.3 * q
     q = q - (q * u).sum(-1, keepdim=True) * u / d - 1.2 / math.sqrt(d) * u  # (their scores are -1.2 times the shift)
     dq, ref = within(lq, lk, d, q.bfloat16(), k.bfloat16(), v, d_o, splits)
-    # its own rounding and that of S times the keys' spread, 0.0017 (HALF / sqrt(3) and less) of its norm each, 0.0024 together
-    assert (dq.double() - ref).norm() < 0.0030 * ref.norm()
+    # 0.0017 of its norm, HALF / sqrt(3) = 0.00226 where every element is at the low end of its binade
+    assert (dq.double() - ref).norm() < 0.0020 * ref.norm()
 
 
 @pytest.mark.parametrize("splits", [1, 3])
@@ -94,15 +94,15 @@ def test_keys_that_one_channel_masks(d, share, splits):
     k[hidden, :, 3] = -30000
     dq, ref = within(lq, lk, d, q, k, v, d_o, splits)
     if share < 1:
-        # its own rounding and that of S, HALF / sqrt(3) of its norm each at most; 400 elements, four deviations
-        assert (dq[..., 3].double() - ref[..., 3]).norm() < R.HALF * math.sqrt(2 / 3 * (1 + 4 * math.sqrt(2 / 400))) * ref[..., 3].norm()
+        # its own rounding, HALF / sqrt(3) of its norm at most; 400 elements, four deviations
+        assert (dq[..., 3].double() - ref[..., 3]).norm() < R.HALF * math.sqrt((1 + 4 * math.sqrt(2 / 400)) / 3) * ref[..., 3].norm()
 
 
 @pytest.mark.parametrize("H", [1, 2])
 @pytest.mark.parametrize("d", [64, 128])
-def test_every_key_counts(d, H):
+def test_three_keys_of_weight_anywhere(d, H):
     """64 segments in which all keys but three are 30000 in one channel, and have no weight by it; the three lie at another place of a
-    64-key tile in each segment, the channel is another one, and whoever passes over them has 30000 where they have 1."""
+    64-key tile in each segment, and the channel is another one."""
     say("every key", d, H)
     n, lq, lk = 195, [5] * 64, [195] * 64
     g = rng(62)
