@@ -247,7 +247,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(RopeBwdArgs a, i
   __shared__ float lds[kWaves][2 * kAngleRow];
   __shared__ double sums[kWaves][2 * D];
   double* const sum = sums[threadIdx.x >> 6];
-  for (int ch = lane; ch < 2 * D; ch += 64) sum[ch] = 0;
+  if (at.left <= 0)
+    for (int ch = lane; ch < 2 * D; ch += 64) sum[ch] = 0;
   float wq[16], wk[16], c[8], s[8], sum_q[16] = {}, sum_k[16] = {};
   auto rows = [&](const Rows& q, const Rows& k, const Steps& at, bool& live) {
     const bool is_k = at.g >= groups_q;
@@ -270,6 +271,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(RopeBwdArgs a, i
   load_weights<D>(a.q_weight, j, wq);
   load_weights<D>(a.k_weight, j, wk);
   int chain = 0;
+  bool begun = false;  // whether the wave's sums hold anything
   while (at.left > 0) {
     if (fresh && a.rope.freq) angles<D, kPairs>(a.rope, place(a.rope, at.t), lane, freq, lds[threadIdx.x >> 6], c, s);
     const Steps here = at;
@@ -318,13 +320,18 @@ __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(RopeBwdArgs a, i
         sum_q[i] += __shfl_xor(sum_q[i], o);
         sum_k[i] += __shfl_xor(sum_k[i], o);
       }
-      if (r == 0) {
-        const int ch = (i < 8 ? 8 * j + i : D / 2 + 8 * j + i - 8);
-        sum[ch] += sum_q[i];
-        sum[D + ch] += sum_k[i];
-      }
-      sum_q[i] = sum_k[i] = 0;
     }
+    auto channel = [&](int i) { return (i < 8 ? 0 : D / 2 - 8) + 8 * j + i; };
+    if (r == 0 && !begun) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[channel(i)] = sum_q[i], sum[D + channel(i)] = sum_k[i];
+    } else if (r == 0) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[channel(i)] += sum_q[i], sum[D + channel(i)] += sum_k[i];
+    }
+    begun = true;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum_q[i] = sum_k[i] = 0;
   }
   if (!a.part) return;
   __syncthreads();
