@@ -408,9 +408,9 @@ __device__ __forceinline__ void run_item(const BwdCall& a, const Item& w, lds_ch
   }
 }
 
-// Bound by the matrix cores under the power cap: 32760 x 32760 x 12 heads (d = 128) 18.0 ms, in which its seven products
-// run at 1280 TFLOP/s, what a large library product reaches on the same device (1290); MFMA busy 71 % of 31 M clocks.  16380 x
-// 16380 x 24 heads of d = 64 5.07 ms, 1140 TFLOP/s: exponentials and sums take as many clocks there as the products, which two
+// Bound by the matrix cores under the power cap: 32760 x 32760 x 12 heads (d = 128) 20.2 ms, in which its eight products
+// run at 1300 TFLOP/s, what a large library product reaches on the same device; MFMA busy 68 % of 36.9 M clocks.  16380 x
+// 16380 x 24 heads of d = 64 5.75 ms, 1150 TFLOP/s: exponentials and sums take as many clocks there as the products, which two
 // of the three workgroups of a CU have to hide.  Each CU takes one item after the other; small calls are bound by the
 // last ones, and by what each takes beside its products, 3 to 5 us (1024 x 1024 x 2 heads of d = 64: 12 us in this kernel).
 template <int D, int W>
